@@ -1,5 +1,5 @@
-"""ctypes binding of include/lqsgd.h.  Argument marshalling only: every step of
-the compressor runs in the HIP library.  torch is used for device memory and
+"""ctypes binding of include/lqsgd.h and include/lqsgd_linear.h.  Argument marshalling only: every step of
+the compressor and of the linear layer runs in the HIP library.  torch is used for device memory and
 the stream handle, nothing else."""
 from __future__ import annotations
 
@@ -31,6 +31,15 @@ SYMBOLS = [
     "lqsgd_set_factor", "lqsgd_wire_bytes", "lqsgd_plan_query", "lqsgd_plan_tiles",
     "lqsgd_timing_enable", "lqsgd_timing_read", "lqsgd_kernel_name", "lqsgd_launched_kernel", "lqsgd_step_static",
 ]
+# ... and lqsgd_linear.h
+LINEAR_SYMBOLS = [
+    "lqsgd_linear_create", "lqsgd_linear_destroy", "lqsgd_linear_synchronize", "lqsgd_linear_last_error", "lqsgd_checkpoint_stride",
+    "lqsgd_checkpoint_save", "lqsgd_checkpoint_load", "lqsgd_linear_forward", "lqsgd_linear_activation_backward",
+    "lqsgd_linear_input_grad", "lqsgd_linear_weight_grad",
+]
+TYPE_F32, TYPE_BF16, TYPE_F16 = range(3)
+ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
+CHECKPOINT_GROUP = 32
 
 
 class LqsgdError(RuntimeError):
@@ -102,6 +111,19 @@ def lib():
     L.lqsgd_kernel_name.restype = C.c_char_p
     L.lqsgd_launched_kernel.argtypes = [vp, i32]
     L.lqsgd_launched_kernel.restype = C.c_char_p
+    L.lqsgd_linear_create.argtypes = [vp, C.POINTER(vp)]
+    L.lqsgd_linear_destroy.argtypes = [vp]
+    L.lqsgd_linear_synchronize.argtypes = [vp]
+    L.lqsgd_linear_last_error.argtypes = [vp]
+    L.lqsgd_linear_last_error.restype = C.c_char_p
+    L.lqsgd_checkpoint_stride.argtypes = [i32]
+    L.lqsgd_checkpoint_stride.restype = i64
+    L.lqsgd_checkpoint_save.argtypes = [vp, i32, i64, i32, vp, i64, vp, vp]
+    L.lqsgd_checkpoint_load.argtypes = [vp, i32, i64, i32, vp, vp, vp, i64]
+    L.lqsgd_linear_forward.argtypes = [vp, i32, i32, i64, i32, i32, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, vp, vp, vp]
+    L.lqsgd_linear_activation_backward.argtypes = [vp, i32, i32, i64, i32, vp, i64, vp, vp, vp, i64, vp, i32]
+    L.lqsgd_linear_input_grad.argtypes = [vp, i32, i64, i32, i32, vp, i64, vp, i64, vp, i64]
+    L.lqsgd_linear_weight_grad.argtypes = [vp, i32, i64, i32, i32, vp, i64, vp, vp, i32, vp, i64, i32]
     _lib = L
     return L
 
@@ -366,3 +388,208 @@ def step_static(layers, rank, bits_p, bits_q, workers, alpha, flags, grads, resi
 
 def kernel_name(k: int) -> str:
     return lib().lqsgd_kernel_name(k).decode()
+
+
+# -- the linear layer --------------------------------------------------------
+class Checkpoint:
+    """A samples x features tensor kept in 8 bits, as include/lqsgd_linear.h lays it out: `codes` (int8, samples x the features rounded
+    up to groups of 32) and `exponents` (uint8, samples x groups)."""
+    __slots__ = ("codes", "exponents", "features")
+
+    def __init__(self, codes, exponents, features):
+        self.codes, self.exponents, self.features = codes, exponents, int(features)
+
+    @classmethod
+    def empty(cls, samples, features, device="cuda"):
+        import torch
+        groups = -(-int(features) // CHECKPOINT_GROUP)
+        return cls(torch.empty((samples, groups * CHECKPOINT_GROUP), dtype=torch.int8, device=device),
+                   torch.empty((samples, groups), dtype=torch.uint8, device=device), features)
+
+    @property
+    def nbytes(self):
+        return self.codes.numel() + self.exponents.numel()
+
+
+class LinearOps:
+    """One lqsgd_linear context: the forward and backward passes of linear layers on torch CUDA tensors (float32, bfloat16 or float16;
+    two-dimensional, the elements of a row contiguous, rows at any stride).  Every call checks shapes, types and devices on the host
+    and enqueues kernels on the stream that was current at construction; it raises where another stream is current, since the outputs
+    that it allocates would belong to that one.  Tensors made on other streams are the caller's to order, as with torch's own calls."""
+
+    def __init__(self):
+        import torch
+        if not torch.cuda.is_available():
+            raise RuntimeError("no GPU visible: the linear layer has no CPU path")
+        self._torch = torch
+        self._types = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16, torch.float16: TYPE_F16}
+        self._h = C.c_void_p()
+        self.device = torch.device("cuda", torch.cuda.current_device())
+        self.stream_handle = int(torch.cuda.current_stream().cuda_stream)
+        self._L = lib()
+        rc = self._L.lqsgd_linear_create(C.c_void_p(self.stream_handle), C.byref(self._h))
+        if rc:
+            self._h = C.c_void_p()
+            raise LqsgdError(rc, self._L.lqsgd_linear_last_error(None).decode())
+
+    # -- helpers ---------------------------------------------------------
+    def _check(self, rc):
+        if rc:
+            raise LqsgdError(rc, self._L.lqsgd_linear_last_error(self._h).decode())
+
+    def _begin(self):
+        if not self._h:
+            raise LqsgdError(ESTATE, "the context is closed")
+        if self._torch.cuda.current_stream(self.device).cuda_stream != self.stream_handle:
+            raise LqsgdError(ESTATE, "the current stream is not the one this context was made on")
+
+    def _bad(self, what, t):
+        raise LqsgdError(ESHAPE, "%s: %s" % (what, "%s %s on %s, strides %s" % (t.dtype, tuple(t.shape), t.device, t.stride())
+                                             if isinstance(t, self._torch.Tensor) else type(t).__name__))
+
+    def _matrix(self, what, t, dtype=None, rows=None, cols=None):
+        """The distance between rows of a two-dimensional tensor that the kernels take as it is."""
+        if not isinstance(t, self._torch.Tensor) or t.dim() != 2 or t.device != self.device:
+            self._bad("%s has to be a two-dimensional tensor on %s" % (what, self.device), t)
+        m, n = t.shape
+        if t.dtype is not dtype if dtype is not None else t.dtype not in self._types:
+            self._bad("%s has the wrong type" % what, t)
+        if (rows is not None and m != rows) or (cols is not None and n != cols):
+            self._bad("%s has the wrong shape, %s x %s wanted" % (what, rows, cols), t)
+        ld, step = t.stride()
+        if step != 1 and n > 1:
+            self._bad("%s: the elements of a row have to be contiguous" % what, t)
+        return ld if m > 1 else max(n, 1)
+
+    def _vector(self, what, t, dtype, n):
+        if not isinstance(t, self._torch.Tensor) or t.device != self.device or t.dtype is not dtype or tuple(t.shape) != (n,) or \
+                not t.is_contiguous():
+            self._bad("%s has to be a contiguous vector of %d %s" % (what, n, dtype), t)
+        return t.data_ptr()
+
+    def _held(self, what, c, samples, features):
+        torch = self._torch
+        if not isinstance(c, Checkpoint):
+            raise LqsgdError(EINVAL, "%s has to be a Checkpoint" % what)
+        groups = -(-features // CHECKPOINT_GROUP)
+        if c.features != features:
+            raise LqsgdError(ESHAPE, "%s has %d features, %d wanted" % (what, c.features, features))
+        for t, dtype, n in ((c.codes, torch.int8, groups * CHECKPOINT_GROUP), (c.exponents, torch.uint8, groups)):
+            if t.dtype is not dtype or tuple(t.shape) != (samples, n) or t.device != self.device or not t.is_contiguous():
+                self._bad("%s: contiguous %s of %d x %d wanted" % (what, dtype, samples, n), t)
+        return c.codes.data_ptr(), c.exponents.data_ptr()
+
+    def close(self):
+        if self._h:
+            self._L.lqsgd_linear_destroy(self._h)
+            self._h = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def synchronize(self):
+        self._check(self._L.lqsgd_linear_synchronize(self._h))
+
+    # -- checkpoints -----------------------------------------------------
+    def save(self, x, out=None):
+        """x in 8 bits."""
+        self._begin()
+        ld = self._matrix("x", x)
+        m, n = x.shape
+        if out is None:
+            out = Checkpoint.empty(m, n, self.device)
+        codes, exps = self._held("out", out, m, n)
+        self._check(self._L.lqsgd_checkpoint_save(self._h, self._types[x.dtype], m, n, x.data_ptr(), ld, codes, exps))
+        return out
+
+    def load(self, held, dtype=None, out=None):
+        """The tensor that a checkpoint stands for, in `dtype` (default: out's, else bfloat16)."""
+        self._begin()
+        if not isinstance(held, Checkpoint):
+            raise LqsgdError(EINVAL, "held has to be a Checkpoint")
+        m, n = held.codes.shape[0], held.features
+        codes, exps = self._held("held", held, m, n)
+        if out is None:
+            out = self._torch.empty((m, n), dtype=dtype or self._torch.bfloat16, device=self.device)
+        ld = self._matrix("out", out, dtype, m, n)
+        self._check(self._L.lqsgd_checkpoint_load(self._h, self._types[out.dtype], m, n, codes, exps, out.data_ptr(), ld))
+        return out
+
+    # -- forward ---------------------------------------------------------
+    def forward(self, x, w, bias=None, residual=None, act="none", out=None, save_z=None, save_y=None):
+        """act(x w^T + bias) + residual.  save_z, save_y: Checkpoints of samples x rows that receive z and y as well."""
+        self._begin()
+        ldx = self._matrix("x", x)
+        m, k = x.shape
+        ldw = self._matrix("w", w, x.dtype, None, k)
+        n = w.shape[0]
+        if act not in ACTS:
+            raise LqsgdError(EINVAL, "unknown activation %r" % (act,))
+        b = self._vector("bias", bias, x.dtype, n) if bias is not None else None
+        r, ldr = (residual.data_ptr(), self._matrix("residual", residual, x.dtype, m, n)) if residual is not None else (None, 0)
+        if out is None:
+            out = self._torch.empty((m, n), dtype=x.dtype, device=self.device)
+        ldy = self._matrix("out", out, x.dtype, m, n)
+        zc, ze = self._held("save_z", save_z, m, n) if save_z is not None else (None, None)
+        yc, ye = self._held("save_y", save_y, m, n) if save_y is not None else (None, None)
+        self._check(self._L.lqsgd_linear_forward(self._h, self._types[x.dtype], ACTS[act], m, n, k, x.data_ptr(), ldx, w.data_ptr(), ldw,
+                                                 b, r, ldr, out.data_ptr(), ldy, zc, ze, yc, ye))
+        return out
+
+    # -- backward --------------------------------------------------------
+    def activation_backward(self, dy, z=None, act="none", dz=None, dbias=None, accumulate=False, want_dz=True, want_dbias=True):
+        """(dz, dbias) of dy and the checkpoint z (not needed without an activation); what is not wanted is None."""
+        self._begin()
+        lddy = self._matrix("dy", dy)
+        m, n = dy.shape
+        if act not in ACTS:
+            raise LqsgdError(EINVAL, "unknown activation %r" % (act,))
+        if z is None and act != "none":
+            raise LqsgdError(EINVAL, "the activation's backward needs the checkpoint of z")
+        zc, ze = self._held("z", z, m, n) if z is not None else (None, None)
+        if dz is None and want_dz:
+            dz = self._torch.empty((m, n), dtype=dy.dtype, device=self.device)
+        lddz = self._matrix("dz", dz, dy.dtype, m, n) if dz is not None else 0
+        if dbias is None and want_dbias:
+            if accumulate:
+                raise LqsgdError(EINVAL, "accumulate needs the dbias to add to")
+            dbias = self._torch.empty(n, dtype=self._torch.float32, device=self.device)
+        db = self._vector("dbias", dbias, self._torch.float32, n) if dbias is not None else None
+        self._check(self._L.lqsgd_linear_activation_backward(self._h, self._types[dy.dtype], ACTS[act], m, n, dy.data_ptr(), lddy, zc, ze,
+                                                             dz.data_ptr() if dz is not None else None, lddz, db, 1 if accumulate else 0))
+        return dz, dbias
+
+    def input_grad(self, dz, w, out=None):
+        """dz w."""
+        self._begin()
+        lddz = self._matrix("dz", dz)
+        m, n = dz.shape
+        ldw = self._matrix("w", w, dz.dtype, n, None)
+        k = w.shape[1]
+        if out is None:
+            out = self._torch.empty((m, k), dtype=dz.dtype, device=self.device)
+        lddx = self._matrix("out", out, dz.dtype, m, k)
+        self._check(self._L.lqsgd_linear_input_grad(self._h, self._types[dz.dtype], m, n, k, dz.data_ptr(), lddz, w.data_ptr(), ldw,
+                                                    out.data_ptr(), lddx))
+        return out
+
+    def weight_grad(self, dz, x, out=None, dtype=None, accumulate=False):
+        """dz^T x^ of the checkpoint x, in float32 or bfloat16 (`dtype`; default: out's, else float32): a gradient for Compressor.step."""
+        self._begin()
+        lddz = self._matrix("dz", dz)
+        m, n = dz.shape
+        if not isinstance(x, Checkpoint):
+            raise LqsgdError(EINVAL, "x has to be a Checkpoint")
+        k = x.features
+        xc, xe = self._held("x", x, m, k)
+        if out is None:
+            if accumulate:
+                raise LqsgdError(EINVAL, "accumulate needs the gradient to add to")
+            out = self._torch.empty((n, k), dtype=dtype or self._torch.float32, device=self.device)
+        lddw = self._matrix("out", out, dtype, n, k)
+        self._check(self._L.lqsgd_linear_weight_grad(self._h, self._types[dz.dtype], m, n, k, dz.data_ptr(), lddz, xc, xe,
+                                                     self._types[out.dtype], out.data_ptr(), lddw, 1 if accumulate else 0))
+        return out

@@ -10,8 +10,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liblqsgd.so")
-SOURCES = ["lqsgd_plan.cpp", "lqsgd_api.cpp", "lqsgd_kernels.hip"]
-KERNEL_PARTS = 6        # the kernel file is compiled in this many parts side by side (LQSGD_PART in the file)
+SOURCES = ["lqsgd_plan.cpp", "lqsgd_api.cpp", "lqsgd_kernels.hip", "lqsgd_linear_api.cpp", "lqsgd_linear.hip"]
+KERNEL_PARTS = {"lqsgd_kernels.hip": 6, "lqsgd_linear.hip": 1}   # parts that a kernel file is compiled in side by side (LQSGD_PART in the file)
 
 
 def hipcc() -> str:
@@ -35,7 +35,7 @@ def build(verbose: bool = True, extra=(), out: str = LIB) -> str:
     dev = ["--offload-arch=gfx950", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
     procs = []
     units = [(s, None) for s in SOURCES if not s.endswith(".hip")]
-    units += [(s, k) for s in SOURCES if s.endswith(".hip") for k in range(KERNEL_PARTS)]
+    units += [(s, k) for s in SOURCES if s.endswith(".hip") for k in range(KERNEL_PARTS[s])]
     for src, part in units:
         obj = os.path.join(bdir, os.path.splitext(src)[0] + ("" if part is None else "_%d" % part) + ".o")
         objs.append(obj)
@@ -61,12 +61,12 @@ def build(verbose: bool = True, extra=(), out: str = LIB) -> str:
 def build_host_sanitize(verbose: bool = True) -> str:
     """The planner and the argument-checking half of the ABI as a host-only program with
     AddressSanitizer and UndefinedBehaviorSanitizer: lqsgd_plan.cpp and lqsgd_api.cpp compiled for
-    the CPU, the kernel launchers replaced by stand-ins, csrc/host_check.cpp as its main.  No device
+    the CPU (lqsgd_linear_api.cpp too), the kernel launchers replaced by stand-ins, csrc/host_check.cpp as its main.  No device
     code is built or sanitized.  Returns the path of the executable; it needs no GPU."""
     bdir = os.path.join(HERE, "_build")
     os.makedirs(bdir, exist_ok=True)
     out = os.path.join(bdir, "lqsgd_host_check")
-    srcs = [os.path.join(CSRC, f) for f in ("lqsgd_plan.cpp", "lqsgd_api.cpp", "host_check_stubs.cpp", "host_check.cpp")]
+    srcs = [os.path.join(CSRC, f) for f in ("lqsgd_plan.cpp", "lqsgd_api.cpp", "lqsgd_linear_api.cpp", "host_check_stubs.cpp", "host_check.cpp")]
     cmd = [hipcc(), "-O1", "-g", "-std=c++17", "-fno-omit-frame-pointer", "-fsanitize=address,undefined",
            "-fno-sanitize-recover=undefined", "-fno-gpu-sanitize", "-Wall", "-Wno-unused-command-line-argument",
            "-I", os.path.join(ROOT, "include"), "-I", CSRC] + srcs + ["-o", out]

@@ -2,6 +2,7 @@
 // argument checking of the C ABI are linked without any device code.  Nothing here is part of
 // the library; every launcher reports that it cannot run.
 #include "lqsgd_kernels.h"
+#include "lqsgd_linear_kernels.h"
 
 namespace lqsgd {
 
@@ -20,4 +21,14 @@ hipError_t static_scratch(int, void**, void**, void**) { return hipErrorNotSuppo
 hipError_t launch_fill_zero(void*, size_t, hipStream_t) { return hipErrorNotSupported; }
 hipError_t launch_write_pointers(const void**, const void* const*, size_t, hipStream_t) { return hipErrorNotSupported; }
 
+namespace linear {
+
+hipError_t launch_product(int, int, const ProductArgs&, hipStream_t) { return hipErrorNotSupported; }
+hipError_t launch_checkpoint_save(int, int64_t, int32_t, const void*, int64_t, Codes, hipStream_t) { return hipErrorNotSupported; }
+hipError_t launch_checkpoint_load(int, int64_t, int32_t, Codes, void*, int64_t, hipStream_t) { return hipErrorNotSupported; }
+hipError_t launch_activation_backward(int, int, int64_t, int32_t, const void*, int64_t, Codes, void*, int64_t, float*, int, void*, hipStream_t) {
+  return hipErrorNotSupported;
+}
+
+}  // namespace linear
 }  // namespace lqsgd
