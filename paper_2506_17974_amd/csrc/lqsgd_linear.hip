@@ -63,28 +63,42 @@ __device__ inline float normal_cdf(float z, float* density) {
 }
 __device__ inline float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950408889634f * z)); }
 
-__device__ inline float activate(float z, int act) {
-  float d;
-  switch (act) {
-    case kRelu: return z < 0.f ? 0.f : z;           // keeps NaN
-    case kGelu: return z * normal_cdf(z, &d);
-    case kSilu: return z * sigmoid(z);
-    default: return z;
+// One branch for all values: which activation it is, is the same for the whole launch.
+template <int N>
+__device__ inline void activate_all(float (&v)[N], int act) {
+  if (act == kRelu) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = v[k] < 0.f ? 0.f : v[k];           // keeps NaN
+  } else if (act == kGelu) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      float g;
+      v[k] *= normal_cdf(v[k], &g);
+    }
+  } else if (act == kSilu) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] *= sigmoid(v[k]);
   }
 }
-__device__ inline float slope(float z, int act) {
-  switch (act) {
-    case kRelu: return z > 0.f ? 1.f : z == z ? 0.f : z;
-    case kGelu: {
+// d *= act'(z)
+template <int N>
+__device__ inline void times_slope(float (&d)[N], const float (&z)[N], int act) {
+  if (act == kRelu) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) d[k] *= z[k] > 0.f ? 1.f : z[k] == z[k] ? 0.f : z[k];
+  } else if (act == kGelu) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
       float g;
-      const float c = normal_cdf(z, &g);
-      return fmaf(0.39894228040143268f * z, g, c);
+      const float c = normal_cdf(z[k], &g);
+      d[k] *= fmaf(0.39894228040143268f * z[k], g, c);
     }
-    case kSilu: {
-      const float s = sigmoid(z);
-      return s * fmaf(z, 1.f - s, 1.f);
+  } else if (act == kSilu) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const float s = sigmoid(z[k]);
+      d[k] *= s * fmaf(z[k], 1.f - s, 1.f);
     }
-    default: return 1.f;
   }
 }
 
@@ -202,11 +216,13 @@ __global__ __launch_bounds__(256) void activation_backward_kernel(const T* dy, i
       if (act != kNone) {
         const uint2 w = *reinterpret_cast<const uint2*>(z.codes + m * ((int64_t)groups * kGroup) + feature);
         const float f = factor_of(z.exponents[m * groups + feature / kGroup]);
+        float zv[kPiece];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          v[k] *= slope((float)(int8_t)(w.x >> (8 * k)) * f, act);
-          v[4 + k] *= slope((float)(int8_t)(w.y >> (8 * k)) * f, act);
+          zv[k] = (float)(int8_t)(w.x >> (8 * k)) * f;
+          zv[4 + k] = (float)(int8_t)(w.y >> (8 * k)) * f;
         }
+        times_slope(v, zv, act);
       }
       if (dz) store_values(dz + m * lddz + feature, v, n);
 #pragma unroll
@@ -304,8 +320,7 @@ __device__ inline void finish(float (&v)[16], const ProductArgs& a, int64_t j, i
     }
   };
   if (a.z.codes) keep(a.z);
-#pragma unroll
-  for (int k = 0; k < 16; ++k) v[k] = activate(v[k], a.act);
+  activate_all(v, a.act);
   if (a.residual) {
     float r[16];
     load_values(r, static_cast<const T*>(a.residual) + j * a.ldr + i0, n);
@@ -320,55 +335,410 @@ __device__ inline void finish(float (&v)[16], const ProductArgs& a, int64_t j, i
   }
 }
 
-// One operand value, 0 outside.
-template <typename T, int PRODUCT>
-__device__ inline float operand_a(const ProductArgs& a, int i, int64_t r) {
-  if (i >= a.ni || r >= a.depth) return 0.f;
-  if (PRODUCT == kForward) return widen(static_cast<const T*>(a.a)[i * a.lda + r]);
-  if (PRODUCT == kInputGrad) return widen(static_cast<const T*>(a.a)[r * a.lda + i]);
-  const int groups = (a.ni + kGroup - 1) / kGroup;
-  const float f = factor_of(a.held.exponents[r * groups + i / kGroup]);
-  return widen(narrow<T>((float)a.held.codes[r * ((int64_t)groups * kGroup) + i] * f));
-}
-template <typename T, int PRODUCT>
-__device__ inline float operand_b(const ProductArgs& a, int64_t j, int64_t r) {
-  if (j >= a.nj || r >= a.depth) return 0.f;
-  return widen(static_cast<const T*>(a.b)[PRODUCT == kWeightGrad ? r * a.ldb + j : j * a.ldb + r]);
+// ---- operands: how a tile gets into LDS, and from there into the matrix instructions ----
+// v_mfma_f32_32x32x16: a lane holds 8 consecutive r of operand row (lane mod 32), r0 = 8 (lane / 32); D comes back with
+// i = 8 (v / 4) + 4 (lane / 32) + v mod 4 in register v, j = lane mod 32.
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef f16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __attribute__((address_space(3))) char lds_char;
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef __attribute__((address_space(3))) s16x8 lds_s16x8;
+typedef __attribute__((address_space(3))) void lds_void;
+
+template <typename E>
+__device__ inline f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
+  if constexpr (std::is_same_v<E, f16>)
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-// 64 x 64 of D to a workgroup, 16 a thread, operands through LDS 16 deep.
-template <typename T, int PRODUCT>
-__global__ __launch_bounds__(256) void product_kernel(ProductArgs a, int tiles_i) {
-  __shared__ float ta[16][68], tb[16][68];
-  const int i0 = (int)(blockIdx.x % tiles_i) * 64;
-  const int64_t j0 = (int64_t)(blockIdx.x / tiles_i) * 64;
-  const int t = threadIdx.x, j = t >> 2, ii = (t & 3) * 16;
-  float v[16] = {};
-  for (int64_t r0 = 0; r0 < a.depth; r0 += 16) {
-    for (int k = t; k < 1024; k += 256) {
-      const int i = PRODUCT == kForward ? k >> 4 : k & 63, ra = PRODUCT == kForward ? k & 15 : k >> 6;
-      ta[ra][i] = operand_a<T, PRODUCT>(a, i0 + i, r0 + ra);
-      const int jj = PRODUCT == kWeightGrad ? k & 63 : k >> 4, rb = PRODUCT == kWeightGrad ? k >> 6 : k & 15;
-      tb[rb][jj] = operand_b<T, PRODUCT>(a, j0 + jj, r0 + rb);
-    }
-    __syncthreads();
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const float b = tb[r][j];
-#pragma unroll
-      for (int k = 0; k < 16; ++k) v[k] = fmaf(ta[r][ii + k], b, v[k]);
-    }
-    __syncthreads();
+enum Order {
+  kDepthRuns = 0,      // memory rows are operand rows, r contiguous: LDS rows too
+  kIndexRuns = 1,      // memory rows are values of r, operand rows contiguous: LDS rows hold one r, read through the transposing load
+  kHeld = 2            // kIndexRuns from a checkpoint
+};
+
+// A tile of N operand rows x K values of r, 16-bit elements in chunks of 8 (16 bytes), LDS rows end to end.  Chunks change places
+// within a row so that what one instruction reads lies in different banks, whether it is served 128 or 256 bytes at a time:
+//   kDepthRuns: ds_read_b128 of one chunk of 32 rows;  kIndexRuns: ds_read_b64_tr_b16 of 4 values of r x 16 or 32 rows.
+template <int ORDER, int N, int K>
+struct Tile {
+  static constexpr int row_chunks = ORDER == kDepthRuns ? K / 8 : N / 8;
+  static constexpr int rows = ORDER == kDepthRuns ? N : K;
+  static constexpr int chunks = row_chunks * rows;
+  static constexpr int bytes = chunks * 16;
+  __device__ static inline int moved(int row) {
+    if (ORDER != kDepthRuns) return (2 * (row & 1) + 5 * (row >> 1 & 1)) << 1;
+    if (row_chunks == 8) return (row & 7) ^ (row >> 3 & 1);
+    return (row >> 1 & 3) ^ (row >> 3 & 1);
   }
-  finish<T, PRODUCT>(v, a, j0 + j, i0 + ii, j0 + j < a.nj, 1);
+  __device__ static inline int place(int row, int chunk) { return (row * row_chunks + (chunk ^ moved(row))) * 16; }
+  // The 8 elements that a lane holds of rows n0 .. n0 + 31 and r = r0 .. r0 + 15 (n0 a multiple of 32, r0 of 16).
+  __device__ static inline s16x8 fragment(const lds_char* tile, int n0, int r0, int lane) {
+    if constexpr (ORDER == kDepthRuns) {
+      return *reinterpret_cast<const lds_s16x8*>(tile + place(n0 + (lane & 31), r0 / 8 + (lane >> 5)));
+    } else {
+      // each 16 lanes read 4 values of r x 16 rows and get them back by rows
+      const int r = r0 + 8 * (lane >> 5) + (lane >> 2 & 3), n = n0 + (lane & 16) + 4 * (lane & 3);
+      lds_char* at = const_cast<lds_char*>(tile) + place(r, n / 8) + 2 * (n & 7);
+      const s16x4 low = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s16x4*>(at));
+      const s16x4 high = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s16x4*>(at + 4 * row_chunks * 16));
+      return __builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+  }
+};
+
+struct Chunk16 { uint32_t w[4]; };
+
+// fp32 in three bfloat16 terms, x = x1 + x2 + x3: the first cut off (so that it cannot overflow), the second rounded, the third exact.
+__device__ inline void split3(const float (&x)[8], Chunk16 (&c)[3]) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    uint32_t h[2], m[2], l[2];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const float v = x[2 * k + q];
+      h[q] = __builtin_bit_cast(uint32_t, v) & 0xffff0000u;
+      const float rest = v - __builtin_bit_cast(float, h[q]);
+      const bf16 second = narrow<bf16>(rest);
+      m[q] = __builtin_bit_cast(uint16_t, second);
+      l[q] = __builtin_bit_cast(uint32_t, rest - widen(second)) >> 16;
+    }
+    c[0].w[k] = h[0] >> 16 | h[1];
+    c[1].w[k] = m[0] | m[1] << 16;
+    c[2].w[k] = l[0] | l[1] << 16;
+  }
+}
+
+// One operand of a workgroup's tile: where it lies, and its way into LDS.  T: type in memory; E: element type in LDS; PLANES: 3 for
+// fp32, else 1; THREADS of the workgroup.
+template <typename T, typename E, int ORDER, int N, int K, int PLANES, int THREADS, bool DIRECT>
+struct Operand {
+  using L = Tile<ORDER, N, K>;
+  static constexpr int bytes = L::bytes * PLANES;
+  // kHeld: a thread takes 16 codes, two chunks
+  static constexpr int per_thread = ORDER == kHeld ? L::chunks / 2 / THREADS : L::chunks / THREADS;
+  static_assert(per_thread > 0 && per_thread * THREADS * (ORDER == kHeld ? 2 : 1) == L::chunks, "the tile has to be shared out evenly");
+
+  const T* base;         // row n0 (kDepthRuns) or column n0 (kIndexRuns)
+  int64_t ld;
+  Codes held; int groups;
+  int n;                 // operand rows from n0 on
+  int64_t depth;
+  int t;
+
+  // in flight between load() and store()
+  struct Empty {};
+  using Raw = std::conditional_t<std::is_same_v<T, float>, float[8], Chunk16>;
+  std::conditional_t<DIRECT, Empty, Raw[ORDER == kHeld ? 1 : per_thread]> raw;
+  std::conditional_t<ORDER == kHeld, Chunk16[per_thread], Empty> codes;
+  std::conditional_t<ORDER == kHeld, uint32_t[per_thread], Empty> exps;
+
+  // Straight into LDS, 16 bytes a lane: memory rows start at multiples of 16 bytes and are whole chunks.  Lanes that have nothing
+  // there get an offset out of the buffer's range, which reads as 0.
+  __device__ inline void load_direct(lds_char* to, int64_t r0) {
+    constexpr int kNowhere = (int)0x80000000u;
+    const int wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63;
+    const int left = (int)min((int64_t)K, depth - r0);
+    const T* from = base + (ORDER == kDepthRuns ? r0 : r0 * ld);
+    __amdgpu_buffer_rsrc_t buffer = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(from), 0, 0x7fffffff, 0x00020000);
+#pragma unroll
+    for (int k = 0; k < per_thread; ++k) {
+      const int piece = (wave * per_thread + k) * 64 + lane, row = piece / L::row_chunks;
+      const int chunk = (piece % L::row_chunks) ^ L::moved(row);
+      const bool there = ORDER == kDepthRuns ? row < n && chunk * 8 < left : row < left && chunk * 8 < n;
+      const int offset = there ? (row * (int)ld + chunk * 8) * 2 : kNowhere;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer, reinterpret_cast<lds_void*>(to + (wave * per_thread + k) * 1024), 16, offset, 0, 0, 0);
+    }
+  }
+
+  // Through registers: memory of any alignment, rows of any length.
+  __device__ inline void load(int64_t r0) {
+    const int left = (int)min((int64_t)K, depth - r0);
+    if constexpr (ORDER == kHeld) {
+#pragma unroll
+      for (int k = 0; k < per_thread; ++k) {
+        const int piece = k * THREADS + t, r = piece / (N / 16), i = piece % (N / 16) * 16;
+        codes[k] = Chunk16{};
+        exps[k] = 0;
+        if (r < left && i < n) {         // codes go on to the end of their group of 32
+          const int64_t row = r0 + r;
+          codes[k] = *reinterpret_cast<const Chunk16*>(held.codes + row * ((int64_t)groups * kGroup) + i);
+          exps[k] = held.exponents[row * groups + i / kGroup];
+        }
+      }
+    } else {
+      const T* from = base + (ORDER == kDepthRuns ? r0 : r0 * ld);
+#pragma unroll
+      for (int k = 0; k < per_thread; ++k) {
+        const int piece = k * THREADS + t, row = piece / L::row_chunks, chunk = piece % L::row_chunks;
+        const int rows = ORDER == kDepthRuns ? n : left, valid = (ORDER == kDepthRuns ? left : n) - chunk * 8;
+        const T* p = from + (int64_t)row * ld + chunk * 8;
+        if (row < rows && valid >= 8) {
+          __builtin_memcpy(&raw[k], p, 8 * sizeof(T));
+        } else {
+          T v[8];
+#pragma unroll
+          for (int q = 0; q < 8; ++q) v[q] = row < rows && q < valid ? p[q] : T(0.f);
+          __builtin_memcpy(&raw[k], v, 8 * sizeof(T));
+        }
+      }
+    }
+  }
+  __device__ inline void store(lds_char* to) {
+    if constexpr (ORDER == kHeld) {
+#pragma unroll
+      for (int k = 0; k < per_thread; ++k) {
+        const int piece = k * THREADS + t, r = piece / (N / 16), i = piece % (N / 16) * 16;
+        const float f = factor_of(exps[k]);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          E e[8];
+#pragma unroll
+          for (int q = 0; q < 8; ++q) e[q] = narrow<E>((float)(int8_t)(codes[k].w[2 * h + q / 4] >> (8 * (q & 3))) * f);
+          put(to + L::place(r, i / 8 + h), __builtin_bit_cast(Chunk16, e));
+        }
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < per_thread; ++k) {
+        const int piece = k * THREADS + t, at = L::place(piece / L::row_chunks, piece % L::row_chunks);
+        if constexpr (PLANES == 3) {
+          Chunk16 c[3];
+          split3(raw[k], c);
+#pragma unroll
+          for (int p = 0; p < 3; ++p) put(to + p * L::bytes + at, c[p]);
+        } else {
+          put(to + at, raw[k]);
+        }
+      }
+    }
+  }
+  __device__ static inline void put(lds_char* to, const Chunk16& c) { *reinterpret_cast<lds_s16x8*>(to) = __builtin_bit_cast(s16x8, c); }
+};
+
+// What a kernel's workgroups look like: BI x BJ of D, WI x WJ wavefronts, BK values of r at a time.
+template <int BI_, int BJ_, int WI_, int WJ_, int BK_>
+struct Shape {
+  static constexpr int BI = BI_, BJ = BJ_, WI = WI_, WJ = WJ_, BK = BK_, threads = 64 * WI * WJ, FI = BI / WI / 32, FJ = BJ / WJ / 32;
+};
+
+// The tile and split of a workgroup.  Workgroups go round the 8 XCDs; each XCD gets a run of consecutive tiles, which go in bands
+// of 4 tile rows so that those that run together share operands in its L2.
+struct Where { int ti, tj, split; };
+__device__ inline Where where(int tiles_i, int tiles_j, int tiles, int splits) {
+  const int all = tiles * splits, b = (int)blockIdx.x, x = b & 7, q = all >> 3, rem = all & 7;
+  const int w = x * q + min(x, rem) + (b >> 3);
+  const int split = w / tiles, tile = w - split * tiles;
+  constexpr int kBand = 4;
+  const int band = tile / (kBand * tiles_i), in = tile - band * kBand * tiles_i, high = min(kBand, tiles_j - band * kBand);
+  return Where{in / high, band * kBand + in % high, split};
+}
+
+struct Split {
+  int tiles_i, tiles_j, splits;
+  int64_t steps;         // values of r of a split, a multiple of BK
+};
+
+template <typename T, int PRODUCT, typename S, bool DIRECT>
+__global__ __launch_bounds__(S::threads, S::threads >= 512 ? 2 : 1) void product_kernel(ProductArgs a, Split sp) {
+  using E = std::conditional_t<std::is_same_v<T, f16>, f16, bf16>;
+  constexpr bool kWide = std::is_same_v<T, float>;
+  constexpr int kOrderA = PRODUCT == kForward ? kDepthRuns : PRODUCT == kInputGrad ? kIndexRuns : kHeld;
+  constexpr int kOrderB = PRODUCT == kWeightGrad ? kIndexRuns : kDepthRuns;
+  constexpr int PA = kWide && PRODUCT != kWeightGrad ? 3 : 1, PB = kWide ? 3 : 1;
+  constexpr bool kDirectA = DIRECT && kOrderA != kHeld;
+  using A = Operand<T, E, kOrderA, S::BI, S::BK, PA, S::threads, kDirectA>;
+  using B = Operand<T, E, kOrderB, S::BJ, S::BK, PB, S::threads, DIRECT>;
+  __shared__ __attribute__((aligned(1024))) char lds0[A::bytes + B::bytes];
+  __shared__ __attribute__((aligned(1024))) char lds1[A::bytes + B::bytes];
+
+  const Where at = where(sp.tiles_i, sp.tiles_j, sp.tiles_i * sp.tiles_j, sp.splits);
+  const int i0 = at.ti * S::BI;
+  const int64_t j0 = (int64_t)at.tj * S::BJ;
+  const int64_t first = at.split * sp.steps, last = min(a.depth, first + sp.steps);
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const int wi = wave % S::WI * (S::FI * 32), wj = wave / S::WI * (S::FJ * 32);
+
+  A oa;
+  oa.ld = a.lda; oa.n = min(S::BI, a.ni - i0); oa.depth = last; oa.t = t;
+  if constexpr (kOrderA == kHeld) {
+    oa.groups = (a.ni + kGroup - 1) / kGroup;
+    oa.held = Codes{a.held.codes + i0, a.held.exponents + i0 / kGroup};
+  } else {
+    oa.base = static_cast<const T*>(a.a) + (kOrderA == kDepthRuns ? i0 * a.lda : i0);
+  }
+  B ob;
+  ob.ld = a.ldb; ob.n = (int)min((int64_t)S::BJ, a.nj - j0); ob.depth = last; ob.t = t;
+  ob.base = static_cast<const T*>(a.b) + (kOrderB == kDepthRuns ? j0 * a.ldb : j0);
+
+  f32x16 acc[S::FI][S::FJ] = {};
+
+  auto request = [&](lds_char* to, int64_t r) {
+    if constexpr (kDirectA) oa.load_direct(to, r); else oa.load(r);
+    if constexpr (DIRECT) ob.load_direct(to + A::bytes, r); else ob.load(r);
+  };
+  auto deliver = [&](lds_char* to) {
+    if constexpr (!kDirectA) oa.store(to);
+    if constexpr (!DIRECT) ob.store(to + A::bytes);
+  };
+  auto multiply = [&](const lds_char* from) {
+#pragma unroll
+    for (int r = 0; r < S::BK; r += 16) {
+      s16x8 fa[PA][S::FI], fb[PB][S::FJ];
+#pragma unroll
+      for (int p = 0; p < PA; ++p)
+#pragma unroll
+        for (int k = 0; k < S::FI; ++k) fa[p][k] = A::L::fragment(from + p * A::L::bytes, wi + 32 * k, r, lane);
+#pragma unroll
+      for (int p = 0; p < PB; ++p)
+#pragma unroll
+        for (int k = 0; k < S::FJ; ++k) fb[p][k] = B::L::fragment(from + A::bytes + p * B::L::bytes, wj + 32 * k, r, lane);
+      // products of terms whose places add up to 2, 1, 0: the smaller ones first; those beyond are under 2^-22 of the product
+#pragma unroll
+      for (int sum = PA + PB > 2 ? 2 : 0; sum >= 0; --sum)
+#pragma unroll
+        for (int p = 0; p < PA; ++p) {
+          if (sum - p < 0 || sum - p >= PB) continue;
+#pragma unroll
+          for (int k = 0; k < S::FI; ++k)
+#pragma unroll
+            for (int q = 0; q < S::FJ; ++q) acc[k][q] = mfma<E>(fa[p][k], fb[sum - p][q], acc[k][q]);
+        }
+    }
+  };
+
+  lds_char* const b0 = (lds_char*)lds0;
+  lds_char* const b1 = (lds_char*)lds1;
+  if (first < last) {
+    request(b0, first);
+    deliver(b0);
+    __syncthreads();
+    for (int64_t r = first;; r += 2 * S::BK) {
+      const bool more = r + S::BK < last;
+      if (more) request(b1, r + S::BK);
+      multiply(b0);
+      if (!more) break;
+      deliver(b1);
+      __syncthreads();
+      const bool again = r + 2 * S::BK < last;
+      if (again) request(b0, r + 2 * S::BK);
+      multiply(b1);
+      if (!again) break;
+      deliver(b0);
+      __syncthreads();
+    }
+  }
+
+  // The tile's end, one block of 32 x 32 after the other.  Lanes l and l + 32 hold runs of 4 of the same column of D: swapped, each
+  // has 16 consecutive i.  The blocks of a column of blocks wait in LDS, so that the code that ends one is there once.
+  constexpr int kBlock = 4096, kHalf = S::WI * S::WJ / 2;
+  static_assert(kHalf * S::FI * kBlock <= A::bytes + B::bytes, "the blocks have to fit the operands' buffers");
+  __syncthreads();
+  lds_char* const mine = (wave < kHalf ? b0 : b1) + (wave % kHalf) * (S::FI * kBlock) + lane * 16;
+#pragma clang loop unroll(disable)
+  for (int q = 0; q < S::FJ; ++q) {
+#pragma unroll
+    for (int qq = 0; qq < S::FJ; ++qq) {
+      if (qq != q) continue;
+#pragma unroll
+      for (int k = 0; k < S::FI; ++k)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          Chunk16 low, high;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const float x = acc[k][qq][4 * h + c], y = acc[k][qq][8 + 4 * h + c];
+            auto s = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, y), false, false);
+            low.w[c] = (uint32_t)s[0];
+            high.w[c] = (uint32_t)s[1];
+          }
+          B::put(mine + k * kBlock + 2 * h * 1024, low);
+          B::put(mine + k * kBlock + (2 * h + 1) * 1024, high);
+        }
+    }
+    const int jj = wj + 32 * q + (lane & 31);
+#pragma clang loop unroll(disable)
+    for (int k = 0; k < S::FI; ++k) {
+      float v[16];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const s16x8 x = *reinterpret_cast<const lds_s16x8*>(mine + k * kBlock + c * 1024);
+        __builtin_memcpy(v + 4 * c, &x, 16);
+      }
+      const int ii = wi + 32 * k + (lane >> 5) * 16;
+      if (sp.splits > 1) {
+        float* to = static_cast<float*>(a.workspace) + (((int64_t)at.split * sp.tiles_j + at.tj) * sp.tiles_i + at.ti) * (S::BI * S::BJ) + jj * S::BI + ii;
+        store_values(to, v, 16);
+      } else {
+        finish<T, PRODUCT>(v, a, j0 + jj, i0 + ii, j0 + jj < a.nj, 32);
+      }
+    }
+  }
+}
+
+// Adds up the splits of a product in their order and ends it.  A thread takes 16 i of one j, neighbours a group of 32.
+template <typename T, int PRODUCT>
+__global__ __launch_bounds__(256) void join_kernel(ProductArgs a, Split sp, int bi, int bj) {
+  const int row = bi / 16;                              // threads to a row of a tile
+  const int64_t piece = (int64_t)blockIdx.x * 256 + threadIdx.x, per_tile = (int64_t)row * bj, tile = piece / per_tile;
+  const int in = (int)(piece - tile * per_tile), jj = in / row, ii = in % row * 16;
+  const int64_t j = tile / sp.tiles_i * bj + jj;
+  const int i = (int)(tile % sp.tiles_i) * bi + ii;
+  const int64_t all = (int64_t)sp.tiles_i * sp.tiles_j * bi * bj;
+  float v[16] = {};
+  if (j < a.nj && i < a.ni) {
+    const float* from = static_cast<const float*>(a.workspace) + tile * (bi * bj) + jj * bi + ii;
+    for (int s = 0; s < sp.splits; ++s) {
+      float w[16];
+      load_values(w, from + s * all, 16);
+#pragma unroll
+      for (int k = 0; k < 16; ++k) v[k] += w[k];
+    }
+  }
+  finish<T, PRODUCT>(v, a, j, i, j < a.nj, 1);
+}
+
+template <typename T, int PRODUCT, typename S, bool DIRECT>
+hipError_t run_product(const ProductArgs& a, hipStream_t s) {
+  Split sp;
+  sp.tiles_i = (a.ni + S::BI - 1) / S::BI;
+  const int64_t tiles_j = (a.nj + S::BJ - 1) / S::BJ, tiles = tiles_j * sp.tiles_i;
+  if (tiles > INT32_MAX) return hipErrorInvalidValue;
+  sp.tiles_j = (int)tiles_j;
+  // Few tiles: the sum is split so that the CUs have work, each part at least 4 steps.
+  const int64_t steps = (a.depth + S::BK - 1) / S::BK, fit = (int64_t)(kWorkspaceBytes / (sizeof(float) * S::BI * S::BJ));
+  int64_t splits = std::max<int64_t>(1, std::min({steps / 4, 256 / tiles, fit / tiles}));
+  const int64_t per = std::max<int64_t>(1, (steps + splits - 1) / splits);
+  sp.splits = (int)std::max<int64_t>(1, (steps + per - 1) / per);
+  sp.steps = per * S::BK;
+  product_kernel<T, PRODUCT, S, DIRECT><<<dim3((unsigned)(tiles * sp.splits)), S::threads, 0, s>>>(a, sp);
+  if (sp.splits > 1) join_kernel<T, PRODUCT><<<dim3((unsigned)(tiles * S::BI * S::BJ / 16 / 256)), 256, 0, s>>>(a, sp, S::BI, S::BJ);
+  return hipGetLastError();
+}
+
+bool whole_chunks(const void* p, int64_t ld, int64_t length) {
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0 && length % 8 == 0;
 }
 
 template <typename T, int PRODUCT>
 hipError_t product(const ProductArgs& a, hipStream_t s) {
-  const int64_t tiles_i = (a.ni + 63) / 64, tiles_j = (a.nj + 63) / 64;
-  if (tiles_i * tiles_j > INT32_MAX) return hipErrorInvalidValue;
-  product_kernel<T, PRODUCT><<<dim3((unsigned)(tiles_i * tiles_j)), 256, 0, s>>>(a, (int)tiles_i);
-  return hipGetLastError();
+  if constexpr (std::is_same_v<T, float>) {
+    const int64_t big = ((a.ni + 255) / 256) * ((a.nj + 127) / 128);
+    if (big >= 128) return run_product<T, PRODUCT, Shape<256, 128, 4, 2, 32>, false>(a, s);
+    return run_product<T, PRODUCT, Shape<128, 128, 2, 2, 32>, false>(a, s);
+  } else {
+    const bool direct = (PRODUCT == kWeightGrad || whole_chunks(a.a, a.lda, PRODUCT == kForward ? a.depth : a.ni)) &&
+                        whole_chunks(a.b, a.ldb, PRODUCT == kWeightGrad ? a.nj : a.depth);
+    const int64_t big = ((a.ni + 255) / 256) * ((a.nj + 255) / 256);
+    if (big >= 128)
+      return direct ? run_product<T, PRODUCT, Shape<256, 256, 2, 4, 64>, true>(a, s) : run_product<T, PRODUCT, Shape<256, 256, 2, 4, 64>, false>(a, s);
+    return direct ? run_product<T, PRODUCT, Shape<128, 128, 2, 2, 64>, true>(a, s) : run_product<T, PRODUCT, Shape<128, 128, 2, 2, 64>, false>(a, s);
+  }
 }
 
 template <typename F>
