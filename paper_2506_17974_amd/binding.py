@@ -421,11 +421,15 @@ class LinearOps:
         import torch
         if not torch.cuda.is_available():
             raise RuntimeError("no GPU visible: the linear layer has no CPU path")
-        self._torch = torch
+        self._torch, self._Tensor, self._empty = torch, torch.Tensor, torch.empty
         self._types = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16, torch.float16: TYPE_F16}
+        self._f32, self._codes_type, self._exponents_type = torch.float32, torch.int8, torch.uint8
         self._h = C.c_void_p()
-        self.device = torch.device("cuda", torch.cuda.current_device())
-        self.stream_handle = int(torch.cuda.current_stream().cuda_stream)
+        self._index = torch.cuda.current_device()
+        self.device = torch.device("cuda", self._index)
+        # the current stream's handle, without the Stream object around it where torch has that
+        self._stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+        self.stream_handle = int(self._stream(self._index))
         self._L = lib()
         rc = self._L.lqsgd_linear_create(C.c_void_p(self.stream_handle), C.byref(self._h))
         if rc:
@@ -440,16 +444,16 @@ class LinearOps:
     def _begin(self):
         if not self._h:
             raise LqsgdError(ESTATE, "the context is closed")
-        if self._torch.cuda.current_stream(self.device).cuda_stream != self.stream_handle:
+        if self._stream(self._index) != self.stream_handle:
             raise LqsgdError(ESTATE, "the current stream is not the one this context was made on")
 
     def _bad(self, what, t):
         raise LqsgdError(ESHAPE, "%s: %s" % (what, "%s %s on %s, strides %s" % (t.dtype, tuple(t.shape), t.device, t.stride())
-                                             if isinstance(t, self._torch.Tensor) else type(t).__name__))
+                                             if isinstance(t, self._Tensor) else type(t).__name__))
 
     def _matrix(self, what, t, dtype=None, rows=None, cols=None):
-        """The distance between rows of a two-dimensional tensor that the kernels take as it is."""
-        if not isinstance(t, self._torch.Tensor) or t.dim() != 2 or t.device != self.device:
+        """(rows, cols, the distance between rows) of a two-dimensional tensor that the kernels take as it is."""
+        if not isinstance(t, self._Tensor) or t.get_device() != self._index or t.dim() != 2:
             self._bad("%s has to be a two-dimensional tensor on %s" % (what, self.device), t)
         m, n = t.shape
         if t.dtype is not dtype if dtype is not None else t.dtype not in self._types:
@@ -459,25 +463,27 @@ class LinearOps:
         ld, step = t.stride()
         if step != 1 and n > 1:
             self._bad("%s: the elements of a row have to be contiguous" % what, t)
-        return ld if m > 1 else max(n, 1)
+        return m, n, ld if m > 1 else max(n, 1)
 
     def _vector(self, what, t, dtype, n):
-        if not isinstance(t, self._torch.Tensor) or t.device != self.device or t.dtype is not dtype or tuple(t.shape) != (n,) or \
-                not t.is_contiguous():
+        if not isinstance(t, self._Tensor) or t.get_device() != self._index or t.dtype is not dtype or t.shape != (n,) or not t.is_contiguous():
             self._bad("%s has to be a contiguous vector of %d %s" % (what, n, dtype), t)
         return t.data_ptr()
 
     def _held(self, what, c, samples, features):
-        torch = self._torch
         if not isinstance(c, Checkpoint):
             raise LqsgdError(EINVAL, "%s has to be a Checkpoint" % what)
-        groups = -(-features // CHECKPOINT_GROUP)
         if c.features != features:
             raise LqsgdError(ESHAPE, "%s has %d features, %d wanted" % (what, c.features, features))
-        for t, dtype, n in ((c.codes, torch.int8, groups * CHECKPOINT_GROUP), (c.exponents, torch.uint8, groups)):
-            if t.dtype is not dtype or tuple(t.shape) != (samples, n) or t.device != self.device or not t.is_contiguous():
-                self._bad("%s: contiguous %s of %d x %d wanted" % (what, dtype, samples, n), t)
-        return c.codes.data_ptr(), c.exponents.data_ptr()
+        groups = -(-features // CHECKPOINT_GROUP)
+        codes, exps = c.codes, c.exponents
+        if codes.dtype is not self._codes_type or codes.shape != (samples, groups * CHECKPOINT_GROUP) or \
+                codes.get_device() != self._index or not codes.is_contiguous():
+            self._bad("%s: contiguous int8 codes of %d x %d wanted" % (what, samples, groups * CHECKPOINT_GROUP), codes)
+        if exps.dtype is not self._exponents_type or exps.shape != (samples, groups) or exps.get_device() != self._index or \
+                not exps.is_contiguous():
+            self._bad("%s: contiguous uint8 exponents of %d x %d wanted" % (what, samples, groups), exps)
+        return codes.data_ptr(), exps.data_ptr()
 
     def close(self):
         if self._h:
@@ -497,8 +503,7 @@ class LinearOps:
     def save(self, x, out=None):
         """x in 8 bits."""
         self._begin()
-        ld = self._matrix("x", x)
-        m, n = x.shape
+        m, n, ld = self._matrix("x", x)
         if out is None:
             out = Checkpoint.empty(m, n, self.device)
         codes, exps = self._held("out", out, m, n)
@@ -513,8 +518,8 @@ class LinearOps:
         m, n = held.codes.shape[0], held.features
         codes, exps = self._held("held", held, m, n)
         if out is None:
-            out = self._torch.empty((m, n), dtype=dtype or self._torch.bfloat16, device=self.device)
-        ld = self._matrix("out", out, dtype, m, n)
+            out = self._empty((m, n), dtype=dtype or self._torch.bfloat16, device=self.device)
+        _, _, ld = self._matrix("out", out, dtype, m, n)
         self._check(self._L.lqsgd_checkpoint_load(self._h, self._types[out.dtype], m, n, codes, exps, out.data_ptr(), ld))
         return out
 
@@ -522,65 +527,67 @@ class LinearOps:
     def forward(self, x, w, bias=None, residual=None, act="none", out=None, save_z=None, save_y=None):
         """act(x w^T + bias) + residual.  save_z, save_y: Checkpoints of samples x rows that receive z and y as well."""
         self._begin()
-        ldx = self._matrix("x", x)
-        m, k = x.shape
-        ldw = self._matrix("w", w, x.dtype, None, k)
-        n = w.shape[0]
+        m, k, ldx = self._matrix("x", x)
+        T = x.dtype
+        n, _, ldw = self._matrix("w", w, T, None, k)
         if act not in ACTS:
             raise LqsgdError(EINVAL, "unknown activation %r" % (act,))
-        b = self._vector("bias", bias, x.dtype, n) if bias is not None else None
-        r, ldr = (residual.data_ptr(), self._matrix("residual", residual, x.dtype, m, n)) if residual is not None else (None, 0)
+        b = self._vector("bias", bias, T, n) if bias is not None else None
+        r, ldr = (residual.data_ptr(), self._matrix("residual", residual, T, m, n)[2]) if residual is not None else (None, 0)
         if out is None:
-            out = self._torch.empty((m, n), dtype=x.dtype, device=self.device)
-        ldy = self._matrix("out", out, x.dtype, m, n)
+            out, ldy = self._empty((m, n), dtype=T, device=self.device), n
+        else:
+            ldy = self._matrix("out", out, T, m, n)[2]
         zc, ze = self._held("save_z", save_z, m, n) if save_z is not None else (None, None)
         yc, ye = self._held("save_y", save_y, m, n) if save_y is not None else (None, None)
-        self._check(self._L.lqsgd_linear_forward(self._h, self._types[x.dtype], ACTS[act], m, n, k, x.data_ptr(), ldx, w.data_ptr(), ldw,
+        self._check(self._L.lqsgd_linear_forward(self._h, self._types[T], ACTS[act], m, n, k, x.data_ptr(), ldx, w.data_ptr(), ldw,
                                                  b, r, ldr, out.data_ptr(), ldy, zc, ze, yc, ye))
         return out
 
     # -- backward --------------------------------------------------------
     def activation_backward(self, dy, z=None, act="none", dz=None, dbias=None, accumulate=False, want_dz=True, want_dbias=True):
-        """(dz, dbias) of dy and the checkpoint z (not needed without an activation); what is not wanted is None."""
+        """(dz, dbias) of dy and the checkpoint z (not needed without an activation); what is not wanted is None.  dz may be dy."""
         self._begin()
-        lddy = self._matrix("dy", dy)
-        m, n = dy.shape
+        m, n, lddy = self._matrix("dy", dy)
+        T = dy.dtype
         if act not in ACTS:
             raise LqsgdError(EINVAL, "unknown activation %r" % (act,))
         if z is None and act != "none":
             raise LqsgdError(EINVAL, "the activation's backward needs the checkpoint of z")
         zc, ze = self._held("z", z, m, n) if z is not None else (None, None)
-        if dz is None and want_dz:
-            dz = self._torch.empty((m, n), dtype=dy.dtype, device=self.device)
-        lddz = self._matrix("dz", dz, dy.dtype, m, n) if dz is not None else 0
+        pz, lddz = None, 0
+        if dz is not None:
+            pz, lddz = dz.data_ptr(), self._matrix("dz", dz, T, m, n)[2]
+        elif want_dz:
+            dz = self._empty((m, n), dtype=T, device=self.device)
+            pz, lddz = dz.data_ptr(), n
         if dbias is None and want_dbias:
             if accumulate:
                 raise LqsgdError(EINVAL, "accumulate needs the dbias to add to")
-            dbias = self._torch.empty(n, dtype=self._torch.float32, device=self.device)
-        db = self._vector("dbias", dbias, self._torch.float32, n) if dbias is not None else None
-        self._check(self._L.lqsgd_linear_activation_backward(self._h, self._types[dy.dtype], ACTS[act], m, n, dy.data_ptr(), lddy, zc, ze,
-                                                             dz.data_ptr() if dz is not None else None, lddz, db, 1 if accumulate else 0))
+            dbias = self._empty(n, dtype=self._f32, device=self.device)
+        db = self._vector("dbias", dbias, self._f32, n) if dbias is not None else None
+        self._check(self._L.lqsgd_linear_activation_backward(self._h, self._types[T], ACTS[act], m, n, dy.data_ptr(), lddy, zc, ze, pz, lddz,
+                                                             db, 1 if accumulate else 0))
         return dz, dbias
 
     def input_grad(self, dz, w, out=None):
         """dz w."""
         self._begin()
-        lddz = self._matrix("dz", dz)
-        m, n = dz.shape
-        ldw = self._matrix("w", w, dz.dtype, n, None)
-        k = w.shape[1]
+        m, n, lddz = self._matrix("dz", dz)
+        T = dz.dtype
+        _, k, ldw = self._matrix("w", w, T, n, None)
         if out is None:
-            out = self._torch.empty((m, k), dtype=dz.dtype, device=self.device)
-        lddx = self._matrix("out", out, dz.dtype, m, k)
-        self._check(self._L.lqsgd_linear_input_grad(self._h, self._types[dz.dtype], m, n, k, dz.data_ptr(), lddz, w.data_ptr(), ldw,
-                                                    out.data_ptr(), lddx))
+            out, lddx = self._empty((m, k), dtype=T, device=self.device), k
+        else:
+            lddx = self._matrix("out", out, T, m, k)[2]
+        self._check(self._L.lqsgd_linear_input_grad(self._h, self._types[T], m, n, k, dz.data_ptr(), lddz, w.data_ptr(), ldw, out.data_ptr(),
+                                                    lddx))
         return out
 
     def weight_grad(self, dz, x, out=None, dtype=None, accumulate=False):
         """dz^T x^ of the checkpoint x, in float32 or bfloat16 (`dtype`; default: out's, else float32): a gradient for Compressor.step."""
         self._begin()
-        lddz = self._matrix("dz", dz)
-        m, n = dz.shape
+        m, n, lddz = self._matrix("dz", dz)
         if not isinstance(x, Checkpoint):
             raise LqsgdError(EINVAL, "x has to be a Checkpoint")
         k = x.features
@@ -588,8 +595,8 @@ class LinearOps:
         if out is None:
             if accumulate:
                 raise LqsgdError(EINVAL, "accumulate needs the gradient to add to")
-            out = self._torch.empty((n, k), dtype=dtype or self._torch.float32, device=self.device)
-        lddw = self._matrix("out", out, dtype, n, k)
+            out = self._empty((n, k), dtype=dtype or self._f32, device=self.device)
+        _, _, lddw = self._matrix("out", out, dtype, n, k)
         self._check(self._L.lqsgd_linear_weight_grad(self._h, self._types[dz.dtype], m, n, k, dz.data_ptr(), lddz, xc, xe,
                                                      self._types[out.dtype], out.data_ptr(), lddw, 1 if accumulate else 0))
         return out

@@ -262,29 +262,29 @@ __global__ __launch_bounds__(256) void sum_runs_kernel(const float* part, float*
 // ---------------------------------------------------------------------------
 // products
 // ---------------------------------------------------------------------------
-// The end of a product: v holds D[j][i0 .. i0 + 15], the lane `partner` away the other half of the group of 32 (i0 a multiple of
-// 16).  All lanes of the wavefront come here together; `there` is false for those that have no row j.
-template <typename T, int PRODUCT>
-__device__ inline void finish(float (&v)[16], const ProductArgs& a, int64_t j, int i0, bool there, int partner) {
+// The end of a product: v holds D[j][i0 .. i0 + N - 1], i0 a multiple of N, and the lanes `near`, 2 near, .. away the rest of the
+// group of 32.  All lanes of the wavefront come here together; `there` is false for those that have no row j.
+template <typename T, int PRODUCT, int N>
+__device__ inline void finish(float (&v)[N], const ProductArgs& a, int64_t j, int i0, bool there, int near) {
   const int n = there ? a.ni - i0 : 0;
   if (PRODUCT == kWeightGrad) {
     if (n <= 0) return;
     if (a.out_type == kF32) {
       float* out = static_cast<float*>(a.out) + j * a.ldo + i0;
       if (a.accumulate) {
-        float before[16];
+        float before[N];
         load_values(before, out, n);
 #pragma unroll
-        for (int k = 0; k < 16; ++k) v[k] += before[k];
+        for (int k = 0; k < N; ++k) v[k] += before[k];
       }
       store_values(out, v, n);
     } else {
       bf16* out = static_cast<bf16*>(a.out) + j * a.ldo + i0;
       if (a.accumulate) {
-        float before[16];
+        float before[N];
         load_values(before, out, n);
 #pragma unroll
-        for (int k = 0; k < 16; ++k) v[k] += before[k];
+        for (int k = 0; k < N; ++k) v[k] += before[k];
       }
       store_values(out, v, n);
     }
@@ -299,38 +299,39 @@ __device__ inline void finish(float (&v)[16], const ProductArgs& a, int64_t j, i
   const bool in_codes = there && i0 < groups * kGroup;
   const int64_t code_at = j * ((int64_t)groups * kGroup) + i0, exp_at = j * groups + i0 / kGroup;
   if (a.bias) {
-    float b[16];
+    float b[N];
     load_values(b, static_cast<const T*>(a.bias) + i0, n);
 #pragma unroll
-    for (int k = 0; k < 16; ++k) v[k] += b[k];
+    for (int k = 0; k < N; ++k) v[k] += b[k];
   }
   auto keep = [&](const Codes& c) {
     uint32_t m = 0;
 #pragma unroll
-    for (int k = 0; k < 16; ++k) {
+    for (int k = 0; k < N; ++k) {
       if (k >= n) v[k] = 0.f;
       m = max(m, magnitude_bits(v[k]));
     }
-    m = max(m, (uint32_t)__shfl_xor((int)m, partner));
-    uint32_t w[4], byte;
+#pragma unroll
+    for (int d = 0; N << d < kGroup; ++d) m = max(m, (uint32_t)__shfl_xor((int)m, near << d));
+    uint32_t w[N / 4], byte;
     pack_codes<T>(w, v, m, &byte);
     if (in_codes) {
-      *reinterpret_cast<uint4*>(c.codes + code_at) = make_uint4(w[0], w[1], w[2], w[3]);
-      if ((i0 & 16) == 0) c.exponents[exp_at] = (uint8_t)byte;
+      __builtin_memcpy(__builtin_assume_aligned(c.codes + code_at, N), w, N);
+      if (i0 % kGroup == 0) c.exponents[exp_at] = (uint8_t)byte;
     }
   };
   if (a.z.codes) keep(a.z);
   activate_all(v, a.act);
   if (a.residual) {
-    float r[16];
+    float r[N];
     load_values(r, static_cast<const T*>(a.residual) + j * a.ldr + i0, n);
 #pragma unroll
-    for (int k = 0; k < 16; ++k) v[k] += r[k];
+    for (int k = 0; k < N; ++k) v[k] += r[k];
   }
   if (n > 0) store_values(out, v, n);
   if (a.y.codes) {
 #pragma unroll
-    for (int k = 0; k < 16; ++k) v[k] = widen(narrow<T>(v[k]));
+    for (int k = 0; k < N; ++k) v[k] = widen(narrow<T>(v[k]));
     keep(a.y);
   }
 }
@@ -372,9 +373,13 @@ struct Tile {
   static constexpr int chunks = row_chunks * rows;
   static constexpr int bytes = chunks * 16;
   __device__ static inline int moved(int row) {
-    if (ORDER != kDepthRuns) return (2 * (row & 1) + 5 * (row >> 1 & 1)) << 1;
-    if (row_chunks == 8) return (row & 7) ^ (row >> 3 & 1);
-    return (row >> 1 & 3) ^ (row >> 3 & 1);
+    static_assert(row_chunks == 4 || row_chunks == 8 || (ORDER != kDepthRuns && row_chunks % 16 == 0), "the exchange stays within a row");
+    if (ORDER != kDepthRuns) {            // pairs of chunks
+      if (row_chunks == 4) return row & 2;
+      if (row_chunks == 8) return (row & 3) << 1;
+      return (2 * (row & 1) + 5 * (row >> 1 & 1)) << 1;
+    }
+    return row_chunks == 8 ? (row & 7) ^ (row >> 3 & 1) : (row >> 1 & 3) ^ (row >> 3 & 1);
   }
   __device__ static inline int place(int row, int chunk) { return (row * row_chunks + (chunk ^ moved(row))) * 16; }
   // The 8 elements that a lane holds of rows n0 .. n0 + 31 and r = r0 .. r0 + 15 (n0 a multiple of 32, r0 of 16).
@@ -393,6 +398,27 @@ struct Tile {
 };
 
 struct Chunk16 { uint32_t w[4]; };
+
+// The first `valid` (0 .. 16 / sizeof(T)) elements from p, zeros behind them, without a branch and without touching memory beyond
+// them: the 16 bytes that end there are read and shifted down.  There have to be 16 bytes of the tensor up to there; 16 bytes at `safe` are read
+// where valid is 0.
+template <typename T>
+__device__ inline Chunk16 load_tail(const T* p, int valid, const T* safe) {
+  constexpr int kAll = 16 / (int)sizeof(T);
+  Chunk16 c;
+  __builtin_memcpy(&c, valid > 0 ? p + (valid - kAll) : safe, 16);
+  const int bytes = (kAll - valid) * (int)sizeof(T);
+  const bool one = bytes & 4, two = bytes & 8;
+  uint32_t w0 = one ? c.w[1] : c.w[0], w1 = one ? c.w[2] : c.w[1], w2 = one ? c.w[3] : c.w[2], w3 = one ? 0u : c.w[3];
+  w0 = two ? w2 : w0, w1 = two ? w3 : w1, w2 = two ? 0u : w2, w3 = two ? 0u : w3;
+  if (sizeof(T) == 2) {
+    const uint32_t half = (bytes & 2) * 8;
+    w0 = __builtin_amdgcn_alignbit(w1, w0, half), w1 = __builtin_amdgcn_alignbit(w2, w1, half);
+    w2 = __builtin_amdgcn_alignbit(w3, w2, half), w3 = w3 >> half;
+  }
+  const uint32_t keep = valid > 0 ? 0xffffffffu : 0u;
+  return Chunk16{{w0 & keep, w1 & keep, w2 & keep, w3 & keep}};
+}
 
 // fp32 in three bfloat16 terms, x = x1 + x2 + x3: the first cut off (so that it cannot overflow), the second rounded, the third exact.
 __device__ inline void split3(const float (&x)[8], Chunk16 (&c)[3]) {
@@ -427,7 +453,8 @@ struct Operand {
   const T* base;         // row n0 (kDepthRuns) or column n0 (kIndexRuns)
   int64_t ld;
   Codes held; int groups;
-  int n;                 // operand rows from n0 on
+  int n;                 // operand rows from n0 on, N at most
+  int length;            // of a memory row: the tensor's
   int64_t depth;
   int t;
 
@@ -473,17 +500,34 @@ struct Operand {
       }
     } else {
       const T* from = base + (ORDER == kDepthRuns ? r0 : r0 * ld);
+      const int rows = ORDER == kDepthRuns ? n : left, run = ORDER == kDepthRuns ? left : n;
+      constexpr int kPart = 16 / (int)sizeof(T), kParts = 8 / kPart;
+      if (n == N && left == K) {
 #pragma unroll
-      for (int k = 0; k < per_thread; ++k) {
-        const int piece = k * THREADS + t, row = piece / L::row_chunks, chunk = piece % L::row_chunks;
-        const int rows = ORDER == kDepthRuns ? n : left, valid = (ORDER == kDepthRuns ? left : n) - chunk * 8;
-        const T* p = from + (int64_t)row * ld + chunk * 8;
-        if (row < rows && valid >= 8) {
-          __builtin_memcpy(&raw[k], p, 8 * sizeof(T));
-        } else {
+        for (int k = 0; k < per_thread; ++k) {
+          const int piece = k * THREADS + t;
+          __builtin_memcpy(&raw[k], from + (int64_t)(piece / L::row_chunks) * ld + piece % L::row_chunks * 8, 8 * sizeof(T));
+        }
+      } else if (length >= kPart) {
+        const T* safe = from + (min(run, kPart) - kPart);      // a run that starts the tensor's first row is that long
+#pragma unroll
+        for (int k = 0; k < per_thread; ++k) {
+          const int piece = k * THREADS + t, row = piece / L::row_chunks, chunk = piece % L::row_chunks;
+#pragma unroll
+          for (int h = 0; h < kParts; ++h) {
+            const int valid = row < rows ? min(max(run - chunk * 8 - h * kPart, 0), kPart) : 0;
+            const Chunk16 c = load_tail(from + (int64_t)row * ld + chunk * 8 + h * kPart, valid, safe);
+            __builtin_memcpy(reinterpret_cast<char*>(&raw[k]) + 16 * h, &c, 16);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < per_thread; ++k) {
+          const int piece = k * THREADS + t, row = piece / L::row_chunks, chunk = piece % L::row_chunks;
+          const T* p = from + (int64_t)row * ld + chunk * 8;
           T v[8];
 #pragma unroll
-          for (int q = 0; q < 8; ++q) v[q] = row < rows && q < valid ? p[q] : T(0.f);
+          for (int q = 0; q < 8; ++q) v[q] = row < rows && q < run - chunk * 8 ? p[q] : T(0.f);
           __builtin_memcpy(&raw[k], v, 8 * sizeof(T));
         }
       }
@@ -544,60 +588,57 @@ struct Split {
   int64_t steps;         // values of r of a split, a multiple of BK
 };
 
-template <typename T, int PRODUCT, typename S, bool DIRECT>
-__global__ __launch_bounds__(S::threads, S::threads >= 512 ? 2 : 1) void product_kernel(ProductArgs a, Split sp) {
+// Types and operands of a product whose workgroups (or wavefronts: THREADS = 64) have a tile of BI x BJ, BK deep.
+template <typename T, int PRODUCT, int BI, int BJ, int BK, int THREADS, bool DIRECT>
+struct Operands {
   using E = std::conditional_t<std::is_same_v<T, f16>, f16, bf16>;
-  constexpr bool kWide = std::is_same_v<T, float>;
-  constexpr int kOrderA = PRODUCT == kForward ? kDepthRuns : PRODUCT == kInputGrad ? kIndexRuns : kHeld;
-  constexpr int kOrderB = PRODUCT == kWeightGrad ? kIndexRuns : kDepthRuns;
-  constexpr int PA = kWide && PRODUCT != kWeightGrad ? 3 : 1, PB = kWide ? 3 : 1;
-  constexpr bool kDirectA = DIRECT && kOrderA != kHeld;
-  using A = Operand<T, E, kOrderA, S::BI, S::BK, PA, S::threads, kDirectA>;
-  using B = Operand<T, E, kOrderB, S::BJ, S::BK, PB, S::threads, DIRECT>;
-  __shared__ __attribute__((aligned(1024))) char lds0[A::bytes + B::bytes];
-  __shared__ __attribute__((aligned(1024))) char lds1[A::bytes + B::bytes];
+  static constexpr bool kWide = std::is_same_v<T, float>;
+  static constexpr int kOrderA = PRODUCT == kForward ? kDepthRuns : PRODUCT == kInputGrad ? kIndexRuns : kHeld;
+  static constexpr int kOrderB = PRODUCT == kWeightGrad ? kIndexRuns : kDepthRuns;
+  static constexpr int PA = kWide && PRODUCT != kWeightGrad ? 3 : 1, PB = kWide ? 3 : 1;
+  static constexpr bool kDirectA = DIRECT && kOrderA != kHeld;
+  using A = Operand<T, E, kOrderA, BI, BK, PA, THREADS, kDirectA>;
+  using B = Operand<T, E, kOrderB, BJ, BK, PB, THREADS, DIRECT>;
+  static constexpr int bytes = A::bytes + B::bytes;
+  A a;
+  B b;
 
-  const Where at = where(sp.tiles_i, sp.tiles_j, sp.tiles_i * sp.tiles_j, sp.splits);
-  const int i0 = at.ti * S::BI;
-  const int64_t j0 = (int64_t)at.tj * S::BJ;
-  const int64_t first = at.split * sp.steps, last = min(a.depth, first + sp.steps);
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-  const int wi = wave % S::WI * (S::FI * 32), wj = wave / S::WI * (S::FJ * 32);
-
-  A oa;
-  oa.ld = a.lda; oa.n = min(S::BI, a.ni - i0); oa.depth = last; oa.t = t;
-  if constexpr (kOrderA == kHeld) {
-    oa.groups = (a.ni + kGroup - 1) / kGroup;
-    oa.held = Codes{a.held.codes + i0, a.held.exponents + i0 / kGroup};
-  } else {
-    oa.base = static_cast<const T*>(a.a) + (kOrderA == kDepthRuns ? i0 * a.lda : i0);
+  __device__ inline Operands(const ProductArgs& p, int i0, int64_t j0, int64_t last, int t) {
+    a.ld = p.lda; a.n = min(BI, p.ni - i0); a.depth = last; a.t = t;
+    a.length = kOrderA == kDepthRuns ? (int)p.depth : p.ni;
+    if constexpr (kOrderA == kHeld) {
+      a.groups = (p.ni + kGroup - 1) / kGroup;
+      a.held = Codes{p.held.codes + i0, p.held.exponents + i0 / kGroup};
+    } else {
+      a.base = static_cast<const T*>(p.a) + (kOrderA == kDepthRuns ? i0 * p.lda : i0);
+    }
+    b.ld = p.ldb; b.n = (int)min((int64_t)BJ, p.nj - j0); b.depth = last; b.t = t;
+    b.length = kOrderB == kDepthRuns ? (int)p.depth : (int)p.nj;
+    b.base = static_cast<const T*>(p.b) + (kOrderB == kDepthRuns ? j0 * p.ldb : j0);
   }
-  B ob;
-  ob.ld = a.ldb; ob.n = (int)min((int64_t)S::BJ, a.nj - j0); ob.depth = last; ob.t = t;
-  ob.base = static_cast<const T*>(a.b) + (kOrderB == kDepthRuns ? j0 * a.ldb : j0);
-
-  f32x16 acc[S::FI][S::FJ] = {};
-
-  auto request = [&](lds_char* to, int64_t r) {
-    if constexpr (kDirectA) oa.load_direct(to, r); else oa.load(r);
-    if constexpr (DIRECT) ob.load_direct(to + A::bytes, r); else ob.load(r);
-  };
-  auto deliver = [&](lds_char* to) {
-    if constexpr (!kDirectA) oa.store(to);
-    if constexpr (!DIRECT) ob.store(to + A::bytes);
-  };
-  auto multiply = [&](const lds_char* from) {
+  // Values of r from r0 on are asked for; deliver() puts those that go through registers into LDS.
+  __device__ inline void request(lds_char* to, int64_t r0) {
+    if constexpr (kDirectA) a.load_direct(to, r0); else a.load(r0);
+    if constexpr (DIRECT) b.load_direct(to + A::bytes, r0); else b.load(r0);
+  }
+  __device__ inline void deliver(lds_char* to) {
+    if constexpr (!kDirectA) a.store(to);
+    if constexpr (!DIRECT) b.store(to + A::bytes);
+  }
+  // acc += the products of the tile's rows from wi, wj on.
+  template <int FI, int FJ>
+  __device__ static inline void multiply(f32x16 (&acc)[FI][FJ], const lds_char* from, int wi, int wj, int lane) {
 #pragma unroll
-    for (int r = 0; r < S::BK; r += 16) {
-      s16x8 fa[PA][S::FI], fb[PB][S::FJ];
+    for (int r = 0; r < BK; r += 16) {
+      s16x8 fa[PA][FI], fb[PB][FJ];
 #pragma unroll
       for (int p = 0; p < PA; ++p)
 #pragma unroll
-        for (int k = 0; k < S::FI; ++k) fa[p][k] = A::L::fragment(from + p * A::L::bytes, wi + 32 * k, r, lane);
+        for (int k = 0; k < FI; ++k) fa[p][k] = A::L::fragment(from + p * A::L::bytes, wi + 32 * k, r, lane);
 #pragma unroll
       for (int p = 0; p < PB; ++p)
 #pragma unroll
-        for (int k = 0; k < S::FJ; ++k) fb[p][k] = B::L::fragment(from + A::bytes + p * B::L::bytes, wj + 32 * k, r, lane);
+        for (int k = 0; k < FJ; ++k) fb[p][k] = B::L::fragment(from + A::bytes + p * B::L::bytes, wj + 32 * k, r, lane);
       // products of terms whose places add up to 2, 1, 0: the smaller ones first; those beyond are under 2^-22 of the product
 #pragma unroll
       for (int sum = PA + PB > 2 ? 2 : 0; sum >= 0; --sum)
@@ -605,39 +646,81 @@ __global__ __launch_bounds__(S::threads, S::threads >= 512 ? 2 : 1) void product
         for (int p = 0; p < PA; ++p) {
           if (sum - p < 0 || sum - p >= PB) continue;
 #pragma unroll
-          for (int k = 0; k < S::FI; ++k)
+          for (int k = 0; k < FI; ++k)
 #pragma unroll
-            for (int q = 0; q < S::FJ; ++q) acc[k][q] = mfma<E>(fa[p][k], fb[sum - p][q], acc[k][q]);
+            for (int q = 0; q < FJ; ++q) acc[k][q] = mfma<E>(fa[p][k], fb[sum - p][q], acc[k][q]);
         }
     }
-  };
+  }
+};
+
+// A block of D as the matrix instructions leave it, put to LDS as 4 pieces of 16 bytes a lane, 1 KiB apart: lanes l and l + 32 hold
+// runs of 4 of the same column; swapped, each has 16 consecutive i: lane l the first 16 of column l, lane l + 32 the others.
+__device__ inline void put_block(lds_char* to, const f32x16& block) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    uint32_t low[4], high[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const float x = block[4 * h + c], y = block[8 + 4 * h + c];
+      auto s = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, y), false, false);
+      low[c] = (uint32_t)s[0];
+      high[c] = (uint32_t)s[1];
+    }
+    s16x8 v;
+    __builtin_memcpy(&v, low, 16);
+    *reinterpret_cast<lds_s16x8*>(to + 2 * h * 1024) = v;
+    __builtin_memcpy(&v, high, 16);
+    *reinterpret_cast<lds_s16x8*>(to + (2 * h + 1) * 1024) = v;
+  }
+}
+__device__ inline void get_piece(float* v, const lds_char* from) {
+  const s16x8 x = *reinterpret_cast<const lds_s16x8*>(from);
+  __builtin_memcpy(v, &x, 16);
+}
+
+template <typename T, int PRODUCT, typename S, bool DIRECT>
+__global__ __launch_bounds__(S::threads, S::threads >= 512 ? 2 : 1) void product_kernel(ProductArgs a, Split sp) {
+  using O = Operands<T, PRODUCT, S::BI, S::BJ, S::BK, S::threads, DIRECT>;
+  __shared__ __attribute__((aligned(1024))) char lds0[O::bytes];
+  __shared__ __attribute__((aligned(1024))) char lds1[O::bytes];
+
+  const Where at = where(sp.tiles_i, sp.tiles_j, sp.tiles_i * sp.tiles_j, sp.splits);
+  const int i0 = at.ti * S::BI;
+  const int64_t j0 = (int64_t)at.tj * S::BJ;
+  const int64_t first = at.split * sp.steps, last = min(a.depth, first + sp.steps);
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const int wi = wave % S::WI * (S::FI * 32), wj = wave / S::WI * (S::FJ * 32);
+  O o(a, i0, j0, last, t);
+
+  f32x16 acc[S::FI][S::FJ] = {};
 
   lds_char* const b0 = (lds_char*)lds0;
   lds_char* const b1 = (lds_char*)lds1;
   if (first < last) {
-    request(b0, first);
-    deliver(b0);
+    o.request(b0, first);
+    o.deliver(b0);
     __syncthreads();
     for (int64_t r = first;; r += 2 * S::BK) {
       const bool more = r + S::BK < last;
-      if (more) request(b1, r + S::BK);
-      multiply(b0);
+      if (more) o.request(b1, r + S::BK);
+      O::multiply(acc, b0, wi, wj, lane);
       if (!more) break;
-      deliver(b1);
+      o.deliver(b1);
       __syncthreads();
       const bool again = r + 2 * S::BK < last;
-      if (again) request(b0, r + 2 * S::BK);
-      multiply(b1);
+      if (again) o.request(b0, r + 2 * S::BK);
+      O::multiply(acc, b1, wi, wj, lane);
       if (!again) break;
-      deliver(b0);
+      o.deliver(b0);
       __syncthreads();
     }
   }
 
-  // The tile's end, one block of 32 x 32 after the other.  Lanes l and l + 32 hold runs of 4 of the same column of D: swapped, each
-  // has 16 consecutive i.  The blocks of a column of blocks wait in LDS, so that the code that ends one is there once.
+  // The tile's end, one block of 32 x 32 after the other; the blocks of a column of blocks wait in LDS, so that the code that ends
+  // one is there once.
   constexpr int kBlock = 4096, kHalf = S::WI * S::WJ / 2;
-  static_assert(kHalf * S::FI * kBlock <= A::bytes + B::bytes, "the blocks have to fit the operands' buffers");
+  static_assert(kHalf * S::FI * kBlock <= O::bytes, "the blocks have to fit the operands' buffers");
   __syncthreads();
   lds_char* const mine = (wave < kHalf ? b0 : b1) + (wave % kHalf) * (S::FI * kBlock) + lane * 16;
 #pragma clang loop unroll(disable)
@@ -646,30 +729,14 @@ __global__ __launch_bounds__(S::threads, S::threads >= 512 ? 2 : 1) void product
     for (int qq = 0; qq < S::FJ; ++qq) {
       if (qq != q) continue;
 #pragma unroll
-      for (int k = 0; k < S::FI; ++k)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          Chunk16 low, high;
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            const float x = acc[k][qq][4 * h + c], y = acc[k][qq][8 + 4 * h + c];
-            auto s = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, y), false, false);
-            low.w[c] = (uint32_t)s[0];
-            high.w[c] = (uint32_t)s[1];
-          }
-          B::put(mine + k * kBlock + 2 * h * 1024, low);
-          B::put(mine + k * kBlock + (2 * h + 1) * 1024, high);
-        }
+      for (int k = 0; k < S::FI; ++k) put_block(mine + k * kBlock, acc[k][qq]);
     }
     const int jj = wj + 32 * q + (lane & 31);
 #pragma clang loop unroll(disable)
     for (int k = 0; k < S::FI; ++k) {
       float v[16];
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const s16x8 x = *reinterpret_cast<const lds_s16x8*>(mine + k * kBlock + c * 1024);
-        __builtin_memcpy(v + 4 * c, &x, 16);
-      }
+      for (int c = 0; c < 4; ++c) get_piece(v + 4 * c, mine + k * kBlock + c * 1024);
       const int ii = wi + 32 * k + (lane >> 5) * 16;
       if (sp.splits > 1) {
         float* to = static_cast<float*>(a.workspace) + (((int64_t)at.split * sp.tiles_j + at.tj) * sp.tiles_i + at.ti) * (S::BI * S::BJ) + jj * S::BI + ii;
@@ -681,64 +748,168 @@ __global__ __launch_bounds__(S::threads, S::threads >= 512 ? 2 : 1) void product
   }
 }
 
-// Adds up the splits of a product in their order and ends it.  A thread takes 16 i of one j, neighbours a group of 32.
+// The same for few tiles: a workgroup's 8 wavefronts (4 of fp32) each have the whole tile and every 8th step of the sum, in LDS of
+// their own, so that nothing waits for another wavefront before the end, where the sums are added up in LDS in the wavefronts' order.
+template <typename T, int PRODUCT, int BI, int BJ, int BK, int WAVES, bool DIRECT>
+__global__ __launch_bounds__(WAVES * 64) void product_by_depth_kernel(ProductArgs a, Split sp) {
+  using O = Operands<T, PRODUCT, BI, BJ, BK, 64, DIRECT>;
+  constexpr int FI = BI / 32, FJ = BJ / 32, kBlock = 4096;
+  static_assert(FI * FJ * kBlock <= O::bytes, "a wavefront's sums have to fit its operands' place");
+  __shared__ __attribute__((aligned(1024))) char lds[WAVES * O::bytes];
+  const Where at = where(sp.tiles_i, sp.tiles_j, sp.tiles_i * sp.tiles_j, sp.splits);
+  const int i0 = at.ti * BI;
+  const int64_t j0 = (int64_t)at.tj * BJ;
+  const int64_t first = at.split * sp.steps, last = min(a.depth, first + sp.steps);
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  lds_char* const all = (lds_char*)lds;
+  lds_char* const mine = all + wave * O::bytes;
+  O o(a, i0, j0, last, lane);
+  f32x16 acc[FI][FJ] = {};
+  int64_t r = first + wave * BK;
+  if (r < last) o.request(mine, r);
+  while (r < last) {
+    o.deliver(mine);
+    // what this wavefront asked for is there
+    __builtin_amdgcn_s_waitcnt(0);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    const int64_t next = r + WAVES * BK;
+    if (!DIRECT && next < last) o.request(mine, next);      // into registers: behind the products
+    O::multiply(acc, mine, 0, 0, lane);
+    // every fragment has been read before LDS is written again
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    if (DIRECT && next < last) {
+      __builtin_amdgcn_s_waitcnt(0xc07f);                   // lgkmcnt(0)
+      o.request(mine, next);
+    }
+    r = next;
+  }
+#pragma unroll
+  for (int k = 0; k < FI; ++k)
+#pragma unroll
+    for (int q = 0; q < FJ; ++q) put_block(mine + (k * FJ + q) * kBlock + lane * 16, acc[k][q]);
+  __syncthreads();
+  // wavefront `block` ends that block: pieces of 16 i x 32 columns x 2
+  for (int block = wave; block < FI * FJ; block += WAVES) {
+    float v[16] = {};
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        float x[4];
+        get_piece(x, all + w * O::bytes + block * kBlock + c * 1024 + lane * 16);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[4 * c + e] += x[e];
+      }
+    const int ii = block / FJ * 32 + (lane >> 5) * 16, jj = block % FJ * 32 + (lane & 31);
+    if (sp.splits > 1) {
+      float* to = static_cast<float*>(a.workspace) + (((int64_t)at.split * sp.tiles_j + at.tj) * sp.tiles_i + at.ti) * (BI * BJ) + jj * BI + ii;
+      store_values(to, v, 16);
+    } else {
+      finish<T, PRODUCT>(v, a, j0 + jj, i0 + ii, j0 + jj < a.nj, 32);
+    }
+  }
+}
+
+// Adds up the splits of a product in their order and ends it.  A thread takes 4 i of one j, 8 neighbours a group of 32.
 template <typename T, int PRODUCT>
 __global__ __launch_bounds__(256) void join_kernel(ProductArgs a, Split sp, int bi, int bj) {
-  const int row = bi / 16;                              // threads to a row of a tile
+  const int row = bi / 4;                               // threads to a row of a tile
   const int64_t piece = (int64_t)blockIdx.x * 256 + threadIdx.x, per_tile = (int64_t)row * bj, tile = piece / per_tile;
-  const int in = (int)(piece - tile * per_tile), jj = in / row, ii = in % row * 16;
+  const int in = (int)(piece - tile * per_tile), jj = in / row, ii = in % row * 4;
   const int64_t j = tile / sp.tiles_i * bj + jj;
   const int i = (int)(tile % sp.tiles_i) * bi + ii;
   const int64_t all = (int64_t)sp.tiles_i * sp.tiles_j * bi * bj;
-  float v[16] = {};
+  float v[4] = {};
   if (j < a.nj && i < a.ni) {
     const float* from = static_cast<const float*>(a.workspace) + tile * (bi * bj) + jj * bi + ii;
+#pragma unroll 8
     for (int s = 0; s < sp.splits; ++s) {
-      float w[16];
-      load_values(w, from + s * all, 16);
-#pragma unroll
-      for (int k = 0; k < 16; ++k) v[k] += w[k];
+      const float4 w = *reinterpret_cast<const float4*>(from + s * all);
+      v[0] += w.x, v[1] += w.y, v[2] += w.z, v[3] += w.w;
     }
   }
   finish<T, PRODUCT>(v, a, j, i, j < a.nj, 1);
 }
 
+// Tiles of bi x bj, and the sum of `depth` in `splits` parts of whole steps.
+struct Plan {
+  Split sp;
+  int64_t tiles;
+};
+Plan plan(const ProductArgs& a, int bi, int bj, int step, int64_t splits) {
+  Plan p;
+  p.sp.tiles_i = (a.ni + bi - 1) / bi;
+  p.tiles = (a.nj + bj - 1) / bj * p.sp.tiles_i;
+  p.sp.tiles_j = (int)((a.nj + bj - 1) / bj);
+  const int64_t steps = (a.depth + step - 1) / step, fit = (int64_t)(kWorkspaceBytes / (sizeof(float) * bi * bj)) / p.tiles;
+  splits = std::max<int64_t>(1, std::min({splits, steps, fit}));
+  const int64_t per = std::max<int64_t>(1, (steps + splits - 1) / splits);
+  p.sp.splits = (int)std::max<int64_t>(1, (steps + per - 1) / per);
+  p.sp.steps = per * step;
+  return p;
+}
+
+template <typename T, int PRODUCT>
+hipError_t join(const ProductArgs& a, const Plan& p, int bi, int bj, hipStream_t s) {
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.sp.splits == 1) return e;
+  join_kernel<T, PRODUCT><<<dim3((unsigned)(p.tiles * bi * bj / 4 / 256)), 256, 0, s>>>(a, p.sp, bi, bj);
+  return hipGetLastError();
+}
+
 template <typename T, int PRODUCT, typename S, bool DIRECT>
 hipError_t run_product(const ProductArgs& a, hipStream_t s) {
-  Split sp;
-  sp.tiles_i = (a.ni + S::BI - 1) / S::BI;
-  const int64_t tiles_j = (a.nj + S::BJ - 1) / S::BJ, tiles = tiles_j * sp.tiles_i;
-  if (tiles > INT32_MAX) return hipErrorInvalidValue;
-  sp.tiles_j = (int)tiles_j;
   // Few tiles: the sum is split so that the CUs have work, each part at least 4 steps.
-  const int64_t steps = (a.depth + S::BK - 1) / S::BK, fit = (int64_t)(kWorkspaceBytes / (sizeof(float) * S::BI * S::BJ));
-  int64_t splits = std::max<int64_t>(1, std::min({steps / 4, 256 / tiles, fit / tiles}));
-  const int64_t per = std::max<int64_t>(1, (steps + splits - 1) / splits);
-  sp.splits = (int)std::max<int64_t>(1, (steps + per - 1) / per);
-  sp.steps = per * S::BK;
-  product_kernel<T, PRODUCT, S, DIRECT><<<dim3((unsigned)(tiles * sp.splits)), S::threads, 0, s>>>(a, sp);
-  if (sp.splits > 1) join_kernel<T, PRODUCT><<<dim3((unsigned)(tiles * S::BI * S::BJ / 16 / 256)), 256, 0, s>>>(a, sp, S::BI, S::BJ);
-  return hipGetLastError();
+  const int64_t tiles = (int64_t)((a.ni + S::BI - 1) / S::BI) * ((a.nj + S::BJ - 1) / S::BJ);
+  const Plan p = plan(a, S::BI, S::BJ, S::BK, std::min<int64_t>((a.depth / S::BK) / 4, 256 / tiles));
+  if (p.tiles > INT32_MAX) return hipErrorInvalidValue;
+  product_kernel<T, PRODUCT, S, DIRECT><<<dim3((unsigned)(p.tiles * p.sp.splits)), S::threads, 0, s>>>(a, p.sp);
+  return join<T, PRODUCT>(a, p, S::BI, S::BJ, s);
+}
+
+template <typename T, int PRODUCT, int BI, int BJ, int BK, int WAVES, bool DIRECT>
+hipError_t run_by_depth(const ProductArgs& a, hipStream_t s) {
+  const int64_t tiles = (int64_t)((a.ni + BI - 1) / BI) * ((a.nj + BJ - 1) / BJ);
+  const int64_t rounds = (a.depth + WAVES * BK - 1) / (WAVES * BK);
+  const Plan p = plan(a, BI, BJ, WAVES * BK, rounds >= 6 ? std::min<int64_t>(rounds / 3, 512 / tiles) : 1);
+  if (p.tiles > INT32_MAX) return hipErrorInvalidValue;
+  product_by_depth_kernel<T, PRODUCT, BI, BJ, BK, WAVES, DIRECT><<<dim3((unsigned)(p.tiles * p.sp.splits)), WAVES * 64, 0, s>>>(a, p.sp);
+  return join<T, PRODUCT>(a, p, BI, BJ, s);
 }
 
 bool whole_chunks(const void* p, int64_t ld, int64_t length) {
   return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0 && length % 8 == 0;
 }
 
+template <typename T, int PRODUCT, bool DIRECT>
+hipError_t by_size(const ProductArgs& a, hipStream_t s) {
+  const int64_t middle = (int64_t)((a.ni + 127) / 128) * ((a.nj + 127) / 128);
+  if constexpr (std::is_same_v<T, float>) {
+    const int64_t big = (int64_t)((a.ni + 255) / 256) * ((a.nj + 127) / 128);
+    if (big >= 128) return run_product<T, PRODUCT, Shape<256, 128, 4, 2, 32>, DIRECT>(a, s);
+    if (middle >= 128) return run_product<T, PRODUCT, Shape<128, 128, 2, 2, 32>, DIRECT>(a, s);
+    if (a.nj <= 32) return run_by_depth<T, PRODUCT, 64, 32, 32, 8, DIRECT>(a, s);
+    return run_by_depth<T, PRODUCT, 64, 64, 32, 6, DIRECT>(a, s);
+  } else {
+    const int64_t big = (int64_t)((a.ni + 255) / 256) * ((a.nj + 255) / 256);
+    // operands that go through registers leave none for 256 x 256
+    if (big >= 128) return run_product<T, PRODUCT, std::conditional_t<DIRECT, Shape<256, 256, 2, 4, 64>, Shape<256, 128, 4, 2, 64>>, DIRECT>(a, s);
+    if (middle >= 128) return run_product<T, PRODUCT, Shape<128, 128, 2, 2, 64>, DIRECT>(a, s);
+    if (a.nj <= 32) return run_by_depth<T, PRODUCT, 64, 32, 64, 8, DIRECT>(a, s);
+    return run_by_depth<T, PRODUCT, 64, 64, 64, 8, DIRECT>(a, s);
+  }
+}
+
 template <typename T, int PRODUCT>
 hipError_t product(const ProductArgs& a, hipStream_t s) {
-  if constexpr (std::is_same_v<T, float>) {
-    const int64_t big = ((a.ni + 255) / 256) * ((a.nj + 127) / 128);
-    if (big >= 128) return run_product<T, PRODUCT, Shape<256, 128, 4, 2, 32>, false>(a, s);
-    return run_product<T, PRODUCT, Shape<128, 128, 2, 2, 32>, false>(a, s);
-  } else {
+  if constexpr (!std::is_same_v<T, float>) {
     const bool direct = (PRODUCT == kWeightGrad || whole_chunks(a.a, a.lda, PRODUCT == kForward ? a.depth : a.ni)) &&
                         whole_chunks(a.b, a.ldb, PRODUCT == kWeightGrad ? a.nj : a.depth);
-    const int64_t big = ((a.ni + 255) / 256) * ((a.nj + 255) / 256);
-    if (big >= 128)
-      return direct ? run_product<T, PRODUCT, Shape<256, 256, 2, 4, 64>, true>(a, s) : run_product<T, PRODUCT, Shape<256, 256, 2, 4, 64>, false>(a, s);
-    return direct ? run_product<T, PRODUCT, Shape<128, 128, 2, 2, 64>, true>(a, s) : run_product<T, PRODUCT, Shape<128, 128, 2, 2, 64>, false>(a, s);
+    if (direct) return by_size<T, PRODUCT, true>(a, s);
   }
+  return by_size<T, PRODUCT, false>(a, s);
 }
 
 template <typename F>
