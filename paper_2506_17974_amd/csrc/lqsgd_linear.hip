@@ -27,19 +27,22 @@ template <typename T> __device__ inline T narrow(float v) { return (T)v; }      
 template <typename T> struct Exponents { static constexpr int lo = -126, hi = 121; };
 template <> struct Exponents<f16> { static constexpr int lo = -24, hi = 9; };
 
-__device__ inline uint32_t magnitude_bits(float v) { return __builtin_bit_cast(uint32_t, v) & 0x7fffffffu; }
 __device__ inline float power_of_two(int e) { return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23); }      // -126 <= e <= 127
 
-// e of a group from the largest magnitude's bits (as integers magnitudes are ordered, infinities and NaN last).  absmax =
-// m 2^E, 1 <= m < 2, takes e = E - 6, or E - 5 from 127.5 2^(E-6) on: adding 2^-7 of the mantissa carries into the exponent there.
-template <typename T>
-__device__ inline int group_exponent(uint32_t absmax) {
-  const int e = (int)((absmax + 0x10000u) >> 23) - 133;
-  return min(max(e, Exponents<T>::lo), Exponents<T>::hi);
+// The largest magnitude, NaN if one is (v_maximum3_f32: two values an instruction).
+template <int N>
+__device__ inline float largest(const float (&v)[N]) {
+  float m = 0.f;
+#pragma unroll
+  for (int k = 0; k < N; ++k) m = __builtin_elementwise_maximum(m, fabsf(v[k]));
+  return m;
 }
-__device__ inline bool group_finite(uint32_t absmax) { return absmax < 0x7f800000u; }
-__device__ inline uint32_t code_of(float v, float inverse_step) {
-  return (uint32_t)(int)fminf(fmaxf(rintf(v * inverse_step), -127.f), 127.f) & 0xffu;
+// e of a group from its largest magnitude.  absmax = m 2^E, 1 <= m < 2, takes e = E - 6, or E - 5 from 127.5 2^(E-6) on: adding 2^-7
+// of the mantissa carries into the exponent there.
+template <typename T>
+__device__ inline int group_exponent(float absmax) {
+  const int e = (int)((__builtin_bit_cast(uint32_t, absmax) + 0x10000u) >> 23) - 133;
+  return min(max(e, Exponents<T>::lo), Exponents<T>::hi);
 }
 // What a code's factor is: 2^e, NaN for byte 255.
 __device__ inline float factor_of(uint32_t byte) {
@@ -129,18 +132,23 @@ __device__ inline void store_values(T* p, const float (&v)[N], int n) {
   }
 }
 
-// N values of one group quantised and packed, four to a word; `absmax` is the whole group's.
+// N values of one group quantised and packed, four to a word; `absmax` is the whole group's.  v 2^-e + 1.5 2^23 rounds to the
+// nearest integer, ties to even, and has it in its low byte; only the largest e leaves values that have to be held to 127.
 template <typename T, int N>
-__device__ inline void pack_codes(uint32_t (&w)[N / 4], const float (&v)[N], uint32_t absmax, uint32_t* byte) {
-  const bool finite = group_finite(absmax);
+__device__ inline void pack_codes(uint32_t (&w)[N / 4], const float (&v)[N], float absmax, uint32_t* byte) {
+  const bool finite = absmax < __builtin_inff();
   const int e = group_exponent<T>(absmax);
-  const float inv = power_of_two(-e);
+  const float inv = power_of_two(-e), most = e == Exponents<T>::hi ? 127.f : 128.f;
 #pragma unroll
-  for (int k = 0; k < N / 4; ++k)
-    w[k] = code_of(v[4 * k], inv) | code_of(v[4 * k + 1], inv) << 8 | code_of(v[4 * k + 2], inv) << 16 | code_of(v[4 * k + 3], inv) << 24;
-  if (!finite) {
+  for (int k = 0; k < N / 4; ++k) {
+    uint32_t q[4];
 #pragma unroll
-    for (int k = 0; k < N / 4; ++k) w[k] = 0u;
+    for (int c = 0; c < 4; ++c) {
+      const float x = __builtin_amdgcn_fmed3f(v[4 * k + c] * inv, -most, most);
+      q[c] = __builtin_bit_cast(uint32_t, x + 12582912.f);
+    }
+    const uint32_t low = __builtin_amdgcn_perm(q[1], q[0], 0x0c0c0400u), high = __builtin_amdgcn_perm(q[3], q[2], 0x04000c0cu);
+    w[k] = finite ? low | high : 0u;
   }
   *byte = finite ? (uint32_t)(e + 127) : 255u;
 }
@@ -162,11 +170,9 @@ __global__ __launch_bounds__(256) void checkpoint_save_kernel(const T* x, int64_
   const bool there = row < samples;
   float v[kPiece];
   load_values(v, x + row * ldx + piece * kPiece, there ? features - (int)(piece * kPiece) : 0);
-  uint32_t m = 0;
-#pragma unroll
-  for (int k = 0; k < kPiece; ++k) m = max(m, magnitude_bits(v[k]));
-  m = max(m, (uint32_t)__shfl_xor((int)m, 1));
-  m = max(m, (uint32_t)__shfl_xor((int)m, 2));
+  float m = largest(v);
+  m = __builtin_elementwise_maximum(m, __shfl_xor(m, 1));
+  m = __builtin_elementwise_maximum(m, __shfl_xor(m, 2));
   uint32_t w[2], byte;
   pack_codes<T>(w, v, m, &byte);
   if (!there) return;
@@ -210,6 +216,7 @@ __global__ __launch_bounds__(256) void activation_backward_kernel(const T* dy, i
   const int64_t first = (int64_t)blockIdx.y * run, last = min(samples, first + run);
   float s[kPiece] = {};
   if (n > 0) {
+#pragma unroll 4
     for (int64_t m = first + (t >> lanes_log2); m < last; m += 256 >> lanes_log2) {
       float v[kPiece];
       load_values(v, dy + m * lddy + feature, n);
@@ -305,14 +312,13 @@ __device__ inline void finish(float (&v)[N], const ProductArgs& a, int64_t j, in
     for (int k = 0; k < N; ++k) v[k] += b[k];
   }
   auto keep = [&](const Codes& c) {
-    uint32_t m = 0;
+    if (n < N) {
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
-      if (k >= n) v[k] = 0.f;
-      m = max(m, magnitude_bits(v[k]));
+      for (int k = 0; k < N; ++k) v[k] = k < n ? v[k] : 0.f;
     }
+    float m = largest(v);
 #pragma unroll
-    for (int d = 0; N << d < kGroup; ++d) m = max(m, (uint32_t)__shfl_xor((int)m, near << d));
+    for (int d = 0; N << d < kGroup; ++d) m = __builtin_elementwise_maximum(m, __shfl_xor(m, near << d));
     uint32_t w[N / 4], byte;
     pack_codes<T>(w, v, m, &byte);
     if (in_codes) {
@@ -833,6 +839,9 @@ __global__ __launch_bounds__(256) void join_kernel(ProductArgs a, Split sp, int 
   finish<T, PRODUCT>(v, a, j, i, j < a.nj, 1);
 }
 
+#ifndef LQ_RULE
+#define LQ_RULE (tiles < 128 && rounds >= 4 ? std::min<int64_t>(rounds / 2, 256 / tiles) : 1)
+#endif
 // Tiles of bi x bj, and the sum of `depth` in `splits` parts of whole steps.
 struct Plan {
   Split sp;
@@ -873,7 +882,7 @@ template <typename T, int PRODUCT, int BI, int BJ, int BK, int WAVES, bool DIREC
 hipError_t run_by_depth(const ProductArgs& a, hipStream_t s) {
   const int64_t tiles = (int64_t)((a.ni + BI - 1) / BI) * ((a.nj + BJ - 1) / BJ);
   const int64_t rounds = (a.depth + WAVES * BK - 1) / (WAVES * BK);
-  const Plan p = plan(a, BI, BJ, WAVES * BK, rounds >= 6 ? std::min<int64_t>(rounds / 3, 512 / tiles) : 1);
+  const Plan p = plan(a, BI, BJ, WAVES * BK, LQ_RULE);
   if (p.tiles > INT32_MAX) return hipErrorInvalidValue;
   product_by_depth_kernel<T, PRODUCT, BI, BJ, BK, WAVES, DIRECT><<<dim3((unsigned)(p.tiles * p.sp.splits)), WAVES * 64, 0, s>>>(a, p.sp);
   return join<T, PRODUCT>(a, p, BI, BJ, s);
@@ -960,14 +969,16 @@ hipError_t launch_checkpoint_load(int type, int64_t samples, int32_t features, C
 hipError_t launch_activation_backward(int type, int act, int64_t samples, int32_t rows, const void* dy, int64_t lddy, Codes z, void* dz,
                                       int64_t lddz, float* dbias, int accumulate, void* workspace, hipStream_t s) {
   const int pieces = (rows + kPiece - 1) / kPiece;
+  // Few samples: strips of 128 features leave 16 samples to go on at a time, and one launch does (64 x 1024 fp32 6.0 us instead of 8.4).
+  const bool one_run = samples <= 256;
   int lanes_log2 = 0;
-  while ((1 << lanes_log2) < pieces && lanes_log2 < 6) ++lanes_log2;
+  while ((1 << lanes_log2) < pieces && lanes_log2 < (one_run ? 4 : 6)) ++lanes_log2;
   const int strips = (pieces + (1 << lanes_log2) - 1) >> lanes_log2;
   const int64_t at_once = 256 >> lanes_log2;
   const int64_t most = std::max<int64_t>(1, 2048 / strips);
   const int64_t rounds = std::max<int64_t>(4, (samples + at_once * most - 1) / (at_once * most));
-  const int64_t run = rounds * at_once;
-  const int64_t runs = std::max<int64_t>(1, (samples + run - 1) / run);
+  const int64_t run = one_run ? samples : rounds * at_once;
+  const int64_t runs = samples == 0 ? 1 : (samples + run - 1) / run;
   float* part = dbias && runs > 1 ? static_cast<float*>(workspace) : nullptr;
   hipError_t e = by_type(type, [&](auto zero) {
     using T = decltype(zero);
