@@ -379,13 +379,13 @@ struct Tile {
   static constexpr int chunks = row_chunks * rows;
   static constexpr int bytes = chunks * 16;
   __device__ static inline int moved(int row) {
-    static_assert(row_chunks == 4 || row_chunks == 8 || (ORDER != kDepthRuns && row_chunks % 16 == 0), "the exchange stays within a row");
+    static_assert(row_chunks == 4 || row_chunks == 8 || (ORDER == kDepthRuns ? row_chunks == 2 : row_chunks % 16 == 0), "the exchange stays within a row");
     if (ORDER != kDepthRuns) {            // pairs of chunks
       if (row_chunks == 4) return row & 2;
       if (row_chunks == 8) return (row & 3) << 1;
       return (2 * (row & 1) + 5 * (row >> 1 & 1)) << 1;
     }
-    return row_chunks == 8 ? (row & 7) ^ (row >> 3 & 1) : (row >> 1 & 3) ^ (row >> 3 & 1);
+    return row_chunks == 8 ? (row & 7) ^ (row >> 3 & 1) : row_chunks == 4 ? (row >> 1 & 3) ^ (row >> 3 & 1) : (row >> 2 ^ row >> 3) & 1;
   }
   __device__ static inline int place(int row, int chunk) { return (row * row_chunks + (chunk ^ moved(row))) * 16; }
   // The 8 elements that a lane holds of rows n0 .. n0 + 31 and r = r0 .. r0 + 15 (n0 a multiple of 32, r0 of 16).
@@ -452,9 +452,10 @@ template <typename T, typename E, int ORDER, int N, int K, int PLANES, int THREA
 struct Operand {
   using L = Tile<ORDER, N, K>;
   static constexpr int bytes = L::bytes * PLANES;
-  // kHeld: a thread takes 16 codes, two chunks
-  static constexpr int per_thread = ORDER == kHeld ? L::chunks / 2 / THREADS : L::chunks / THREADS;
-  static_assert(per_thread > 0 && per_thread * THREADS * (ORDER == kHeld ? 2 : 1) == L::chunks, "the tile has to be shared out evenly");
+  // kHeld: a thread takes 16 codes, two chunks.  Some wavefronts may have no part of a small tile.
+  static constexpr int pieces = ORDER == kHeld ? L::chunks / 2 : L::chunks, per_thread = (pieces + THREADS - 1) / THREADS;
+  static_assert(pieces % 64 == 0 && (!DIRECT || pieces % THREADS == 0), "the tile has to be shared out evenly");
+  __device__ static inline bool mine(int piece) { return pieces % THREADS == 0 || piece < pieces; }
 
   const T* base;         // row n0 (kDepthRuns) or column n0 (kIndexRuns)
   int64_t ld;
@@ -467,41 +468,60 @@ struct Operand {
   // in flight between load() and store()
   struct Empty {};
   using Raw = std::conditional_t<std::is_same_v<T, float>, float[8], Chunk16>;
-  std::conditional_t<DIRECT, Empty, Raw[ORDER == kHeld ? 1 : per_thread]> raw;
-  std::conditional_t<ORDER == kHeld, Chunk16[per_thread], Empty> codes;
-  std::conditional_t<ORDER == kHeld, uint32_t[per_thread], Empty> exps;
+  struct Regs {
+    std::conditional_t<DIRECT || ORDER == kHeld, Empty, Raw[per_thread]> raw;
+    std::conditional_t<ORDER == kHeld, Chunk16[per_thread], Empty> codes;
+    std::conditional_t<ORDER == kHeld, uint32_t[per_thread], Empty> exps;
+  };
 
   // Straight into LDS, 16 bytes a lane: memory rows start at multiples of 16 bytes and are whole chunks.  Lanes that have nothing
-  // there get an offset out of the buffer's range, which reads as 0.
-  __device__ inline void load_direct(lds_char* to, int64_t r0) {
-    constexpr int kNowhere = (int)0x80000000u;
+  // there get an offset out of the buffer's range, which reads as 0.  The load is written out because the compiler, which knows
+  // what it writes but not which of it has been waited for, would wait for all of them before any read of LDS: whoever calls this
+  // waits for it (vmcnt) before a barrier and the first read.
+  static constexpr int kNowhere = (int)0x80000000u;
+  int offset[DIRECT ? per_thread : 1];
+  __device__ inline void prepare_direct() {
     const int wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63;
-    const int left = (int)min((int64_t)K, depth - r0);
-    const T* from = base + (ORDER == kDepthRuns ? r0 : r0 * ld);
-    __amdgpu_buffer_rsrc_t buffer = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(from), 0, 0x7fffffff, 0x00020000);
 #pragma unroll
     for (int k = 0; k < per_thread; ++k) {
       const int piece = (wave * per_thread + k) * 64 + lane, row = piece / L::row_chunks;
       const int chunk = (piece % L::row_chunks) ^ L::moved(row);
-      const bool there = ORDER == kDepthRuns ? row < n && chunk * 8 < left : row < left && chunk * 8 < n;
-      const int offset = there ? (row * (int)ld + chunk * 8) * 2 : kNowhere;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer, reinterpret_cast<lds_void*>(to + (wave * per_thread + k) * 1024), 16, offset, 0, 0, 0);
+      offset[k] = (ORDER == kDepthRuns ? row : chunk * 8) < n ? (row * (int)ld + chunk * 8) * 2 : kNowhere;
+    }
+  }
+  __device__ inline void load_direct(lds_char* to, int64_t r0) const {
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    const int wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63;
+    const uint64_t from = (uint64_t)(base + (ORDER == kDepthRuns ? r0 : r0 * ld));
+    const u32x4 buffer = {(uint32_t)from, (uint32_t)(from >> 32) & 0xffffu, 0x7fffffffu, 0x00020000u};
+    const uint32_t at = (uint32_t)(uintptr_t)to + (uint32_t)(wave * per_thread) * 1024;
+    const int64_t left = depth - r0;
+#pragma unroll
+    for (int k = 0; k < per_thread; ++k) {
+      int o = offset[k];
+      if (left < K) {
+        const int piece = (wave * per_thread + k) * 64 + lane, row = piece / L::row_chunks;
+        const int r = ORDER == kDepthRuns ? ((piece % L::row_chunks) ^ L::moved(row)) * 8 : row;
+        o = r < left ? o : kNowhere;
+      }
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                   :: "s"(at + k * 1024), "v"(o), "s"(buffer) : "memory", "m0");
     }
   }
 
   // Through registers: memory of any alignment, rows of any length.
-  __device__ inline void load(int64_t r0) {
+  __device__ inline void load(Regs& g, int64_t r0) {
     const int left = (int)min((int64_t)K, depth - r0);
     if constexpr (ORDER == kHeld) {
 #pragma unroll
       for (int k = 0; k < per_thread; ++k) {
         const int piece = k * THREADS + t, r = piece / (N / 16), i = piece % (N / 16) * 16;
-        codes[k] = Chunk16{};
-        exps[k] = 0;
-        if (r < left && i < n) {         // codes go on to the end of their group of 32
+        g.codes[k] = Chunk16{};
+        g.exps[k] = 0;
+        if (mine(piece) && r < left && i < n) {         // codes go on to the end of their group of 32
           const int64_t row = r0 + r;
-          codes[k] = *reinterpret_cast<const Chunk16*>(held.codes + row * ((int64_t)groups * kGroup) + i);
-          exps[k] = held.exponents[row * groups + i / kGroup];
+          g.codes[k] = *reinterpret_cast<const Chunk16*>(held.codes + row * ((int64_t)groups * kGroup) + i);
+          g.exps[k] = held.exponents[row * groups + i / kGroup];
         }
       }
     } else {
@@ -512,44 +532,48 @@ struct Operand {
 #pragma unroll
         for (int k = 0; k < per_thread; ++k) {
           const int piece = k * THREADS + t;
-          __builtin_memcpy(&raw[k], from + (int64_t)(piece / L::row_chunks) * ld + piece % L::row_chunks * 8, 8 * sizeof(T));
+          if (!mine(piece)) break;
+          __builtin_memcpy(&g.raw[k], from + (int64_t)(piece / L::row_chunks) * ld + piece % L::row_chunks * 8, 8 * sizeof(T));
         }
       } else if (length >= kPart) {
         const T* safe = from + (min(run, kPart) - kPart);      // a run that starts the tensor's first row is that long
 #pragma unroll
         for (int k = 0; k < per_thread; ++k) {
           const int piece = k * THREADS + t, row = piece / L::row_chunks, chunk = piece % L::row_chunks;
+          if (!mine(piece)) break;
 #pragma unroll
           for (int h = 0; h < kParts; ++h) {
             const int valid = row < rows ? min(max(run - chunk * 8 - h * kPart, 0), kPart) : 0;
             const Chunk16 c = load_tail(from + (int64_t)row * ld + chunk * 8 + h * kPart, valid, safe);
-            __builtin_memcpy(reinterpret_cast<char*>(&raw[k]) + 16 * h, &c, 16);
+            __builtin_memcpy(reinterpret_cast<char*>(&g.raw[k]) + 16 * h, &c, 16);
           }
         }
       } else {
 #pragma unroll
         for (int k = 0; k < per_thread; ++k) {
           const int piece = k * THREADS + t, row = piece / L::row_chunks, chunk = piece % L::row_chunks;
+          if (!mine(piece)) break;
           const T* p = from + (int64_t)row * ld + chunk * 8;
           T v[8];
 #pragma unroll
           for (int q = 0; q < 8; ++q) v[q] = row < rows && q < run - chunk * 8 ? p[q] : T(0.f);
-          __builtin_memcpy(&raw[k], v, 8 * sizeof(T));
+          __builtin_memcpy(&g.raw[k], v, 8 * sizeof(T));
         }
       }
     }
   }
-  __device__ inline void store(lds_char* to) {
+  __device__ inline void store(const Regs& g, lds_char* to) const {
     if constexpr (ORDER == kHeld) {
 #pragma unroll
       for (int k = 0; k < per_thread; ++k) {
         const int piece = k * THREADS + t, r = piece / (N / 16), i = piece % (N / 16) * 16;
-        const float f = factor_of(exps[k]);
+        if (!mine(piece)) break;
+        const float f = factor_of(g.exps[k]);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           E e[8];
 #pragma unroll
-          for (int q = 0; q < 8; ++q) e[q] = narrow<E>((float)(int8_t)(codes[k].w[2 * h + q / 4] >> (8 * (q & 3))) * f);
+          for (int q = 0; q < 8; ++q) e[q] = narrow<E>((float)(int8_t)(g.codes[k].w[2 * h + q / 4] >> (8 * (q & 3))) * f);
           put(to + L::place(r, i / 8 + h), __builtin_bit_cast(Chunk16, e));
         }
       }
@@ -557,13 +581,14 @@ struct Operand {
 #pragma unroll
       for (int k = 0; k < per_thread; ++k) {
         const int piece = k * THREADS + t, at = L::place(piece / L::row_chunks, piece % L::row_chunks);
+        if (!mine(piece)) break;
         if constexpr (PLANES == 3) {
           Chunk16 c[3];
-          split3(raw[k], c);
+          split3(g.raw[k], c);
 #pragma unroll
           for (int p = 0; p < 3; ++p) put(to + p * L::bytes + at, c[p]);
         } else {
-          put(to + at, raw[k]);
+          put(to + at, g.raw[k]);
         }
       }
     }
@@ -571,10 +596,10 @@ struct Operand {
   __device__ static inline void put(lds_char* to, const Chunk16& c) { *reinterpret_cast<lds_s16x8*>(to) = __builtin_bit_cast(s16x8, c); }
 };
 
-// What a kernel's workgroups look like: BI x BJ of D, WI x WJ wavefronts, BK values of r at a time.
-template <int BI_, int BJ_, int WI_, int WJ_, int BK_>
+// What a kernel's workgroups look like: BI x BJ of D, WI x WJ wavefronts, steps of BK values of r, BUFFERS of them in LDS.
+template <int BI_, int BJ_, int WI_, int WJ_, int BK_, int BUFFERS_>
 struct Shape {
-  static constexpr int BI = BI_, BJ = BJ_, WI = WI_, WJ = WJ_, BK = BK_, threads = 64 * WI * WJ, FI = BI / WI / 32, FJ = BJ / WJ / 32;
+  static constexpr int BI = BI_, BJ = BJ_, WI = WI_, WJ = WJ_, BK = BK_, buffers = BUFFERS_, threads = 64 * WI * WJ, FI = BI / WI / 32, FJ = BJ / WJ / 32;
 };
 
 // The tile and split of a workgroup.  Workgroups go round the 8 XCDs; each XCD gets a run of consecutive tiles, which go in bands
@@ -621,30 +646,44 @@ struct Operands {
     b.ld = p.ldb; b.n = (int)min((int64_t)BJ, p.nj - j0); b.depth = last; b.t = t;
     b.length = kOrderB == kDepthRuns ? (int)p.depth : (int)p.nj;
     b.base = static_cast<const T*>(p.b) + (kOrderB == kDepthRuns ? j0 * p.ldb : j0);
+    if constexpr (kDirectA) a.prepare_direct();
+    if constexpr (DIRECT) b.prepare_direct();
   }
-  // Values of r from r0 on are asked for; deliver() puts those that go through registers into LDS.
-  __device__ inline void request(lds_char* to, int64_t r0) {
-    if constexpr (kDirectA) a.load_direct(to, r0); else a.load(r0);
-    if constexpr (DIRECT) b.load_direct(to + A::bytes, r0); else b.load(r0);
+  static constexpr bool kRegisters = !kDirectA || !DIRECT;     // something goes through registers
+  static constexpr int direct_loads = (kDirectA ? A::per_thread : 0) + (DIRECT ? B::per_thread : 0);
+  struct Regs {
+    typename A::Regs a;
+    typename B::Regs b;
+  };
+  // Values of r from r0 on: fetch() brings those that go straight into LDS (beyond the end: zeros), request() asks for those that
+  // go through registers, deliver() puts those into LDS.
+  __device__ inline void fetch(lds_char* to, int64_t r0) {
+    if constexpr (kDirectA) a.load_direct(to, r0);
+    if constexpr (DIRECT) b.load_direct(to + A::bytes, r0);
   }
-  __device__ inline void deliver(lds_char* to) {
-    if constexpr (!kDirectA) a.store(to);
-    if constexpr (!DIRECT) b.store(to + A::bytes);
+  __device__ inline void request(Regs& g, int64_t r0) {
+    if constexpr (!kDirectA) a.load(g.a, r0);
+    if constexpr (!DIRECT) b.load(g.b, r0);
   }
-  // acc += the products of the tile's rows from wi, wj on.
+  __device__ inline void deliver(const Regs& g, lds_char* to) const {
+    if constexpr (!kDirectA) a.store(g.a, to);
+    if constexpr (!DIRECT) b.store(g.b, to + A::bytes);
+  }
+  // The operands of 16 values of r, FI x FJ blocks from rows wi, wj of the tile on, and acc += their products.
   template <int FI, int FJ>
-  __device__ static inline void multiply(f32x16 (&acc)[FI][FJ], const lds_char* from, int wi, int wj, int lane) {
-#pragma unroll
-    for (int r = 0; r < BK; r += 16) {
-      s16x8 fa[PA][FI], fb[PB][FJ];
+  struct Fragments {
+    s16x8 a[PA][FI], b[PB][FJ];
+    __device__ inline void read(const lds_char* from, int wi, int wj, int r, int lane) {
 #pragma unroll
       for (int p = 0; p < PA; ++p)
 #pragma unroll
-        for (int k = 0; k < FI; ++k) fa[p][k] = A::L::fragment(from + p * A::L::bytes, wi + 32 * k, r, lane);
+        for (int k = 0; k < FI; ++k) a[p][k] = A::L::fragment(from + p * A::L::bytes, wi + 32 * k, r, lane);
 #pragma unroll
       for (int p = 0; p < PB; ++p)
 #pragma unroll
-        for (int k = 0; k < FJ; ++k) fb[p][k] = B::L::fragment(from + A::bytes + p * B::L::bytes, wj + 32 * k, r, lane);
+        for (int k = 0; k < FJ; ++k) b[p][k] = B::L::fragment(from + A::bytes + p * B::L::bytes, wj + 32 * k, r, lane);
+    }
+    __device__ inline void multiply(f32x16 (&acc)[FI][FJ]) const {
       // products of terms whose places add up to 2, 1, 0: the smaller ones first; those beyond are under 2^-22 of the product
 #pragma unroll
       for (int sum = PA + PB > 2 ? 2 : 0; sum >= 0; --sum)
@@ -654,10 +693,10 @@ struct Operands {
 #pragma unroll
           for (int k = 0; k < FI; ++k)
 #pragma unroll
-            for (int q = 0; q < FJ; ++q) acc[k][q] = mfma<E>(fa[p][k], fb[sum - p][q], acc[k][q]);
+            for (int q = 0; q < FJ; ++q) acc[k][q] = mfma<E>(a[p][k], b[sum - p][q], acc[k][q]);
         }
     }
-  }
+  };
 };
 
 // A block of D as the matrix instructions leave it, put to LDS as 4 pieces of 16 bytes a lane, 1 KiB apart: lanes l and l + 32 hold
@@ -688,8 +727,13 @@ __device__ inline void get_piece(float* v, const lds_char* from) {
 template <typename T, int PRODUCT, typename S, bool DIRECT>
 __global__ __launch_bounds__(S::threads, S::threads >= 512 ? 2 : 1) void product_kernel(ProductArgs a, Split sp) {
   using O = Operands<T, PRODUCT, S::BI, S::BJ, S::BK, S::threads, DIRECT>;
+  // an array each: what is on its way into one is not waited for where another is read
   __shared__ __attribute__((aligned(1024))) char lds0[O::bytes];
   __shared__ __attribute__((aligned(1024))) char lds1[O::bytes];
+  __shared__ __attribute__((aligned(1024))) char lds2[O::bytes];
+  __shared__ __attribute__((aligned(1024))) char lds3[S::buffers == 4 ? O::bytes : 1024];
+  static_assert(S::buffers == 3 || S::buffers == 4);
+  auto buffer = [&](int k) { return k == 0 ? (lds_char*)lds0 : k == 1 ? (lds_char*)lds1 : k == 2 ? (lds_char*)lds2 : (lds_char*)lds3; };
 
   const Where at = where(sp.tiles_i, sp.tiles_j, sp.tiles_i * sp.tiles_j, sp.splits);
   const int i0 = at.ti * S::BI;
@@ -701,34 +745,68 @@ __global__ __launch_bounds__(S::threads, S::threads >= 512 ? 2 : 1) void product
 
   f32x16 acc[S::FI][S::FJ] = {};
 
-  lds_char* const b0 = (lds_char*)lds0;
-  lds_char* const b1 = (lds_char*)lds1;
+  // A step's last products run from registers, behind the barrier that makes the next step's operands everyone's, beside the reads of
+  // those; its buffer is free from that barrier on and is filled for `buffers` steps ahead.  What goes through registers is asked for
+  // four steps ahead and put to LDS two steps ahead, with vector instructions (splitting, decoding) that one half of the wavefronts
+  // (a SIMD has one of each half) executes before its products and the other half behind them, beside the other's matrix instructions.
+  constexpr int kWaitFetched = 0x0070 | ((S::buffers - 2) * O::direct_loads & 15) | ((S::buffers - 2) * O::direct_loads >> 4) << 14;   // vmcnt, lgkmcnt(0)
+  const bool early = wave < S::WI * S::WJ / 2;
+  typename O::template Fragments<S::FI, S::FJ> now, next;
+  typename O::Regs g0, g1;
+  auto step = [&](lds_char* const here, lds_char* const there, lds_char* const ahead, typename O::Regs& g, int64_t r) {
+#pragma unroll
+    for (int k = 16; k < S::BK; k += 16) {
+      next.read(here, wi, wj, k, lane);
+      now.multiply(acc);
+      now = next;
+    }
+    __builtin_amdgcn_s_waitcnt(kWaitFetched);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    o.fetch(here, r + S::buffers * S::BK);
+    next.read(there, wi, wj, 0, lane);
+    auto bring = [&]() {
+      if (!O::kRegisters) return;
+      o.deliver(g, ahead);
+      if (r + 4 * S::BK < last) o.request(g, r + 4 * S::BK);
+    };
+    if (early) bring();
+    now.multiply(acc);
+    if (!early) bring();
+    now = next;
+  };
   if (first < last) {
-    o.request(b0, first);
-    o.deliver(b0);
+    o.request(g0, first);
+    if (first + S::BK < last) o.request(g1, first + S::BK);
+#pragma unroll
+    for (int k = 0; k < S::buffers; ++k) o.fetch(buffer(k), first + k * S::BK);
+    o.deliver(g0, buffer(0));
+    o.deliver(g1, buffer(1));
+    if (first + 2 * S::BK < last) o.request(g0, first + 2 * S::BK);
+    if (first + 3 * S::BK < last) o.request(g1, first + 3 * S::BK);
+    __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
-    for (int64_t r = first;; r += 2 * S::BK) {
-      const bool more = r + S::BK < last;
-      if (more) o.request(b1, r + S::BK);
-      O::multiply(acc, b0, wi, wj, lane);
-      if (!more) break;
-      o.deliver(b1);
-      __syncthreads();
-      const bool again = r + 2 * S::BK < last;
-      if (again) o.request(b0, r + 2 * S::BK);
-      O::multiply(acc, b1, wi, wj, lane);
-      if (!again) break;
-      o.deliver(b0);
-      __syncthreads();
+    now.read(buffer(0), wi, wj, 0, lane);
+    constexpr int kTurn = S::buffers == 4 ? 4 : 6;       // steps until buffers and registers are the same again
+    for (int64_t r = first; r < last;) {
+#pragma unroll
+      for (int k = 0; k < kTurn; ++k) {
+        step(buffer(k % S::buffers), buffer((k + 1) % S::buffers), buffer((k + 2) % S::buffers), k & 1 ? g1 : g0, r);
+        r += S::BK;
+        if (r >= last) break;
+      }
     }
   }
 
   // The tile's end, one block of 32 x 32 after the other; the blocks of a column of blocks wait in LDS, so that the code that ends
   // one is there once.
-  constexpr int kBlock = 4096, kHalf = S::WI * S::WJ / 2;
-  static_assert(kHalf * S::FI * kBlock <= O::bytes, "the blocks have to fit the operands' buffers");
+  constexpr int kBlock = 4096;
+  constexpr int kEach = O::bytes / (S::FI * kBlock);      // wavefronts that a buffer holds the blocks of
+  static_assert(kEach > 0 && (S::WI * S::WJ + kEach - 1) / kEach <= S::buffers, "the blocks have to fit the operands' buffers");
+  __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();
-  lds_char* const mine = (wave < kHalf ? b0 : b1) + (wave % kHalf) * (S::FI * kBlock) + lane * 16;
+  lds_char* const mine = buffer(wave / kEach) + (wave % kEach) * (S::FI * kBlock) + lane * 16;
 #pragma clang loop unroll(disable)
   for (int q = 0; q < S::FJ; ++q) {
 #pragma unroll
@@ -771,23 +849,32 @@ __global__ __launch_bounds__(WAVES * 64) void product_by_depth_kernel(ProductArg
   lds_char* const mine = all + wave * O::bytes;
   O o(a, i0, j0, last, lane);
   f32x16 acc[FI][FJ] = {};
+  typename O::Regs g;
   int64_t r = first + wave * BK;
-  if (r < last) o.request(mine, r);
+  if (r < last) {
+    o.fetch(mine, r);
+    o.request(g, r);
+  }
   while (r < last) {
-    o.deliver(mine);
+    o.deliver(g, mine);
     // what this wavefront asked for is there
     __builtin_amdgcn_s_waitcnt(0);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
     const int64_t next = r + WAVES * BK;
-    if (!DIRECT && next < last) o.request(mine, next);      // into registers: behind the products
-    O::multiply(acc, mine, 0, 0, lane);
+    if (next < last) o.request(g, next);
+#pragma unroll
+    for (int k = 0; k < BK; k += 16) {
+      typename O::template Fragments<FI, FJ> f;
+      f.read(mine, 0, 0, k, lane);
+      f.multiply(acc);
+    }
     // every fragment has been read before LDS is written again
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
     if (DIRECT && next < last) {
       __builtin_amdgcn_s_waitcnt(0xc07f);                   // lgkmcnt(0)
-      o.request(mine, next);
+      o.fetch(mine, next);
     }
     r = next;
   }
@@ -897,15 +984,15 @@ hipError_t by_size(const ProductArgs& a, hipStream_t s) {
   const int64_t middle = (int64_t)((a.ni + 127) / 128) * ((a.nj + 127) / 128);
   if constexpr (std::is_same_v<T, float>) {
     const int64_t big = (int64_t)((a.ni + 255) / 256) * ((a.nj + 127) / 128);
-    if (big >= 128) return run_product<T, PRODUCT, Shape<256, 128, 4, 2, 32>, DIRECT>(a, s);
-    if (middle >= 128) return run_product<T, PRODUCT, Shape<128, 128, 2, 2, 32>, DIRECT>(a, s);
+    if (big >= 128) return run_product<T, PRODUCT, std::conditional_t<PRODUCT == kWeightGrad, Shape<256, 128, 4, 2, 32, 3>, Shape<256, 128, 4, 2, 16, 4>>, DIRECT>(a, s);
+    if (middle >= 128) return run_product<T, PRODUCT, Shape<128, 128, 2, 2, 32, 3>, DIRECT>(a, s);
     if (a.nj <= 32) return run_by_depth<T, PRODUCT, 64, 32, 32, 8, DIRECT>(a, s);
     return run_by_depth<T, PRODUCT, 64, 64, 32, 6, DIRECT>(a, s);
   } else {
     const int64_t big = (int64_t)((a.ni + 255) / 256) * ((a.nj + 255) / 256);
     // operands that go through registers leave none for 256 x 256
-    if (big >= 128) return run_product<T, PRODUCT, std::conditional_t<DIRECT, Shape<256, 256, 2, 4, 64>, Shape<256, 128, 4, 2, 64>>, DIRECT>(a, s);
-    if (middle >= 128) return run_product<T, PRODUCT, Shape<128, 128, 2, 2, 64>, DIRECT>(a, s);
+    if (big >= 128) return run_product<T, PRODUCT, std::conditional_t<DIRECT, Shape<256, 256, 2, 4, 32, 4>, Shape<256, 128, 4, 2, 32, 4>>, DIRECT>(a, s);
+    if (middle >= 128) return run_product<T, PRODUCT, Shape<128, 128, 2, 2, 32, 4>, DIRECT>(a, s);
     if (a.nj <= 32) return run_by_depth<T, PRODUCT, 64, 32, 64, 8, DIRECT>(a, s);
     return run_by_depth<T, PRODUCT, 64, 64, 64, 8, DIRECT>(a, s);
   }
