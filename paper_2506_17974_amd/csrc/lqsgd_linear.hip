@@ -730,9 +730,8 @@ __global__ __launch_bounds__(S::threads, S::threads >= 512 ? 2 : 1) void product
   // an array each: what is on its way into one is not waited for where another is read
   __shared__ __attribute__((aligned(1024))) char lds0[O::bytes];
   __shared__ __attribute__((aligned(1024))) char lds1[O::bytes];
-  __shared__ __attribute__((aligned(1024))) char lds2[O::bytes];
-  __shared__ __attribute__((aligned(1024))) char lds3[S::buffers == 4 ? O::bytes : 1024];
-  static_assert(S::buffers == 3 || S::buffers == 4);
+  __shared__ __attribute__((aligned(1024))) char lds2[S::buffers > 2 ? O::bytes : 16];
+  __shared__ __attribute__((aligned(1024))) char lds3[S::buffers > 3 ? O::bytes : 16];
   auto buffer = [&](int k) { return k == 0 ? (lds_char*)lds0 : k == 1 ? (lds_char*)lds1 : k == 2 ? (lds_char*)lds2 : (lds_char*)lds3; };
 
   const Where at = where(sp.tiles_i, sp.tiles_j, sp.tiles_i * sp.tiles_j, sp.splits);
@@ -746,53 +745,56 @@ __global__ __launch_bounds__(S::threads, S::threads >= 512 ? 2 : 1) void product
   f32x16 acc[S::FI][S::FJ] = {};
 
   // A step's last products run from registers, behind the barrier that makes the next step's operands everyone's, beside the reads of
-  // those; its buffer is free from that barrier on and is filled for `buffers` steps ahead.  What goes through registers is asked for
-  // four steps ahead and put to LDS two steps ahead, with vector instructions (splitting, decoding) that one half of the wavefronts
-  // (a SIMD has one of each half) executes before its products and the other half behind them, beside the other's matrix instructions.
-  constexpr int kWaitFetched = 0x0070 | ((S::buffers - 2) * O::direct_loads & 15) | ((S::buffers - 2) * O::direct_loads >> 4) << 14;   // vmcnt, lgkmcnt(0)
+  // those; its buffer is free from that barrier on and is filled for `buffers` steps ahead.  What goes through registers is put to
+  // LDS a step ahead, with vector instructions (splitting, decoding) that one half of the wavefronts (a SIMD has one of each half)
+  // executes before its first products and the other half behind them, beside the other's matrix instructions; it has been asked for
+  // one step before (fp32, whose steps are long) or two.
+  constexpr int kFetched = (S::buffers - 2) * O::direct_loads, kWaitFetched = 0x0070 | (kFetched & 15) | (kFetched >> 4) << 14;      // vmcnt, lgkmcnt(0)
+  constexpr int kSets = std::is_same_v<T, float> ? 1 : 2;
   const bool early = wave < S::WI * S::WJ / 2;
   typename O::template Fragments<S::FI, S::FJ> now, next;
-  typename O::Regs g0, g1;
-  auto step = [&](lds_char* const here, lds_char* const there, lds_char* const ahead, typename O::Regs& g, int64_t r) {
+  typename O::Regs set[kSets];
+  auto request = [&](typename O::Regs& g, int64_t r) {
+    if (r < last) o.request(g, r);
+  };
+  auto step = [&](lds_char* const here, lds_char* const there, typename O::Regs& g, int64_t r) {
+    auto bring = [&]() {
+      if (!O::kRegisters || r + S::BK >= last) return;
+      o.deliver(g, there);
+      request(g, r + (1 + kSets) * S::BK);
+    };
+    if (early) bring();
 #pragma unroll
     for (int k = 16; k < S::BK; k += 16) {
       next.read(here, wi, wj, k, lane);
       now.multiply(acc);
       now = next;
     }
+    if (!early) bring();
     __builtin_amdgcn_s_waitcnt(kWaitFetched);
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     o.fetch(here, r + S::buffers * S::BK);
     next.read(there, wi, wj, 0, lane);
-    auto bring = [&]() {
-      if (!O::kRegisters) return;
-      o.deliver(g, ahead);
-      if (r + 4 * S::BK < last) o.request(g, r + 4 * S::BK);
-    };
-    if (early) bring();
     now.multiply(acc);
-    if (!early) bring();
     now = next;
   };
   if (first < last) {
-    o.request(g0, first);
-    if (first + S::BK < last) o.request(g1, first + S::BK);
+#pragma unroll
+    for (int k = 0; k < kSets; ++k) request(set[k], first + k * S::BK);
 #pragma unroll
     for (int k = 0; k < S::buffers; ++k) o.fetch(buffer(k), first + k * S::BK);
-    o.deliver(g0, buffer(0));
-    o.deliver(g1, buffer(1));
-    if (first + 2 * S::BK < last) o.request(g0, first + 2 * S::BK);
-    if (first + 3 * S::BK < last) o.request(g1, first + 3 * S::BK);
+    o.deliver(set[0], buffer(0));
+    request(set[0], first + kSets * S::BK);
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
     now.read(buffer(0), wi, wj, 0, lane);
-    constexpr int kTurn = S::buffers == 4 ? 4 : 6;       // steps until buffers and registers are the same again
+    static_assert(S::buffers % kSets == 0);
     for (int64_t r = first; r < last;) {
 #pragma unroll
-      for (int k = 0; k < kTurn; ++k) {
-        step(buffer(k % S::buffers), buffer((k + 1) % S::buffers), buffer((k + 2) % S::buffers), k & 1 ? g1 : g0, r);
+      for (int k = 0; k < S::buffers; ++k) {
+        step(buffer(k), buffer((k + 1) % S::buffers), set[(k + 1) % kSets], r);
         r += S::BK;
         if (r >= last) break;
       }
@@ -984,8 +986,8 @@ hipError_t by_size(const ProductArgs& a, hipStream_t s) {
   const int64_t middle = (int64_t)((a.ni + 127) / 128) * ((a.nj + 127) / 128);
   if constexpr (std::is_same_v<T, float>) {
     const int64_t big = (int64_t)((a.ni + 255) / 256) * ((a.nj + 127) / 128);
-    if (big >= 128) return run_product<T, PRODUCT, std::conditional_t<PRODUCT == kWeightGrad, Shape<256, 128, 4, 2, 32, 3>, Shape<256, 128, 4, 2, 16, 4>>, DIRECT>(a, s);
-    if (middle >= 128) return run_product<T, PRODUCT, Shape<128, 128, 2, 2, 32, 3>, DIRECT>(a, s);
+    if (big >= 128) return run_product<T, PRODUCT, Shape<256, 128, 4, 2, 32, 2>, DIRECT>(a, s);
+    if (middle >= 128) return run_product<T, PRODUCT, Shape<128, 128, 2, 2, 32, 2>, DIRECT>(a, s);
     if (a.nj <= 32) return run_by_depth<T, PRODUCT, 64, 32, 32, 8, DIRECT>(a, s);
     return run_by_depth<T, PRODUCT, 64, 64, 32, 6, DIRECT>(a, s);
   } else {
