@@ -472,6 +472,7 @@ struct Operand {
     std::conditional_t<DIRECT || ORDER == kHeld, Empty, Raw[per_thread]> raw;
     std::conditional_t<ORDER == kHeld, Chunk16[per_thread], Empty> codes;
     std::conditional_t<ORDER == kHeld, uint32_t[per_thread], Empty> exps;
+    std::conditional_t<ORDER == kHeld, bool[per_thread], Empty> there;
   };
 
   // Straight into LDS, 16 bytes a lane: memory rows start at multiples of 16 bytes and are whole chunks.  Lanes that have nothing
@@ -515,14 +516,14 @@ struct Operand {
     if constexpr (ORDER == kHeld) {
 #pragma unroll
       for (int k = 0; k < per_thread; ++k) {
+        // loaded in any case, as product_kernel counts loads; codes go on to the end of their group of 32
         const int piece = k * THREADS + t, r = piece / (N / 16), i = piece % (N / 16) * 16;
-        g.codes[k] = Chunk16{};
-        g.exps[k] = 0;
-        if (mine(piece) && r < left && i < n) {         // codes go on to the end of their group of 32
-          const int64_t row = r0 + r;
-          g.codes[k] = *reinterpret_cast<const Chunk16*>(held.codes + row * ((int64_t)groups * kGroup) + i);
-          g.exps[k] = held.exponents[row * groups + i / kGroup];
-        }
+        const int whole = (n + kGroup - 1) / kGroup * kGroup;
+        const int64_t row = min(r0 + r, depth - 1);
+        const int col = min(i, whole - 16);
+        g.codes[k] = *reinterpret_cast<const Chunk16*>(held.codes + row * ((int64_t)groups * kGroup) + col);
+        g.exps[k] = held.exponents[row * groups + col / kGroup];
+        g.there[k] = r0 + r < depth && i < n;            // else zeros: decided when they have come
       }
     } else {
       const T* from = base + (ORDER == kDepthRuns ? r0 : r0 * ld);
@@ -568,7 +569,7 @@ struct Operand {
       for (int k = 0; k < per_thread; ++k) {
         const int piece = k * THREADS + t, r = piece / (N / 16), i = piece % (N / 16) * 16;
         if (!mine(piece)) break;
-        const float f = factor_of(g.exps[k]);
+        const float f = g.there[k] ? factor_of(g.exps[k]) : 0.f;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           E e[8];
@@ -651,6 +652,7 @@ struct Operands {
   }
   static constexpr bool kRegisters = !kDirectA || !DIRECT;     // something goes through registers
   static constexpr int direct_loads = (kDirectA ? A::per_thread : 0) + (DIRECT ? B::per_thread : 0);
+  static constexpr int held_loads = kOrderA == kHeld ? 2 * A::per_thread : 0;
   struct Regs {
     typename A::Regs a;
     typename B::Regs b;
@@ -749,13 +751,17 @@ __global__ __launch_bounds__(S::threads, S::threads >= 512 ? 2 : 1) void product
   // LDS a step ahead, with vector instructions (splitting, decoding) that one half of the wavefronts (a SIMD has one of each half)
   // executes before its first products and the other half behind them, beside the other's matrix instructions; it has been asked for
   // one step before (fp32, whose steps are long) or two.
-  constexpr int kFetched = (S::buffers - 2) * O::direct_loads, kWaitFetched = 0x0070 | (kFetched & 15) | (kFetched >> 4) << 14;      // vmcnt, lgkmcnt(0)
+  // What may still be on its way at the barrier: the fetches of the steps behind the next, and the codes asked for since the next
+  // step's fetches were.
+  constexpr int kOnTheWay = DIRECT ? (S::buffers - 2) * O::direct_loads + (S::buffers - 1) * O::held_loads : 63;
+  static_assert(kOnTheWay < 64);
+  constexpr int kWait = 0x0070 | (kOnTheWay & 15) | (kOnTheWay >> 4) << 14;            // vmcnt(kOnTheWay), lgkmcnt(0)
   constexpr int kSets = std::is_same_v<T, float> ? 1 : 2;
   const bool early = wave < S::WI * S::WJ / 2;
   typename O::template Fragments<S::FI, S::FJ> now, next;
   typename O::Regs set[kSets];
   auto request = [&](typename O::Regs& g, int64_t r) {
-    if (r < last) o.request(g, r);
+    if (DIRECT || r < last) o.request(g, r);
   };
   auto step = [&](lds_char* const here, lds_char* const there, typename O::Regs& g, int64_t r) {
     auto bring = [&]() {
@@ -771,7 +777,8 @@ __global__ __launch_bounds__(S::threads, S::threads >= 512 ? 2 : 1) void product
       now = next;
     }
     if (!early) bring();
-    __builtin_amdgcn_s_waitcnt(kWaitFetched);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(kWait);
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
