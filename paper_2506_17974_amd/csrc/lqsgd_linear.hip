@@ -37,6 +37,18 @@ __device__ inline float largest(const float (&v)[N]) {
   for (int k = 0; k < N; ++k) m = __builtin_elementwise_maximum(m, fabsf(v[k]));
   return m;
 }
+// The largest of the 32 / N neighbouring lanes that share a group: lanes exchanged within fours and, for N = 4, within eights.
+template <int N>
+__device__ inline float group_largest(float m) {
+  static_assert(N == 8 || N == 4);
+  auto of = [](float v, auto control) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), decltype(control)::value, 0xf, 0xf, true));
+  };
+  m = __builtin_elementwise_maximum(m, of(m, std::integral_constant<int, 0xb1>{}));        // lane ^ 1
+  m = __builtin_elementwise_maximum(m, of(m, std::integral_constant<int, 0x4e>{}));        // lane ^ 2
+  if (N == 4) m = __builtin_elementwise_maximum(m, of(m, std::integral_constant<int, 0x141>{}));   // 7 - lane
+  return m;
+}
 // e of a group from its largest magnitude.  absmax = m 2^E, 1 <= m < 2, takes e = E - 6, or E - 5 from 127.5 2^(E-6) on: adding 2^-7
 // of the mantissa carries into the exponent there.
 template <typename T>
@@ -170,11 +182,8 @@ __global__ __launch_bounds__(256) void checkpoint_save_kernel(const T* x, int64_
   const bool there = row < samples;
   float v[kPiece];
   load_values(v, x + row * ldx + piece * kPiece, there ? features - (int)(piece * kPiece) : 0);
-  float m = largest(v);
-  m = __builtin_elementwise_maximum(m, __shfl_xor(m, 1));
-  m = __builtin_elementwise_maximum(m, __shfl_xor(m, 2));
   uint32_t w[2], byte;
-  pack_codes<T>(w, v, m, &byte);
+  pack_codes<T>(w, v, group_largest<kPiece>(largest(v)), &byte);
   if (!there) return;
   *reinterpret_cast<uint2*>(c.codes + row * ((int64_t)pieces * kPiece) + piece * kPiece) = make_uint2(w[0], w[1]);
   if ((piece & 3u) == 0) c.exponents[row * (pieces >> 2) + (piece >> 2)] = (uint8_t)byte;
@@ -269,10 +278,18 @@ __global__ __launch_bounds__(256) void sum_runs_kernel(const float* part, float*
 // ---------------------------------------------------------------------------
 // products
 // ---------------------------------------------------------------------------
-// The end of a product: v holds D[j][i0 .. i0 + N - 1], i0 a multiple of N, and the lanes `near`, 2 near, .. away the rest of the
-// group of 32.  All lanes of the wavefront come here together; `there` is false for those that have no row j.
+// The end of a product: v holds D[j][i0 .. i0 + N - 1], i0 a multiple of N, and neighbouring lanes the rest of the group of 32.  All
+// lanes of the wavefront come here together; `there` is false for those that have no row j.  N: 16 bytes of what is written.
+template <typename T, int PRODUCT> constexpr int kRun = std::is_same_v<T, float> || PRODUCT == kWeightGrad ? 4 : 8;
+
 template <typename T, int PRODUCT, int N>
-__device__ inline void finish(float (&v)[N], const ProductArgs& a, int64_t j, int i0, bool there, int near) {
+__device__ inline void load_bias(float (&b)[N], const ProductArgs& a, int i0) {
+  if (PRODUCT != kForward) return;
+  load_values(b, static_cast<const T*>(a.bias) + i0, a.bias ? a.ni - i0 : 0);
+}
+
+template <typename T, int PRODUCT, int N>
+__device__ inline void finish(float (&v)[N], const float (&bias)[N], const ProductArgs& a, int64_t j, int i0, bool there) {
   const int n = there ? a.ni - i0 : 0;
   if (PRODUCT == kWeightGrad) {
     if (n <= 0) return;
@@ -305,22 +322,15 @@ __device__ inline void finish(float (&v)[N], const ProductArgs& a, int64_t j, in
   const int groups = (a.ni + kGroup - 1) / kGroup;
   const bool in_codes = there && i0 < groups * kGroup;
   const int64_t code_at = j * ((int64_t)groups * kGroup) + i0, exp_at = j * groups + i0 / kGroup;
-  if (a.bias) {
-    float b[N];
-    load_values(b, static_cast<const T*>(a.bias) + i0, n);
 #pragma unroll
-    for (int k = 0; k < N; ++k) v[k] += b[k];
-  }
+  for (int k = 0; k < N; ++k) v[k] += bias[k];
   auto keep = [&](const Codes& c) {
     if (n < N) {
 #pragma unroll
       for (int k = 0; k < N; ++k) v[k] = k < n ? v[k] : 0.f;
     }
-    float m = largest(v);
-#pragma unroll
-    for (int d = 0; N << d < kGroup; ++d) m = __builtin_elementwise_maximum(m, __shfl_xor(m, near << d));
     uint32_t w[N / 4], byte;
-    pack_codes<T>(w, v, m, &byte);
+    pack_codes<T>(w, v, group_largest<N>(largest(v)), &byte);
     if (in_codes) {
       __builtin_memcpy(__builtin_assume_aligned(c.codes + code_at, N), w, N);
       if (i0 % kGroup == 0) c.exponents[exp_at] = (uint8_t)byte;
@@ -701,29 +711,58 @@ struct Operands {
   };
 };
 
-// A block of D as the matrix instructions leave it, put to LDS as 4 pieces of 16 bytes a lane, 1 KiB apart: lanes l and l + 32 hold
-// runs of 4 of the same column; swapped, each has 16 consecutive i: lane l the first 16 of column l, lane l + 32 the others.
-__device__ inline void put_block(lds_char* to, const f32x16& block) {
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    uint32_t low[4], high[4];
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      const float x = block[4 * h + c], y = block[8 + 4 * h + c];
-      auto s = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, y), false, false);
-      low[c] = (uint32_t)s[0];
-      high[c] = (uint32_t)s[1];
-    }
-    s16x8 v;
-    __builtin_memcpy(&v, low, 16);
-    *reinterpret_cast<lds_s16x8*>(to + 2 * h * 1024) = v;
-    __builtin_memcpy(&v, high, 16);
-    *reinterpret_cast<lds_s16x8*>(to + (2 * h + 1) * 1024) = v;
+// How a tile's sums leave the matrix instructions' layout: a wavefront's blocks of FI x FJ go to LDS strip by strip, 32 rows j of
+// 32 FI values, and come back with the lanes along the rows, N values of i each, so that each instruction that stores them writes
+// whole runs of memory (16 bytes a lane scattered over 64 rows took four times as long).  Pieces of 64 lanes are numbered through the tile.
+// Chunks of 4 values change places within a row as a tile's do, for writes of one chunk of 32 rows and reads along rows.
+template <int FI, int FJ, int WI, int WJ, int N>
+struct Strips {
+  static constexpr int lanes = FI * 32 / N, rows = 64 / lanes, turns = 32 / rows, chunks = FI * 8, bytes = 32 * chunks * 16;
+  static constexpr int per_wave = FJ * turns, pieces = WI * WJ * per_wave;
+  __device__ static inline int column(int piece, int lane) { return piece / per_wave % WI * (FI * 32) + lane % lanes * N; }
+  __device__ static inline int row(int piece, int lane) {
+    return (piece / per_wave / WI * FJ + piece / turns % FJ) * 32 + piece % turns * rows + lane / lanes;
   }
+  __device__ static inline int place(int row, int chunk) { return (row * chunks + (chunk ^ (row & (chunks - 1)))) * 16; }
+  __device__ static inline void put(lds_char* strip, int k, const f32x16& block, int lane) {
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      float x[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) x[c] = block[4 * g + c];
+      s16x8 v;
+      __builtin_memcpy(&v, x, 16);
+      *reinterpret_cast<lds_s16x8*>(strip + place(lane & 31, 8 * k + 2 * g + (lane >> 5))) = v;
+    }
+  }
+  // What piece `turn` of a strip has for a lane.
+  __device__ static inline void get(float (&v)[N], const lds_char* strip, int turn, int lane) {
+    const int row = turn * rows + lane / lanes, u = lane % lanes;
+    if constexpr (N == 4) {
+      const s16x8 x = *reinterpret_cast<const lds_s16x8*>(strip + place(row, u));
+      __builtin_memcpy(v, &x, 16);
+    } else {
+      const int second = (u >> 2 ^ u >> 3) & 1;           // which of the two is read first
+      const s16x8 x = *reinterpret_cast<const lds_s16x8*>(strip + place(row, 2 * u + second));
+      const s16x8 y = *reinterpret_cast<const lds_s16x8*>(strip + place(row, 2 * u + 1 - second));
+      float p[4], q[4];
+      __builtin_memcpy(p, &x, 16);
+      __builtin_memcpy(q, &y, 16);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) v[c] = second ? q[c] : p[c], v[4 + c] = second ? p[c] : q[c];
+    }
+  }
+};
+
+// Where the sums of a piece of a split wait for the join: lanes side by side.
+template <int N>
+__device__ inline float* waiting(const ProductArgs& a, int64_t split, int64_t tile, int64_t tiles, int piece, int pieces, int lane) {
+  return static_cast<float*>(a.workspace) + ((split * tiles + tile) * pieces + piece) * (64 * N) + lane * 4;
 }
-__device__ inline void get_piece(float* v, const lds_char* from) {
-  const s16x8 x = *reinterpret_cast<const lds_s16x8*>(from);
-  __builtin_memcpy(v, &x, 16);
+template <int N>
+__device__ inline void put_waiting(float* to, const float (&v)[N]) {
+#pragma unroll
+  for (int c = 0; c < N / 4; ++c) *reinterpret_cast<float4*>(to + c * 256) = make_float4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
 }
 
 template <typename T, int PRODUCT, typename S, bool DIRECT>
@@ -808,34 +847,35 @@ __global__ __launch_bounds__(S::threads, S::threads >= 512 ? 2 : 1) void product
     }
   }
 
-  // The tile's end, one block of 32 x 32 after the other; the blocks of a column of blocks wait in LDS, so that the code that ends
-  // one is there once.
-  constexpr int kBlock = 4096;
-  constexpr int kEach = O::bytes / (S::FI * kBlock);      // wavefronts that a buffer holds the blocks of
-  static_assert(kEach > 0 && (S::WI * S::WJ + kEach - 1) / kEach <= S::buffers, "the blocks have to fit the operands' buffers");
+  // The tile's end, one strip of blocks after the other, by code that is there once.
+  using P = Strips<S::FI, S::FJ, S::WI, S::WJ, kRun<T, PRODUCT>>;
+  constexpr int N = kRun<T, PRODUCT>;
+  constexpr int kEach = O::bytes / P::bytes;              // wavefronts that a buffer holds the strips of
+  static_assert(kEach > 0 && (S::WI * S::WJ + kEach - 1) / kEach <= S::buffers, "the strips have to fit the operands' buffers");
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();
-  lds_char* const mine = buffer(wave / kEach) + (wave % kEach) * (S::FI * kBlock) + lane * 16;
+  lds_char* const strip = buffer(wave / kEach) + (wave % kEach) * P::bytes;
+  const int i = i0 + P::column(wave * P::per_wave, lane);
+  float bias[N];
+  load_bias<T, PRODUCT>(bias, a, i);
 #pragma clang loop unroll(disable)
   for (int q = 0; q < S::FJ; ++q) {
 #pragma unroll
     for (int qq = 0; qq < S::FJ; ++qq) {
       if (qq != q) continue;
 #pragma unroll
-      for (int k = 0; k < S::FI; ++k) put_block(mine + k * kBlock, acc[k][qq]);
+      for (int k = 0; k < S::FI; ++k) P::put(strip, k, acc[k][qq], lane);
     }
-    const int jj = wj + 32 * q + (lane & 31);
 #pragma clang loop unroll(disable)
-    for (int k = 0; k < S::FI; ++k) {
-      float v[16];
-#pragma unroll
-      for (int c = 0; c < 4; ++c) get_piece(v + 4 * c, mine + k * kBlock + c * 1024);
-      const int ii = wi + 32 * k + (lane >> 5) * 16;
+    for (int turn = 0; turn < P::turns; ++turn) {
+      const int piece = wave * P::per_wave + q * P::turns + turn;
+      float v[N];
+      P::get(v, strip, turn, lane);
+      const int64_t j = j0 + P::row(piece, lane);
       if (sp.splits > 1) {
-        float* to = static_cast<float*>(a.workspace) + (((int64_t)at.split * sp.tiles_j + at.tj) * sp.tiles_i + at.ti) * (S::BI * S::BJ) + jj * S::BI + ii;
-        store_values(to, v, 16);
+        put_waiting<N>(waiting<N>(a, at.split, (int64_t)at.tj * sp.tiles_i + at.ti, (int64_t)sp.tiles_i * sp.tiles_j, piece, P::pieces, lane), v);
       } else {
-        finish<T, PRODUCT>(v, a, j0 + jj, i0 + ii, j0 + jj < a.nj, 32);
+        finish<T, PRODUCT>(v, bias, a, j, i, j < a.nj);
       }
     }
   }
@@ -846,8 +886,9 @@ __global__ __launch_bounds__(S::threads, S::threads >= 512 ? 2 : 1) void product
 template <typename T, int PRODUCT, int BI, int BJ, int BK, int WAVES, bool DIRECT>
 __global__ __launch_bounds__(WAVES * 64) void product_by_depth_kernel(ProductArgs a, Split sp) {
   using O = Operands<T, PRODUCT, BI, BJ, BK, 64, DIRECT>;
-  constexpr int FI = BI / 32, FJ = BJ / 32, kBlock = 4096;
-  static_assert(FI * FJ * kBlock <= O::bytes, "a wavefront's sums have to fit its operands' place");
+  constexpr int FI = BI / 32, FJ = BJ / 32, N = kRun<T, PRODUCT>;
+  using P = Strips<FI, FJ, 1, 1, N>;
+  static_assert(FJ * P::bytes <= O::bytes, "a wavefront's sums have to fit its operands' place");
   __shared__ __attribute__((aligned(1024))) char lds[WAVES * O::bytes];
   const Where at = where(sp.tiles_i, sp.tiles_j, sp.tiles_i * sp.tiles_j, sp.splits);
   const int i0 = at.ti * BI;
@@ -888,51 +929,51 @@ __global__ __launch_bounds__(WAVES * 64) void product_by_depth_kernel(ProductArg
     r = next;
   }
 #pragma unroll
-  for (int k = 0; k < FI; ++k)
+  for (int q = 0; q < FJ; ++q)
 #pragma unroll
-    for (int q = 0; q < FJ; ++q) put_block(mine + (k * FJ + q) * kBlock + lane * 16, acc[k][q]);
+    for (int k = 0; k < FI; ++k) P::put(mine + q * P::bytes, k, acc[k][q], lane);
   __syncthreads();
-  // wavefront `block` ends that block: pieces of 16 i x 32 columns x 2
-  for (int block = wave; block < FI * FJ; block += WAVES) {
-    float v[16] = {};
+  for (int piece = wave; piece < P::pieces; piece += WAVES) {
+    float v[N] = {}, bias[N];
+    const int i = i0 + P::column(piece, lane);
+    const int64_t j = j0 + P::row(piece, lane);
+    load_bias<T, PRODUCT>(bias, a, i);
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w)
+    for (int w = 0; w < WAVES; ++w) {
+      float x[N];
+      P::get(x, all + w * O::bytes + piece / P::turns * P::bytes, piece % P::turns, lane);
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        float x[4];
-        get_piece(x, all + w * O::bytes + block * kBlock + c * 1024 + lane * 16);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[4 * c + e] += x[e];
-      }
-    const int ii = block / FJ * 32 + (lane >> 5) * 16, jj = block % FJ * 32 + (lane & 31);
+      for (int e = 0; e < N; ++e) v[e] += x[e];
+    }
     if (sp.splits > 1) {
-      float* to = static_cast<float*>(a.workspace) + (((int64_t)at.split * sp.tiles_j + at.tj) * sp.tiles_i + at.ti) * (BI * BJ) + jj * BI + ii;
-      store_values(to, v, 16);
+      put_waiting<N>(waiting<N>(a, at.split, (int64_t)at.tj * sp.tiles_i + at.ti, (int64_t)sp.tiles_i * sp.tiles_j, piece, P::pieces, lane), v);
     } else {
-      finish<T, PRODUCT>(v, a, j0 + jj, i0 + ii, j0 + jj < a.nj, 32);
+      finish<T, PRODUCT>(v, bias, a, j, i, j < a.nj);
     }
   }
 }
 
-// Adds up the splits of a product in their order and ends it.  A thread takes 4 i of one j, 8 neighbours a group of 32.
-template <typename T, int PRODUCT>
-__global__ __launch_bounds__(256) void join_kernel(ProductArgs a, Split sp, int bi, int bj) {
-  const int row = bi / 4;                               // threads to a row of a tile
-  const int64_t piece = (int64_t)blockIdx.x * 256 + threadIdx.x, per_tile = (int64_t)row * bj, tile = piece / per_tile;
-  const int in = (int)(piece - tile * per_tile), jj = in / row, ii = in % row * 4;
-  const int64_t j = tile / sp.tiles_i * bj + jj;
-  const int i = (int)(tile % sp.tiles_i) * bi + ii;
-  const int64_t all = (int64_t)sp.tiles_i * sp.tiles_j * bi * bj;
-  float v[4] = {};
-  if (j < a.nj && i < a.ni) {
-    const float* from = static_cast<const float*>(a.workspace) + tile * (bi * bj) + jj * bi + ii;
-#pragma unroll 8
-    for (int s = 0; s < sp.splits; ++s) {
-      const float4 w = *reinterpret_cast<const float4*>(from + s * all);
-      v[0] += w.x, v[1] += w.y, v[2] += w.z, v[3] += w.w;
+// Adds up the splits of a product in their order and ends it, a piece of a tile to a wavefront.
+template <typename T, int PRODUCT, typename P, int BI, int BJ>
+__global__ __launch_bounds__(256) void join_kernel(ProductArgs a, Split sp) {
+  constexpr int N = kRun<T, PRODUCT>;
+  const int lane = threadIdx.x & 63;
+  const int64_t all = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), tile = all / P::pieces, tiles = (int64_t)sp.tiles_i * sp.tiles_j;
+  const int piece = (int)(all - tile * P::pieces);
+  const int i = (int)(tile % sp.tiles_i) * BI + P::column(piece, lane);
+  const int64_t j = tile / sp.tiles_i * BJ + P::row(piece, lane);
+  float v[N] = {}, bias[N];
+  load_bias<T, PRODUCT>(bias, a, i);
+#pragma unroll 4
+  for (int s = 0; s < sp.splits; ++s) {
+    const float* from = waiting<N>(a, s, tile, tiles, piece, P::pieces, lane);
+#pragma unroll
+    for (int c = 0; c < N / 4; ++c) {
+      const float4 w = *reinterpret_cast<const float4*>(from + c * 256);
+      v[4 * c] += w.x, v[4 * c + 1] += w.y, v[4 * c + 2] += w.z, v[4 * c + 3] += w.w;
     }
   }
-  finish<T, PRODUCT>(v, a, j, i, j < a.nj, 1);
+  finish<T, PRODUCT>(v, bias, a, j, i, j < a.nj);
 }
 
 #ifndef LQ_RULE
@@ -956,11 +997,12 @@ Plan plan(const ProductArgs& a, int bi, int bj, int step, int64_t splits) {
   return p;
 }
 
-template <typename T, int PRODUCT>
-hipError_t join(const ProductArgs& a, const Plan& p, int bi, int bj, hipStream_t s) {
+template <typename T, int PRODUCT, typename P, int BI, int BJ>
+hipError_t join(const ProductArgs& a, const Plan& p, hipStream_t s) {
+  static_assert(P::pieces % 4 == 0);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.sp.splits == 1) return e;
-  join_kernel<T, PRODUCT><<<dim3((unsigned)(p.tiles * bi * bj / 4 / 256)), 256, 0, s>>>(a, p.sp, bi, bj);
+  join_kernel<T, PRODUCT, P, BI, BJ><<<dim3((unsigned)(p.tiles * P::pieces / 4)), 256, 0, s>>>(a, p.sp);
   return hipGetLastError();
 }
 
@@ -971,7 +1013,7 @@ hipError_t run_product(const ProductArgs& a, hipStream_t s) {
   const Plan p = plan(a, S::BI, S::BJ, S::BK, std::min<int64_t>((a.depth / S::BK) / 4, 256 / tiles));
   if (p.tiles > INT32_MAX) return hipErrorInvalidValue;
   product_kernel<T, PRODUCT, S, DIRECT><<<dim3((unsigned)(p.tiles * p.sp.splits)), S::threads, 0, s>>>(a, p.sp);
-  return join<T, PRODUCT>(a, p, S::BI, S::BJ, s);
+  return join<T, PRODUCT, Strips<S::FI, S::FJ, S::WI, S::WJ, kRun<T, PRODUCT>>, S::BI, S::BJ>(a, p, s);
 }
 
 template <typename T, int PRODUCT, int BI, int BJ, int BK, int WAVES, bool DIRECT>
@@ -981,7 +1023,7 @@ hipError_t run_by_depth(const ProductArgs& a, hipStream_t s) {
   const Plan p = plan(a, BI, BJ, WAVES * BK, LQ_RULE);
   if (p.tiles > INT32_MAX) return hipErrorInvalidValue;
   product_by_depth_kernel<T, PRODUCT, BI, BJ, BK, WAVES, DIRECT><<<dim3((unsigned)(p.tiles * p.sp.splits)), WAVES * 64, 0, s>>>(a, p.sp);
-  return join<T, PRODUCT>(a, p, BI, BJ, s);
+  return join<T, PRODUCT, Strips<BI / 32, BJ / 32, 1, 1, kRun<T, PRODUCT>>, BI, BJ>(a, p, s);
 }
 
 bool whole_chunks(const void* p, int64_t ld, int64_t length) {
