@@ -976,25 +976,57 @@ __global__ __launch_bounds__(256) void join_kernel(ProductArgs a, Split sp) {
   finish<T, PRODUCT>(v, bias, a, j, i, j < a.nj);
 }
 
-#ifndef LQ_RULE
-#define LQ_RULE (tiles < 128 && rounds >= 4 ? std::min<int64_t>(rounds / 2, 256 / tiles) : 1)
-#endif
-// Tiles of bi x bj, and the sum of `depth` in `splits` parts of whole steps.
+// ---- which kernel a product takes ----
+// Three kernels serve a product: by depth (64 x 64 tiles, the sum shared out among a workgroup's wavefronts), 128 x 128 tiles and
+// the largest ones, each with the sum whole or in parts that a join adds up.  The one with the least expected time is taken:
+//   1.5 us + turns (turn + steps (step + more w)) + [parts > 1] (4 us + what the join reads and writes at 4.5 TB/s)
+// for `turns` rounds of 256 workgroups of `steps` steps each and w = the share of the CUs that have one.  The figures are fits to
+// the three kernels' times over 60 products from 64 x 64 x 1024 to 8192 x 2048 x 1024 in bfloat16 and fp32; taken by them the
+// products cost 2 % more than each one's best.  E.g. (bf16, ni x nj x depth: by depth / 128 x 128 / 256 x 256) 1024 x 1024 x 1024
+// 8 / 17 / 30 us, 2048 x 2048 x 2048 40 / 30 / 51, 4096 x 4096 x 512 74 / 29 / 24; fp32 512 x 4096 x 4096 154 / 239 / 283, in 4 parts
+// by the last 99.
+struct Rate { float turn, step, more; };
+enum Kernel { kByDepth = 0, kMiddle = 1, kLarge = 2 };
 struct Plan {
+  Kernel kernel;
   Split sp;
   int64_t tiles;
 };
-Plan plan(const ProductArgs& a, int bi, int bj, int step, int64_t splits) {
-  Plan p;
-  p.sp.tiles_i = (a.ni + bi - 1) / bi;
-  p.tiles = (a.nj + bj - 1) / bj * p.sp.tiles_i;
-  p.sp.tiles_j = (int)((a.nj + bj - 1) / bj);
-  const int64_t steps = (a.depth + step - 1) / step, fit = (int64_t)(kWorkspaceBytes / (sizeof(float) * bi * bj)) / p.tiles;
-  splits = std::max<int64_t>(1, std::min({splits, steps, fit}));
-  const int64_t per = std::max<int64_t>(1, (steps + splits - 1) / splits);
-  p.sp.splits = (int)std::max<int64_t>(1, (steps + per - 1) / per);
-  p.sp.steps = per * step;
-  return p;
+struct Geometry { int bi, bj, step; };
+
+template <typename T, int PRODUCT, bool DIRECT>
+Plan plan(const ProductArgs& a) {
+  constexpr bool kWide = std::is_same_v<T, float>, kGrad = PRODUCT == kWeightGrad;
+  constexpr Rate rates[3] = {kWide ? kGrad ? Rate{2.6f, 1.9f, .2f} : Rate{3.2f, 2.7f, .3f}
+                             : DIRECT ? kGrad ? Rate{3.6f, 1.5f, .35f} : Rate{3.4f, 1.f, .45f} : Rate{3.6f, 2.2f, .6f},
+                             kWide ? kGrad ? Rate{6.f, 1.35f, .05f} : Rate{8.f, 1.85f, .05f}
+                             : DIRECT ? kGrad ? Rate{4.f, .58f, .12f} : Rate{2.8f, .34f, 0.f} : Rate{5.f, .9f, .1f},
+                             kWide ? kGrad ? Rate{6.5f, 1.36f, .1f} : Rate{8.f, 2.f, .5f}
+                             : DIRECT ? kGrad ? Rate{9.f, .78f, .22f} : Rate{9.f, .62f, .25f} : Rate{8.f, .8f, .1f}};
+  const Geometry shapes[3] = {{64, a.nj <= 32 ? 32 : 64, kWide ? a.nj <= 32 ? 256 : 192 : 512}, {128, 128, 32}, {256, !kWide && DIRECT ? 256 : 128, 32}};
+  Plan best{};
+  float least = 0.f;
+  for (int k = 0; k < 3; ++k) {
+    const Geometry& g = shapes[k];
+    const int64_t ti = (a.ni + g.bi - 1) / g.bi, tj = (a.nj + g.bj - 1) / g.bj, tiles = ti * tj, steps = (a.depth + g.step - 1) / g.step;
+    const int64_t fit = (int64_t)(kWorkspaceBytes / (sizeof(float) * g.bi * g.bj)) / tiles;
+    for (int64_t parts = 1; parts <= 16; ++parts) {
+      if (parts > 1 && (parts > steps || parts > fit)) break;
+      const int64_t per = parts > 1 ? (steps + parts - 1) / parts : steps;
+      if (parts > 1 && (steps + per - 1) / per != parts) continue;         // as many steps a part as with fewer parts
+      const int64_t groups = tiles * parts, turns = (groups + 255) / 256;
+      const Rate& r = rates[k];
+      float us = 1.5f + (float)turns * (r.turn + (float)per * (r.step + r.more * std::min(1.f, (float)groups / 256.f)));
+      if (parts > 1) us += 4.f + 4e-6f / 4.5f * (float)(groups * g.bi * g.bj);
+      if (k + parts == 1 || us < least) {
+        least = us;
+        best.kernel = (Kernel)k;
+        best.sp = Split{(int)ti, (int)std::min<int64_t>(tj, INT32_MAX), (int)parts, std::max<int64_t>(1, per) * g.step};
+        best.tiles = tiles;
+      }
+    }
+  }
+  return best;
 }
 
 template <typename T, int PRODUCT, typename P, int BI, int BJ>
@@ -1007,21 +1039,13 @@ hipError_t join(const ProductArgs& a, const Plan& p, hipStream_t s) {
 }
 
 template <typename T, int PRODUCT, typename S, bool DIRECT>
-hipError_t run_product(const ProductArgs& a, hipStream_t s) {
-  // Few tiles: the sum is split so that the CUs have work, each part at least 4 steps.
-  const int64_t tiles = (int64_t)((a.ni + S::BI - 1) / S::BI) * ((a.nj + S::BJ - 1) / S::BJ);
-  const Plan p = plan(a, S::BI, S::BJ, S::BK, std::min<int64_t>((a.depth / S::BK) / 4, 256 / tiles));
-  if (p.tiles > INT32_MAX) return hipErrorInvalidValue;
+hipError_t run_product(const ProductArgs& a, const Plan& p, hipStream_t s) {
   product_kernel<T, PRODUCT, S, DIRECT><<<dim3((unsigned)(p.tiles * p.sp.splits)), S::threads, 0, s>>>(a, p.sp);
   return join<T, PRODUCT, Strips<S::FI, S::FJ, S::WI, S::WJ, kRun<T, PRODUCT>>, S::BI, S::BJ>(a, p, s);
 }
 
 template <typename T, int PRODUCT, int BI, int BJ, int BK, int WAVES, bool DIRECT>
-hipError_t run_by_depth(const ProductArgs& a, hipStream_t s) {
-  const int64_t tiles = (int64_t)((a.ni + BI - 1) / BI) * ((a.nj + BJ - 1) / BJ);
-  const int64_t rounds = (a.depth + WAVES * BK - 1) / (WAVES * BK);
-  const Plan p = plan(a, BI, BJ, WAVES * BK, LQ_RULE);
-  if (p.tiles > INT32_MAX) return hipErrorInvalidValue;
+hipError_t run_by_depth(const ProductArgs& a, const Plan& p, hipStream_t s) {
   product_by_depth_kernel<T, PRODUCT, BI, BJ, BK, WAVES, DIRECT><<<dim3((unsigned)(p.tiles * p.sp.splits)), WAVES * 64, 0, s>>>(a, p.sp);
   return join<T, PRODUCT, Strips<BI / 32, BJ / 32, 1, 1, kRun<T, PRODUCT>>, BI, BJ>(a, p, s);
 }
@@ -1032,20 +1056,19 @@ bool whole_chunks(const void* p, int64_t ld, int64_t length) {
 
 template <typename T, int PRODUCT, bool DIRECT>
 hipError_t by_size(const ProductArgs& a, hipStream_t s) {
-  const int64_t middle = (int64_t)((a.ni + 127) / 128) * ((a.nj + 127) / 128);
+  const Plan p = plan<T, PRODUCT, DIRECT>(a);
+  if (p.tiles > INT32_MAX) return hipErrorInvalidValue;
   if constexpr (std::is_same_v<T, float>) {
-    const int64_t big = (int64_t)((a.ni + 255) / 256) * ((a.nj + 127) / 128);
-    if (big >= 128) return run_product<T, PRODUCT, Shape<256, 128, 4, 2, 32, 2>, DIRECT>(a, s);
-    if (middle >= 128) return run_product<T, PRODUCT, Shape<128, 128, 2, 2, 32, 2>, DIRECT>(a, s);
-    if (a.nj <= 32) return run_by_depth<T, PRODUCT, 64, 32, 32, 8, DIRECT>(a, s);
-    return run_by_depth<T, PRODUCT, 64, 64, 32, 6, DIRECT>(a, s);
+    if (p.kernel == kLarge) return run_product<T, PRODUCT, Shape<256, 128, 4, 2, 32, 2>, DIRECT>(a, p, s);
+    if (p.kernel == kMiddle) return run_product<T, PRODUCT, Shape<128, 128, 2, 2, 32, 2>, DIRECT>(a, p, s);
+    if (a.nj <= 32) return run_by_depth<T, PRODUCT, 64, 32, 32, 8, DIRECT>(a, p, s);
+    return run_by_depth<T, PRODUCT, 64, 64, 32, 6, DIRECT>(a, p, s);
   } else {
-    const int64_t big = (int64_t)((a.ni + 255) / 256) * ((a.nj + 255) / 256);
     // operands that go through registers leave none for 256 x 256
-    if (big >= 128) return run_product<T, PRODUCT, std::conditional_t<DIRECT, Shape<256, 256, 2, 4, 32, 4>, Shape<256, 128, 4, 2, 32, 4>>, DIRECT>(a, s);
-    if (middle >= 128) return run_product<T, PRODUCT, Shape<128, 128, 2, 2, 32, 4>, DIRECT>(a, s);
-    if (a.nj <= 32) return run_by_depth<T, PRODUCT, 64, 32, 64, 8, DIRECT>(a, s);
-    return run_by_depth<T, PRODUCT, 64, 64, 64, 8, DIRECT>(a, s);
+    if (p.kernel == kLarge) return run_product<T, PRODUCT, std::conditional_t<DIRECT, Shape<256, 256, 2, 4, 32, 4>, Shape<256, 128, 4, 2, 32, 4>>, DIRECT>(a, p, s);
+    if (p.kernel == kMiddle) return run_product<T, PRODUCT, Shape<128, 128, 2, 2, 32, 4>, DIRECT>(a, p, s);
+    if (a.nj <= 32) return run_by_depth<T, PRODUCT, 64, 32, 64, 8, DIRECT>(a, p, s);
+    return run_by_depth<T, PRODUCT, 64, 64, 64, 8, DIRECT>(a, p, s);
   }
 }
 
