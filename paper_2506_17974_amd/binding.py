@@ -393,22 +393,50 @@ def kernel_name(k: int) -> str:
 # -- the linear layer --------------------------------------------------------
 class Checkpoint:
     """A samples x features tensor kept in 8 bits, as include/lqsgd_linear.h lays it out: `codes` (int8, samples x the features rounded
-    up to groups of 32) and `exponents` (uint8, samples x groups)."""
-    __slots__ = ("codes", "exponents", "features")
+    up to groups of 32) and `exponents` (uint8, samples x groups).  Made of those two, or by empty() with both in one allocation."""
+    __slots__ = ("features", "_codes", "_exponents", "_both", "_at")
 
     def __init__(self, codes, exponents, features):
-        self.codes, self.exponents, self.features = codes, exponents, int(features)
+        self.features, self._codes, self._exponents = int(features), codes, exponents
+        self._both = self._at = None
 
     @classmethod
     def empty(cls, samples, features, device="cuda"):
         import torch
-        groups = -(-int(features) // CHECKPOINT_GROUP)
-        return cls(torch.empty((samples, groups * CHECKPOINT_GROUP), dtype=torch.int8, device=device),
-                   torch.empty((samples, groups), dtype=torch.uint8, device=device), features)
+        self = cls(None, None, features)
+        groups = -(-self.features // CHECKPOINT_GROUP)
+        n = samples * groups * CHECKPOINT_GROUP
+        self._both = torch.empty(n + samples * groups, dtype=torch.uint8, device=device)
+        at = self._both.data_ptr()
+        self._at = (samples, self._both.get_device(), at, at + n, self.features)       # what LinearOps would find out about the two
+        return self
+
+    def _parts(self):
+        samples, groups = self._at[0], -(-self._at[4] // CHECKPOINT_GROUP)
+        n = samples * groups * CHECKPOINT_GROUP
+        import torch
+        self._codes = self._both[:n].view(torch.int8).view(samples, groups * CHECKPOINT_GROUP)
+        self._exponents = self._both[n:].view(samples, groups)
+
+    @property
+    def codes(self):
+        if self._codes is None:
+            self._parts()
+        return self._codes
+
+    @property
+    def exponents(self):
+        if self._exponents is None:
+            self._parts()
+        return self._exponents
+
+    @property
+    def samples(self):
+        return self._at[0] if self._at else self._codes.shape[0]
 
     @property
     def nbytes(self):
-        return self.codes.numel() + self.exponents.numel()
+        return self.samples * -(-self.features // CHECKPOINT_GROUP) * (CHECKPOINT_GROUP + 1)
 
 
 class LinearOps:
@@ -475,6 +503,9 @@ class LinearOps:
             raise LqsgdError(EINVAL, "%s has to be a Checkpoint" % what)
         if c.features != features:
             raise LqsgdError(ESHAPE, "%s has %d features, %d wanted" % (what, c.features, features))
+        at = c._at
+        if at is not None and at[0] == samples and at[1] == self._index and at[4] == features:
+            return at[2], at[3]
         groups = -(-features // CHECKPOINT_GROUP)
         codes, exps = c.codes, c.exponents
         if codes.dtype is not self._codes_type or codes.shape != (samples, groups * CHECKPOINT_GROUP) or \
@@ -515,11 +546,15 @@ class LinearOps:
         self._begin()
         if not isinstance(held, Checkpoint):
             raise LqsgdError(EINVAL, "held has to be a Checkpoint")
-        m, n = held.codes.shape[0], held.features
+        m, n = held.samples, held.features
         codes, exps = self._held("held", held, m, n)
         if out is None:
-            out = self._empty((m, n), dtype=dtype or self._torch.bfloat16, device=self.device)
-        _, _, ld = self._matrix("out", out, dtype, m, n)
+            dtype, ld = dtype or self._torch.bfloat16, n
+            if dtype not in self._types:
+                raise LqsgdError(EINVAL, "a checkpoint is not loaded as %s" % (dtype,))
+            out = self._empty(m, n, dtype=dtype, device=self.device)
+        else:
+            ld = self._matrix("out", out, dtype, m, n)[2]
         self._check(self._L.lqsgd_checkpoint_load(self._h, self._types[out.dtype], m, n, codes, exps, out.data_ptr(), ld))
         return out
 
@@ -535,7 +570,7 @@ class LinearOps:
         b = self._vector("bias", bias, T, n) if bias is not None else None
         r, ldr = (residual.data_ptr(), self._matrix("residual", residual, T, m, n)[2]) if residual is not None else (None, 0)
         if out is None:
-            out, ldy = self._empty((m, n), dtype=T, device=self.device), n
+            out, ldy = self._empty(m, n, dtype=T, device=self.device), n
         else:
             ldy = self._matrix("out", out, T, m, n)[2]
         zc, ze = self._held("save_z", save_z, m, n) if save_z is not None else (None, None)
@@ -559,7 +594,7 @@ class LinearOps:
         if dz is not None:
             pz, lddz = dz.data_ptr(), self._matrix("dz", dz, T, m, n)[2]
         elif want_dz:
-            dz = self._empty((m, n), dtype=T, device=self.device)
+            dz = self._empty(m, n, dtype=T, device=self.device)
             pz, lddz = dz.data_ptr(), n
         if dbias is None and want_dbias:
             if accumulate:
@@ -577,7 +612,7 @@ class LinearOps:
         T = dz.dtype
         _, k, ldw = self._matrix("w", w, T, n, None)
         if out is None:
-            out, lddx = self._empty((m, k), dtype=T, device=self.device), k
+            out, lddx = self._empty(m, k, dtype=T, device=self.device), k
         else:
             lddx = self._matrix("out", out, T, m, k)[2]
         self._check(self._L.lqsgd_linear_input_grad(self._h, self._types[T], m, n, k, dz.data_ptr(), lddz, w.data_ptr(), ldw, out.data_ptr(),
@@ -595,8 +630,12 @@ class LinearOps:
         if out is None:
             if accumulate:
                 raise LqsgdError(EINVAL, "accumulate needs the gradient to add to")
-            out = self._empty((n, k), dtype=dtype or self._f32, device=self.device)
-        _, _, lddw = self._matrix("out", out, dtype, n, k)
+            dtype, lddw = dtype or self._f32, k
+            if dtype not in self._types:
+                raise LqsgdError(EINVAL, "a gradient is not written as %s" % (dtype,))
+            out = self._empty(n, k, dtype=dtype, device=self.device)
+        else:
+            lddw = self._matrix("out", out, dtype, n, k)[2]
         self._check(self._L.lqsgd_linear_weight_grad(self._h, self._types[dz.dtype], m, n, k, dz.data_ptr(), lddz, xc, xe,
                                                      self._types[out.dtype], out.data_ptr(), lddw, 1 if accumulate else 0))
         return out

@@ -625,6 +625,7 @@ __device__ inline Where where(int tiles_i, int tiles_j, int tiles, int splits) {
   return Where{in / high, band * kBand + in % high, split};
 }
 
+// A tile's sum in `splits` parts.
 struct Split {
   int tiles_i, tiles_j, splits;
   int64_t steps;         // values of r of a split, a multiple of BK
@@ -759,10 +760,44 @@ template <int N>
 __device__ inline float* waiting(const ProductArgs& a, int64_t split, int64_t tile, int64_t tiles, int piece, int pieces, int lane) {
   return static_cast<float*>(a.workspace) + ((split * tiles + tile) * pieces + piece) * (64 * N) + lane * 4;
 }
-template <int N>
+template <int N, bool ATOMIC>
 __device__ inline void put_waiting(float* to, const float (&v)[N]) {
 #pragma unroll
-  for (int c = 0; c < N / 4; ++c) *reinterpret_cast<float4*>(to + c * 256) = make_float4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
+  for (int c = 0; c < N / 4; ++c) {
+    if constexpr (ATOMIC) {
+      uint64_t x[2];
+      __builtin_memcpy(x, v + 4 * c, 16);
+      uint64_t* p = reinterpret_cast<uint64_t*>(to + c * 256);
+      __hip_atomic_store(p, x[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __hip_atomic_store(p + 1, x[1], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    } else {
+      *reinterpret_cast<float4*>(to + c * 256) = make_float4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
+    }
+  }
+}
+
+template <int N, bool ATOMIC>
+__device__ inline void add_parts(float (&v)[N], const ProductArgs& a, const Split& sp, int64_t tile, int piece, int pieces, int lane) {
+#pragma unroll
+  for (int k = 0; k < N; ++k) v[k] = 0.f;
+#pragma unroll 4
+  for (int s = 0; s < sp.splits; ++s) {
+    const float* from = waiting<N>(a, s, tile, (int64_t)sp.tiles_i * sp.tiles_j, piece, pieces, lane);
+#pragma unroll
+    for (int c = 0; c < N / 4; ++c) {
+      float w[4];
+      if constexpr (ATOMIC) {
+        const uint64_t* p = reinterpret_cast<const uint64_t*>(from + c * 256);
+        const uint64_t x[2] = {__hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT),
+                               __hip_atomic_load(p + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)};
+        __builtin_memcpy(w, x, 16);
+      } else {
+        __builtin_memcpy(w, __builtin_assume_aligned(from + c * 256, 16), 16);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[4 * c + e] += w[e];
+    }
+  }
 }
 
 template <typename T, int PRODUCT, typename S, bool DIRECT>
@@ -873,7 +908,7 @@ __global__ __launch_bounds__(S::threads, S::threads >= 512 ? 2 : 1) void product
       P::get(v, strip, turn, lane);
       const int64_t j = j0 + P::row(piece, lane);
       if (sp.splits > 1) {
-        put_waiting<N>(waiting<N>(a, at.split, (int64_t)at.tj * sp.tiles_i + at.ti, (int64_t)sp.tiles_i * sp.tiles_j, piece, P::pieces, lane), v);
+        put_waiting<N, false>(waiting<N>(a, at.split, (int64_t)at.tj * sp.tiles_i + at.ti, (int64_t)sp.tiles_i * sp.tiles_j, piece, P::pieces, lane), v);
       } else {
         finish<T, PRODUCT>(v, bias, a, j, i, j < a.nj);
       }
@@ -888,15 +923,15 @@ __global__ __launch_bounds__(WAVES * 64) void product_by_depth_kernel(ProductArg
   using O = Operands<T, PRODUCT, BI, BJ, BK, 64, DIRECT>;
   constexpr int FI = BI / 32, FJ = BJ / 32, N = kRun<T, PRODUCT>;
   using P = Strips<FI, FJ, 1, 1, N>;
-  static_assert(FJ * P::bytes <= O::bytes, "a wavefront's sums have to fit its operands' place");
-  __shared__ __attribute__((aligned(1024))) char lds[WAVES * O::bytes];
+  constexpr int kPlace = O::bytes > FJ * P::bytes ? O::bytes : FJ * P::bytes;       // of a wavefront: its operands, then its sums
+  __shared__ __attribute__((aligned(1024))) char lds[WAVES * kPlace];
   const Where at = where(sp.tiles_i, sp.tiles_j, sp.tiles_i * sp.tiles_j, sp.splits);
   const int i0 = at.ti * BI;
   const int64_t j0 = (int64_t)at.tj * BJ;
   const int64_t first = at.split * sp.steps, last = min(a.depth, first + sp.steps);
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   lds_char* const all = (lds_char*)lds;
-  lds_char* const mine = all + wave * O::bytes;
+  lds_char* const mine = all + wave * kPlace;
   O o(a, i0, j0, last, lane);
   f32x16 acc[FI][FJ] = {};
   typename O::Regs g;
@@ -941,15 +976,38 @@ __global__ __launch_bounds__(WAVES * 64) void product_by_depth_kernel(ProductArg
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) {
       float x[N];
-      P::get(x, all + w * O::bytes + piece / P::turns * P::bytes, piece % P::turns, lane);
+      P::get(x, all + w * kPlace + piece / P::turns * P::bytes, piece % P::turns, lane);
 #pragma unroll
       for (int e = 0; e < N; ++e) v[e] += x[e];
     }
     if (sp.splits > 1) {
-      put_waiting<N>(waiting<N>(a, at.split, (int64_t)at.tj * sp.tiles_i + at.ti, (int64_t)sp.tiles_i * sp.tiles_j, piece, P::pieces, lane), v);
+      put_waiting<N, true>(waiting<N>(a, at.split, (int64_t)at.tj * sp.tiles_i + at.ti, (int64_t)sp.tiles_i * sp.tiles_j, piece, P::pieces, lane), v);
     } else {
       finish<T, PRODUCT>(v, bias, a, j, i, j < a.nj);
     }
+  }
+  if (sp.splits == 1) return;
+  // The workgroup that comes last to a tile adds up its parts, in the parts' order, whichever it is.  Parts are stored and read with
+  // agent-scope atomics, which go past the caches that the XCDs do not share: every store has arrived when vmcnt says so, and the
+  // barrier puts all of the workgroup's before its count.  (A release at agent scope would write back the XCD's whole L2, 8 us.)
+  const int tile = at.tj * sp.tiles_i + at.ti;
+  int* const arrived = a.arrived + tile;
+  __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();
+  if (t == 0) {
+    const bool last_one = __hip_atomic_fetch_add(arrived, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == sp.splits - 1;
+    if (last_one) __hip_atomic_store(arrived, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);        // for the next launch
+    *reinterpret_cast<volatile int*>(lds) = last_one;
+  }
+  __syncthreads();
+  if (*reinterpret_cast<volatile int*>(lds) == 0) return;
+  for (int piece = wave; piece < P::pieces; piece += WAVES) {
+    float v[N], bias[N];
+    const int i = i0 + P::column(piece, lane);
+    const int64_t j = j0 + P::row(piece, lane);
+    load_bias<T, PRODUCT>(bias, a, i);
+    add_parts<N, true>(v, a, sp, tile, piece, P::pieces, lane);
+    finish<T, PRODUCT>(v, bias, a, j, i, j < a.nj);
   }
 }
 
@@ -958,21 +1016,13 @@ template <typename T, int PRODUCT, typename P, int BI, int BJ>
 __global__ __launch_bounds__(256) void join_kernel(ProductArgs a, Split sp) {
   constexpr int N = kRun<T, PRODUCT>;
   const int lane = threadIdx.x & 63;
-  const int64_t all = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), tile = all / P::pieces, tiles = (int64_t)sp.tiles_i * sp.tiles_j;
+  const int64_t all = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), tile = all / P::pieces;
   const int piece = (int)(all - tile * P::pieces);
   const int i = (int)(tile % sp.tiles_i) * BI + P::column(piece, lane);
   const int64_t j = tile / sp.tiles_i * BJ + P::row(piece, lane);
-  float v[N] = {}, bias[N];
+  float v[N], bias[N];
   load_bias<T, PRODUCT>(bias, a, i);
-#pragma unroll 4
-  for (int s = 0; s < sp.splits; ++s) {
-    const float* from = waiting<N>(a, s, tile, tiles, piece, P::pieces, lane);
-#pragma unroll
-    for (int c = 0; c < N / 4; ++c) {
-      const float4 w = *reinterpret_cast<const float4*>(from + c * 256);
-      v[4 * c] += w.x, v[4 * c + 1] += w.y, v[4 * c + 2] += w.z, v[4 * c + 3] += w.w;
-    }
-  }
+  add_parts<N, false>(v, a, sp, tile, piece, P::pieces, lane);
   finish<T, PRODUCT>(v, bias, a, j, i, j < a.nj);
 }
 
@@ -997,13 +1047,13 @@ struct Geometry { int bi, bj, step; };
 template <typename T, int PRODUCT, bool DIRECT>
 Plan plan(const ProductArgs& a) {
   constexpr bool kWide = std::is_same_v<T, float>, kGrad = PRODUCT == kWeightGrad;
-  constexpr Rate rates[3] = {kWide ? kGrad ? Rate{2.6f, 1.9f, .2f} : Rate{3.2f, 2.7f, .3f}
+  constexpr Rate rates[3] = {kWide ? kGrad ? Rate{2.6f, 1.f, .1f} : Rate{3.2f, 1.2f, .2f}
                              : DIRECT ? kGrad ? Rate{3.6f, 1.5f, .35f} : Rate{3.4f, 1.f, .45f} : Rate{3.6f, 2.2f, .6f},
                              kWide ? kGrad ? Rate{6.f, 1.35f, .05f} : Rate{8.f, 1.85f, .05f}
                              : DIRECT ? kGrad ? Rate{4.f, .58f, .12f} : Rate{2.8f, .34f, 0.f} : Rate{5.f, .9f, .1f},
                              kWide ? kGrad ? Rate{6.5f, 1.36f, .1f} : Rate{8.f, 2.f, .5f}
                              : DIRECT ? kGrad ? Rate{9.f, .78f, .22f} : Rate{9.f, .62f, .25f} : Rate{8.f, .8f, .1f}};
-  const Geometry shapes[3] = {{64, a.nj <= 32 ? 32 : 64, kWide ? a.nj <= 32 ? 256 : 192 : 512}, {128, 128, 32}, {256, !kWide && DIRECT ? 256 : 128, 32}};
+  const Geometry shapes[3] = {{64, a.nj <= 32 ? 32 : 64, kWide ? a.nj <= 32 ? 256 : 128 : 512}, {128, 128, 32}, {256, !kWide && DIRECT ? 256 : 128, 32}};
   Plan best{};
   float least = 0.f;
   for (int k = 0; k < 3; ++k) {
@@ -1047,7 +1097,7 @@ hipError_t run_product(const ProductArgs& a, const Plan& p, hipStream_t s) {
 template <typename T, int PRODUCT, int BI, int BJ, int BK, int WAVES, bool DIRECT>
 hipError_t run_by_depth(const ProductArgs& a, const Plan& p, hipStream_t s) {
   product_by_depth_kernel<T, PRODUCT, BI, BJ, BK, WAVES, DIRECT><<<dim3((unsigned)(p.tiles * p.sp.splits)), WAVES * 64, 0, s>>>(a, p.sp);
-  return join<T, PRODUCT, Strips<BI / 32, BJ / 32, 1, 1, kRun<T, PRODUCT>>, BI, BJ>(a, p, s);
+  return hipGetLastError();
 }
 
 bool whole_chunks(const void* p, int64_t ld, int64_t length) {
@@ -1062,7 +1112,7 @@ hipError_t by_size(const ProductArgs& a, hipStream_t s) {
     if (p.kernel == kLarge) return run_product<T, PRODUCT, Shape<256, 128, 4, 2, 32, 2>, DIRECT>(a, p, s);
     if (p.kernel == kMiddle) return run_product<T, PRODUCT, Shape<128, 128, 2, 2, 32, 2>, DIRECT>(a, p, s);
     if (a.nj <= 32) return run_by_depth<T, PRODUCT, 64, 32, 32, 8, DIRECT>(a, p, s);
-    return run_by_depth<T, PRODUCT, 64, 64, 32, 6, DIRECT>(a, p, s);
+    return run_by_depth<T, PRODUCT, 64, 64, 16, 8, DIRECT>(a, p, s);
   } else {
     // operands that go through registers leave none for 256 x 256
     if (p.kernel == kLarge) return run_product<T, PRODUCT, std::conditional_t<DIRECT, Shape<256, 256, 2, 4, 32, 4>, Shape<256, 128, 4, 2, 32, 4>>, DIRECT>(a, p, s);

@@ -14,6 +14,7 @@ using namespace lqsgd::linear;
 struct lqsgd_linear {
   hipStream_t stream = nullptr;
   void* workspace = nullptr;
+  int* arrived = nullptr;     // behind it
   std::string err;
 };
 
@@ -65,11 +66,18 @@ int lqsgd_linear_create(void* hip_stream, lqsgd_linear** out) {
   lqsgd_linear* c = new (std::nothrow) lqsgd_linear;
   if (!c) return fail(nullptr, LQSGD_ENOMEM, "out of host memory");
   c->stream = static_cast<hipStream_t>(hip_stream);
-  hipError_t e = hipMalloc(&c->workspace, kWorkspaceBytes);
+  hipError_t e = hipMalloc(&c->workspace, kWorkspaceBytes + kTiles * sizeof(int));
   if (e != hipSuccess) {
     delete c;
     const int rc = done(nullptr, e, "hipMalloc of the workspace");
     return e == hipErrorOutOfMemory ? LQSGD_ENOMEM : rc;
+  }
+  c->arrived = reinterpret_cast<int*>(static_cast<char*>(c->workspace) + kWorkspaceBytes);
+  e = hipMemsetAsync(c->arrived, 0, kTiles * sizeof(int), c->stream);
+  if (e != hipSuccess) {
+    (void)hipFree(c->workspace);
+    delete c;
+    return done(nullptr, e, "clearing the workspace");
   }
   *out = c;
   return LQSGD_OK;
@@ -139,7 +147,7 @@ int lqsgd_linear_forward(lqsgd_linear* c, int32_t type, int32_t act, int64_t sam
   a.a = w; a.lda = ldw; a.b = x; a.ldb = ldx;
   a.bias = bias; a.residual = residual; a.ldr = ldr; a.act = act;
   a.z = Codes{z_codes, z_exponents}; a.y = Codes{y_codes, y_exponents};
-  a.out = y; a.ldo = ldy; a.workspace = c->workspace;
+  a.out = y; a.ldo = ldy; a.workspace = c->workspace; a.arrived = c->arrived;
   return done(c, launch_product(kForward, type, a, c->stream), "lqsgd_linear_forward");
 }
 
@@ -176,7 +184,7 @@ int lqsgd_linear_input_grad(lqsgd_linear* c, int32_t type, int64_t samples, int3
   ProductArgs a{};
   a.ni = cols; a.nj = samples; a.depth = rows;
   a.a = w; a.lda = ldw; a.b = dz; a.ldb = lddz;
-  a.out = dx; a.ldo = lddx; a.workspace = c->workspace;
+  a.out = dx; a.ldo = lddx; a.workspace = c->workspace; a.arrived = c->arrived;
   return done(c, launch_product(kInputGrad, type, a, c->stream), "lqsgd_linear_input_grad");
 }
 
@@ -195,7 +203,7 @@ int lqsgd_linear_weight_grad(lqsgd_linear* c, int32_t type, int64_t samples, int
   a.ni = cols; a.nj = rows; a.depth = samples;
   a.held = Codes{const_cast<int8_t*>(x_codes), const_cast<uint8_t*>(x_exponents)};
   a.b = dz; a.ldb = lddz;
-  a.out = dw; a.ldo = lddw; a.out_type = grad_type; a.accumulate = accumulate != 0; a.workspace = c->workspace;
+  a.out = dw; a.ldo = lddw; a.out_type = grad_type; a.accumulate = accumulate != 0; a.workspace = c->workspace; a.arrived = c->arrived;
   return done(c, launch_product(kWeightGrad, type, a, c->stream), "lqsgd_linear_weight_grad");
 }
 

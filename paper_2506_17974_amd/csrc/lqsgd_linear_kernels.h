@@ -10,7 +10,8 @@ namespace lqsgd {
 namespace linear {
 
 constexpr int kGroup = 32;                        // features that share an exponent in a checkpoint
-constexpr size_t kWorkspaceBytes = 64ull << 20;
+constexpr size_t kWorkspaceBytes = 64ull << 20;   // sums of parts, at most
+constexpr int kTiles = 8192;                      // tiles whose sum is in parts, at most (64 x 32, two parts)
 
 enum Type { kF32 = 0, kBF16 = 1, kF16 = 2 };
 enum Act { kNone = 0, kRelu = 1, kGelu = 2, kSilu = 3 };
@@ -39,6 +40,7 @@ struct ProductArgs {
   int32_t out_type;                               // kWeightGrad: kF32 or kBF16
   int32_t accumulate;                             // kWeightGrad
   void* workspace;
+  int* arrived;                                   // kTiles zeros: parts of a tile's sum that have come; the kernels leave zeros
 };
 
 hipError_t launch_product(int product, int type, const ProductArgs& a, hipStream_t s);
