@@ -1047,7 +1047,7 @@ struct Geometry { int bi, bj, step; };
 template <typename T, int PRODUCT, bool DIRECT>
 Plan plan(const ProductArgs& a) {
   constexpr bool kWide = std::is_same_v<T, float>, kGrad = PRODUCT == kWeightGrad;
-  constexpr Rate rates[3] = {kWide ? kGrad ? Rate{2.6f, 1.f, .1f} : Rate{3.2f, 1.2f, .2f}
+  constexpr Rate rates[3] = {kWide ? kGrad ? Rate{2.8f, 1.15f, .2f} : Rate{3.2f, 1.65f, .35f}
                              : DIRECT ? kGrad ? Rate{3.6f, 1.5f, .35f} : Rate{3.4f, 1.f, .45f} : Rate{3.6f, 2.2f, .6f},
                              kWide ? kGrad ? Rate{6.f, 1.35f, .05f} : Rate{8.f, 1.85f, .05f}
                              : DIRECT ? kGrad ? Rate{4.f, .58f, .12f} : Rate{2.8f, .34f, 0.f} : Rate{5.f, .9f, .1f},
