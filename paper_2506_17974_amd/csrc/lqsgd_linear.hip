@@ -61,6 +61,14 @@ __device__ inline float factor_of(uint32_t byte) {
   return byte == 255u ? __builtin_nanf("") : __builtin_bit_cast(float, byte << 23);
 }
 
+__device__ inline void decode(float (&v)[8], uint2 w, float f) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    v[k] = (float)(int8_t)(w.x >> (8 * k)) * f;
+    v[4 + k] = (float)(int8_t)(w.y >> (8 * k)) * f;
+  }
+}
+
 // Phi(z) = erfc(-z / sqrt 2) / 2 by the rational form of Hastings (Abramowitz and Stegun 7.1.26, |error| <= 1.5e-7): with
 // t = 1 / (1 + p |x|), erfc(|x|) = (a1 t + ... + a5 t^5) exp(-x^2).  Half the instructions of a correctly rounded erf, and its
 // error is that of a few fp32 operations.  `density`: exp(-z^2 / 2).
@@ -130,13 +138,27 @@ __device__ inline void load_values(float (&v)[N], const T* p, int n) {
     for (int k = 0; k < N; ++k) v[k] = k < n ? widen(p[k]) : 0.f;
   }
 }
+// BYTES to memory of any alignment, past the caches: nothing here reads its outputs again, and what does soon after finds them no
+// later (8192 x 4096 values: loading a checkpoint 20 -> 16 us, that and an addition that reads them 39.8 -> 38.0; small tensors alike).
+// Not so the codes of checkpoints, which fit the memory-side cache longer (saving and loading 8192 x 4096 values 34 us, past it 40).
+template <int BYTES>
+__device__ inline void stream_out(void* p, const void* from) {
+  constexpr int kWords = BYTES >= 16 ? 4 : BYTES / 4;
+  typedef uint32_t Words __attribute__((ext_vector_type(kWords), aligned(1)));
+#pragma unroll
+  for (int k = 0; k < BYTES / 4 / kWords; ++k) {
+    Words w;
+    __builtin_memcpy(&w, static_cast<const char*>(from) + 16 * k, sizeof w);
+    __builtin_nontemporal_store(w, reinterpret_cast<Words*>(p) + k);
+  }
+}
 template <int N, typename T>
 __device__ inline void store_values(T* p, const float (&v)[N], int n) {
   if (n >= N) {
     T t[N];
 #pragma unroll
     for (int k = 0; k < N; ++k) t[k] = narrow<T>(v[k]);
-    __builtin_memcpy(p, t, sizeof t);
+    stream_out<sizeof t>(p, t);
   } else {
 #pragma unroll
     for (int k = 0; k < N; ++k)
@@ -168,17 +190,16 @@ __device__ inline void pack_codes(uint32_t (&w)[N / 4], const float (&v)[N], flo
 // ---------------------------------------------------------------------------
 // checkpoints
 // ---------------------------------------------------------------------------
-// A thread takes 8 consecutive values, four lanes a group; a workgroup a run of 256 such pieces of the whole tensor, rows end to
-// end, so that narrow tensors fill their lanes too.  Bound by memory: s + 33/32 bytes per value.
+// A thread takes a piece of 8 consecutive values, four lanes a group; a workgroup a run of 256 pieces of the whole tensor, rows end to
+// end, so that narrow tensors fill their lanes too.  Bound by memory: s + 33/32 bytes per value (four pieces a thread on their way at
+// once: no faster, small tensors 2.8 -> 3.9 us).
 constexpr int kPiece = 8;
 
 template <typename T>
 __global__ __launch_bounds__(256) void checkpoint_save_kernel(const T* x, int64_t ldx, Codes c, int64_t samples, int features, uint32_t pieces) {
-  const int64_t first = (int64_t)blockIdx.x * 256;
-  const int64_t row0 = first / pieces;
-  const uint32_t at = (uint32_t)(first - row0 * pieces) + threadIdx.x;
+  const int64_t first = (int64_t)blockIdx.x * 256, row0 = first / pieces;
+  const uint32_t at = (uint32_t)(first - row0 * pieces) + threadIdx.x, piece = at % pieces;
   const int64_t row = row0 + at / pieces;
-  const uint32_t piece = at % pieces;
   const bool there = row < samples;
   float v[kPiece];
   load_values(v, x + row * ldx + piece * kPiece, there ? features - (int)(piece * kPiece) : 0);
@@ -191,58 +212,95 @@ __global__ __launch_bounds__(256) void checkpoint_save_kernel(const T* x, int64_
 
 template <typename T>
 __global__ __launch_bounds__(256) void checkpoint_load_kernel(T* x, int64_t ldx, Codes c, int64_t samples, int features, uint32_t pieces) {
-  const int64_t first = (int64_t)blockIdx.x * 256;
-  const int64_t row0 = first / pieces;
-  const uint32_t at = (uint32_t)(first - row0 * pieces) + threadIdx.x;
+  const int64_t first = (int64_t)blockIdx.x * 256, row0 = first / pieces;
+  const uint32_t at = (uint32_t)(first - row0 * pieces) + threadIdx.x, piece = at % pieces;
   const int64_t row = row0 + at / pieces;
-  const uint32_t piece = at % pieces;
   if (row >= samples) return;
   const uint2 w = *reinterpret_cast<const uint2*>(c.codes + row * ((int64_t)pieces * kPiece) + piece * kPiece);
-  const float f = factor_of(c.exponents[row * (pieces >> 2) + (piece >> 2)]);
   float v[kPiece];
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    v[k] = (float)(int8_t)(w.x >> (8 * k)) * f;
-    v[4 + k] = (float)(int8_t)(w.y >> (8 * k)) * f;
-  }
+  decode(v, w, factor_of(c.exponents[row * (pieces >> 2) + (piece >> 2)]));
   store_values(x + row * ldx + piece * kPiece, v, features - (int)(piece * kPiece));
 }
 
 // ---------------------------------------------------------------------------
 // activation backward
 // ---------------------------------------------------------------------------
-// A workgroup takes a strip of 8 << lanes_log2 features and a run of samples; a lane keeps 8 features' sums.  Lanes that the strip
-// does not fill take further samples.  Strips' sums over runs go to `part` (runs x rows) where there is more than one run.
-template <typename T>
+// Slopes as a table: act'(z) for z = |q| 2^e has 128 values an exponent, and act'(-z) = 1 - act'(z) for gelu and silu.  Rows e = -30
+// (below, z is under 2^-23 and the slope 1/2) to 5 (above, it is 0 or 1 to 2^-24 but for q = 0), each entry act'(z) - 1/2.
+constexpr int kSlopeRows = 36, kSlopes = kSlopeRows * 128, kSlopeLow = -30;
+static_assert(2 * kSlopes == kSlopeFloats);
+
+__global__ __launch_bounds__(256) void slopes_kernel(float* table) {
+  const int at = (int)blockIdx.x * 256 + threadIdx.x;              // gelu's, then silu's
+  const int act = at < kSlopes ? kGelu : kSilu, in = at % kSlopes;
+  const float z[1] = {(float)(in & 127) * power_of_two(kSlopeLow + (in >> 7))};
+  float d[1] = {1.f};
+  times_slope(d, z, act);
+  table[at] = d[0] - 0.5f;
+}
+
+// d *= act'(z) of 8 codes of a group.
+__device__ inline void times_tabled_slope(float (&d)[8], uint2 w, uint32_t byte, const float* table) {
+  const float* row = table + min(max((int)byte - 127 - kSlopeLow, 0), kSlopeRows - 1) * 128;
+  const float half = byte == 255u ? __builtin_nanf("") : 0.5f;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const int q = (int8_t)((k < 4 ? w.x : w.y) >> (8 * (k & 3)));
+    const float s = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, row[abs(q) & 127]) ^ ((uint32_t)q & 0x80000000u));
+    d[k] *= s + half;
+  }
+}
+
+// A workgroup takes a strip of 8 << lanes_log2 features and a run of samples; a lane keeps 8 features' sums and has 4 samples on
+// their way.  Lanes that the strip does not fill take further samples.  Strips' sums over runs go to `part` (runs x rows) where
+// there is more than one run.  TABLE: gelu or silu of many samples, slopes from LDS (by their formulas, 27 instructions a value, the
+// vector units took 54 us for 4096 x 11008 bfloat16 values, whose memory traffic takes 32).
+template <typename T, bool TABLE>
 __global__ __launch_bounds__(256) void activation_backward_kernel(const T* dy, int64_t lddy, Codes z, T* dz, int64_t lddz, float* dbias,
-                                                                  int accumulate, float* part, int64_t samples, int rows, int act,
-                                                                  int lanes_log2, int64_t run) {
+                                                                  int accumulate, float* part, const float* slopes, int64_t samples,
+                                                                  int rows, int act, int lanes_log2, int64_t run) {
   __shared__ float sums[256][kPiece + 1];
+  __shared__ float table[TABLE ? kSlopes : 1];
   const int lanes = 1 << lanes_log2, t = threadIdx.x;
+  if constexpr (TABLE) {
+    for (int k = t * 4; k < kSlopes; k += 1024) *reinterpret_cast<float4*>(table + k) = *reinterpret_cast<const float4*>(slopes + k);
+    __syncthreads();
+  }
   const int feature = ((int)blockIdx.x * lanes + (t & (lanes - 1))) * kPiece;
   const int n = rows - feature;
   const int groups = (rows + kGroup - 1) / kGroup;
   const int64_t first = (int64_t)blockIdx.y * run, last = min(samples, first + run);
   float s[kPiece] = {};
   if (n > 0) {
-#pragma unroll 4
-    for (int64_t m = first + (t >> lanes_log2); m < last; m += 256 >> lanes_log2) {
-      float v[kPiece];
-      load_values(v, dy + m * lddy + feature, n);
-      if (act != kNone) {
-        const uint2 w = *reinterpret_cast<const uint2*>(z.codes + m * ((int64_t)groups * kGroup) + feature);
-        const float f = factor_of(z.exponents[m * groups + feature / kGroup]);
-        float zv[kPiece];
+    constexpr int kAtOnce = 4;
+    const int step = 256 >> lanes_log2;
+    for (int64_t m = first + (t >> lanes_log2); m < last; m += kAtOnce * step) {
+      float v[kAtOnce][kPiece];
+      uint2 w[kAtOnce] = {};
+      uint32_t e[kAtOnce] = {};
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          zv[k] = (float)(int8_t)(w.x >> (8 * k)) * f;
-          zv[4 + k] = (float)(int8_t)(w.y >> (8 * k)) * f;
-        }
-        times_slope(v, zv, act);
+      for (int k = 0; k < kAtOnce; ++k) {
+        const int64_t row = min(m + k * step, last - 1);   // beyond the end: read, not used
+        load_values(v[k], dy + row * lddy + feature, n);
+        if (act == kNone) continue;
+        w[k] = *reinterpret_cast<const uint2*>(z.codes + row * ((int64_t)groups * kGroup) + feature);
+        e[k] = z.exponents[row * groups + feature / kGroup];
       }
-      if (dz) store_values(dz + m * lddz + feature, v, n);
 #pragma unroll
-      for (int k = 0; k < kPiece; ++k) s[k] += v[k];
+      for (int k = 0; k < kAtOnce; ++k) {
+        const int64_t row = m + k * step;
+        if (row >= last) break;
+        if constexpr (TABLE) {
+          times_tabled_slope(v[k], w[k], e[k], table);
+        } else if (act != kNone) {
+          float zv[kPiece];
+          decode(zv, w[k], factor_of(e[k]));
+          times_slope(v[k], zv, act);
+        }
+        if (dz) store_values(dz + row * lddz + feature, v[k], n);
+#pragma unroll
+        for (int c = 0; c < kPiece; ++c) s[c] += v[k][c];
+      }
     }
   }
   if (!dbias) return;
@@ -265,8 +323,10 @@ __global__ __launch_bounds__(256) void sum_runs_kernel(const float* part, float*
   __shared__ float sums[4][64];
   const int f = (int)blockIdx.x * 64 + (threadIdx.x & 63), w = threadIdx.x >> 6;
   float s = 0.f;
-  if (f < rows)
+  if (f < rows) {
+#pragma unroll 8
     for (int k = w; k < runs; k += 4) s += part[(int64_t)k * rows + f];
+  }
   sums[w][threadIdx.x & 63] = s;
   __syncthreads();
   if (w == 0 && f < rows) {
@@ -1177,24 +1237,34 @@ hipError_t launch_checkpoint_load(int type, int64_t samples, int32_t features, C
   });
 }
 
+hipError_t launch_slopes(float* slopes, hipStream_t s) {
+  slopes_kernel<<<dim3(kSlopeFloats / 256), 256, 0, s>>>(slopes);
+  return hipGetLastError();
+}
+
 hipError_t launch_activation_backward(int type, int act, int64_t samples, int32_t rows, const void* dy, int64_t lddy, Codes z, void* dz,
-                                      int64_t lddz, float* dbias, int accumulate, void* workspace, hipStream_t s) {
+                                      int64_t lddz, float* dbias, int accumulate, void* workspace, const float* slopes, hipStream_t s) {
   const int pieces = (rows + kPiece - 1) / kPiece;
-  // Few samples: strips of 128 features leave 16 samples to go on at a time, and one launch does (64 x 1024 fp32 6.0 us instead of 8.4).
+  // Few samples: strips of 128 features leave 16 samples to go on at a time, and one launch does (64 x 1024 fp32 6.8 us instead of 6.4 + 2.1).
   const bool one_run = samples <= 256;
   int lanes_log2 = 0;
   while ((1 << lanes_log2) < pieces && lanes_log2 < (one_run ? 4 : 6)) ++lanes_log2;
   const int strips = (pieces + (1 << lanes_log2) - 1) >> lanes_log2;
-  const int64_t at_once = 256 >> lanes_log2;
-  const int64_t most = std::max<int64_t>(1, 2048 / strips);
-  const int64_t rounds = std::max<int64_t>(4, (samples + at_once * most - 1) / (at_once * most));
+  const int64_t at_once = 4 * (256 >> lanes_log2);
+  // otherwise about 1024 workgroups, four a CU
+  const int64_t most = std::max<int64_t>(1, 1024 / strips);
+  const int64_t rounds = (samples + at_once * most - 1) / (at_once * most);
   const int64_t run = one_run ? samples : rounds * at_once;
   const int64_t runs = samples == 0 ? 1 : (samples + run - 1) / run;
   float* part = dbias && runs > 1 ? static_cast<float*>(workspace) : nullptr;
+  // the table pays from about 12 samples a lane on
+  const bool table = (act == kGelu || act == kSilu) && !one_run && rounds >= 3;
+  if (act == kSilu) slopes += kSlopes;
   hipError_t e = by_type(type, [&](auto zero) {
     using T = decltype(zero);
-    activation_backward_kernel<T><<<dim3((unsigned)strips, (unsigned)runs), 256, 0, s>>>(
-        static_cast<const T*>(dy), lddy, z, static_cast<T*>(dz), lddz, dbias, accumulate, part, samples, rows, act, lanes_log2, run);
+    auto* kernel = table ? activation_backward_kernel<T, true> : activation_backward_kernel<T, false>;
+    kernel<<<dim3((unsigned)strips, (unsigned)runs), 256, 0, s>>>(static_cast<const T*>(dy), lddy, z, static_cast<T*>(dz), lddz, dbias, accumulate,
+                                                                  part, slopes, samples, rows, act, lanes_log2, run);
     return hipGetLastError();
   });
   if (e != hipSuccess || !part) return e;

@@ -15,6 +15,7 @@ struct lqsgd_linear {
   hipStream_t stream = nullptr;
   void* workspace = nullptr;
   int* arrived = nullptr;     // behind it
+  float* slopes = nullptr;    // behind those
   std::string err;
 };
 
@@ -66,18 +67,20 @@ int lqsgd_linear_create(void* hip_stream, lqsgd_linear** out) {
   lqsgd_linear* c = new (std::nothrow) lqsgd_linear;
   if (!c) return fail(nullptr, LQSGD_ENOMEM, "out of host memory");
   c->stream = static_cast<hipStream_t>(hip_stream);
-  hipError_t e = hipMalloc(&c->workspace, kWorkspaceBytes + kTiles * sizeof(int));
+  hipError_t e = hipMalloc(&c->workspace, kWorkspaceBytes + kTiles * sizeof(int) + kSlopeFloats * sizeof(float));
   if (e != hipSuccess) {
     delete c;
     const int rc = done(nullptr, e, "hipMalloc of the workspace");
     return e == hipErrorOutOfMemory ? LQSGD_ENOMEM : rc;
   }
   c->arrived = reinterpret_cast<int*>(static_cast<char*>(c->workspace) + kWorkspaceBytes);
+  c->slopes = reinterpret_cast<float*>(c->arrived + kTiles);
   e = hipMemsetAsync(c->arrived, 0, kTiles * sizeof(int), c->stream);
+  if (e == hipSuccess) e = launch_slopes(c->slopes, c->stream);
   if (e != hipSuccess) {
     (void)hipFree(c->workspace);
     delete c;
-    return done(nullptr, e, "clearing the workspace");
+    return done(nullptr, e, "preparing the workspace");
   }
   *out = c;
   return LQSGD_OK;
@@ -166,7 +169,7 @@ int lqsgd_linear_activation_backward(lqsgd_linear* c, int32_t type, int32_t act,
   if (!aligned(dy, size_of(type)) || !aligned(dz, size_of(type)) || !aligned(dbias, 4)) return fail(c, LQSGD_EINVAL, kBadAlign);
   if (samples == 0 && !dbias) return LQSGD_OK;
   const Codes held{const_cast<int8_t*>(z_codes), const_cast<uint8_t*>(z_exponents)};
-  return done(c, launch_activation_backward(type, act, samples, rows, dy, lddy, held, dz, lddz, dbias, accumulate != 0, c->workspace, c->stream),
+  return done(c, launch_activation_backward(type, act, samples, rows, dy, lddy, held, dz, lddz, dbias, accumulate != 0, c->workspace, c->slopes, c->stream),
               "lqsgd_linear_activation_backward");
 }
 

@@ -11,6 +11,7 @@ namespace linear {
 
 constexpr int kGroup = 32;                        // features that share an exponent in a checkpoint
 constexpr size_t kWorkspaceBytes = 64ull << 20;   // sums of parts, at most
+constexpr int kSlopeFloats = 2 * 36 * 128;        // slopes of gelu and silu for every code and exponent that needs one
 constexpr int kTiles = 8192;                      // tiles whose sum is in parts, at most (64 x 32, two parts)
 
 enum Type { kF32 = 0, kBF16 = 1, kF16 = 2 };
@@ -47,7 +48,8 @@ hipError_t launch_product(int product, int type, const ProductArgs& a, hipStream
 hipError_t launch_checkpoint_save(int type, int64_t samples, int32_t features, const void* x, int64_t ldx, Codes c, hipStream_t s);
 hipError_t launch_checkpoint_load(int type, int64_t samples, int32_t features, Codes c, void* x, int64_t ldx, hipStream_t s);
 hipError_t launch_activation_backward(int type, int act, int64_t samples, int32_t rows, const void* dy, int64_t lddy, Codes z, void* dz,
-                                      int64_t lddz, float* dbias, int accumulate, void* workspace, hipStream_t s);
+                                      int64_t lddz, float* dbias, int accumulate, void* workspace, const float* slopes, hipStream_t s);
+hipError_t launch_slopes(float* slopes, hipStream_t s);       // kSlopeFloats of them, once for a context
 
 }  // namespace linear
 }  // namespace lqsgd
