@@ -9,6 +9,7 @@
 #include <vector>
 
 #include "lqsgd.h"
+#include "lqsgd_linear.h"
 #include "lqsgd_plan.h"
 
 static int failures = 0;
@@ -76,6 +77,13 @@ static void check_tiles(const lqsgd_config& c, const std::vector<lqsgd_layer>& l
 }
 
 int main() {
+  // the linear layer's entry points without a context, and sizes of checkpoints
+  EXPECT(lqsgd_checkpoint_stride(1) == 32 && lqsgd_checkpoint_stride(513) == 544 && lqsgd_checkpoint_stride(LQSGD_LINEAR_MAX_FEATURES) == LQSGD_LINEAR_MAX_FEATURES);
+  EXPECT(lqsgd_checkpoint_stride(0) == LQSGD_ESHAPE && lqsgd_checkpoint_stride(INT32_MIN) == LQSGD_ESHAPE && lqsgd_checkpoint_stride(INT32_MAX) == LQSGD_ESHAPE);
+  EXPECT(lqsgd_linear_create(nullptr, nullptr) == LQSGD_EINVAL && lqsgd_linear_destroy(nullptr) == LQSGD_OK);
+  EXPECT(lqsgd_linear_synchronize(nullptr) == LQSGD_EINVAL && std::strlen(lqsgd_linear_last_error(nullptr)) > 0);
+  EXPECT(lqsgd_linear_weight_grad(nullptr, 0, 1, 1, 1, nullptr, 1, nullptr, nullptr, 0, nullptr, 1, 0) == LQSGD_EINVAL);
+
   lqsgd_plan_info info;
   std::vector<lqsgd_layer> resnet = {{64, 27, 0}, {64, 576, 0}, {128, 1152, 0}, {512, 4608, 0}, {10, 512, 0},
                                      {64, 1, LQSGD_LAYER_VECTOR}, {10, 1, LQSGD_LAYER_VECTOR}};
