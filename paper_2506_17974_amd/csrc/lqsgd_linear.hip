@@ -907,6 +907,8 @@ __global__ __launch_bounds__(S::threads, S::threads >= 512 ? 2 : 1) void product
 #pragma unroll
     for (int k = 16; k < S::BK; k += 16) {
       next.read(here, wi, wj, k, lane);
+      // the reads go first, for the products to hide them (registers for that are left where nothing else goes through them)
+      if constexpr (!O::kRegisters) __builtin_amdgcn_sched_barrier(0);
       now.multiply(acc);
       now = next;
     }
@@ -918,6 +920,7 @@ __global__ __launch_bounds__(S::threads, S::threads >= 512 ? 2 : 1) void product
     asm volatile("" ::: "memory");
     o.fetch(here, r + S::buffers * S::BK);
     next.read(there, wi, wj, 0, lane);
+    if constexpr (!O::kRegisters) __builtin_amdgcn_sched_barrier(0);
     now.multiply(acc);
     now = next;
   };
@@ -1251,8 +1254,8 @@ hipError_t launch_activation_backward(int type, int act, int64_t samples, int32_
   while ((1 << lanes_log2) < pieces && lanes_log2 < (one_run ? 4 : 6)) ++lanes_log2;
   const int strips = (pieces + (1 << lanes_log2) - 1) >> lanes_log2;
   const int64_t at_once = 4 * (256 >> lanes_log2);
-  // otherwise about 1024 workgroups, four a CU
-  const int64_t most = std::max<int64_t>(1, 1024 / strips);
+  // otherwise up to 1280 workgroups, the five a CU that run together (4096 x 11008 bf16: 58 us, 768 66, 2048 65)
+  const int64_t most = std::max<int64_t>(1, 1280 / strips);
   const int64_t rounds = (samples + at_once * most - 1) / (at_once * most);
   const int64_t run = one_run ? samples : rounds * at_once;
   const int64_t runs = samples == 0 ? 1 : (samples + run - 1) / run;
