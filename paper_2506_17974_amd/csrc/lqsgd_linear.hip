@@ -1055,7 +1055,9 @@ __global__ __launch_bounds__(WAVES * 64) void product_by_depth_kernel(ProductArg
   // barrier puts all of the workgroup's before its count.  (A release at agent scope would write back the XCD's whole L2, 8 us.)
   const int tile = at.tj * sp.tiles_i + at.ti;
   int* const arrived = a.arrived + tile;
+  asm volatile("" ::: "memory");
   __builtin_amdgcn_s_waitcnt(0);
+  asm volatile("" ::: "memory");
   __syncthreads();
   if (t == 0) {
     const bool last_one = __hip_atomic_fetch_add(arrived, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == sp.splits - 1;
@@ -1091,13 +1093,13 @@ __global__ __launch_bounds__(256) void join_kernel(ProductArgs a, Split sp) {
 
 // ---- which kernel a product takes ----
 // Three kernels serve a product: by depth (64 x 64 tiles, the sum shared out among a workgroup's wavefronts), 128 x 128 tiles and
-// the largest ones, each with the sum whole or in parts that a join adds up.  The one with the least expected time is taken:
-//   1.5 us + turns (turn + steps (step + more w)) + [parts > 1] (4 us + what the join reads and writes at 4.5 TB/s)
-// for `turns` rounds of 256 workgroups of `steps` steps each and w = the share of the CUs that have one.  The figures are fits to
-// the three kernels' times over 60 products from 64 x 64 x 1024 to 8192 x 2048 x 1024 in bfloat16 and fp32; taken by them the
-// products cost 2 % more than each one's best.  E.g. (bf16, ni x nj x depth: by depth / 128 x 128 / 256 x 256) 1024 x 1024 x 1024
-// 8 / 17 / 30 us, 2048 x 2048 x 2048 40 / 30 / 51, 4096 x 4096 x 512 74 / 29 / 24; fp32 512 x 4096 x 4096 154 / 239 / 283, in 4 parts
-// by the last 99.
+// the largest ones, each with the sum whole or in parts that are added up at the end.  The one with the least expected time is taken:
+//   1.5 us + turns (turn + steps (step + more w)) + [parts > 1] (4 us + what the join writes and reads at 4.5 TB/s)
+// for `turns` rounds of 256 workgroups of `steps` steps each and w = the share of the CUs that have one; by depth, where one workgroup
+// adds up a tile, 0.35 us a part more.  The figures are fits to the three kernels' times over 120 products from 64 x 1024 x 64 to
+// 8192 x 2048 x 1024 in bfloat16 and fp32; taken by them the products cost 2 % more than each one's best.  E.g. (bf16,
+// ni x nj x depth: by depth / 128 x 128 / 256 x 256) 1024 x 1024 x 1024 8 / 16 / 29 us, 2048 x 2048 x 2048 39 / 28 / 50,
+// 4096 x 4096 x 512 72 / 28 / 23; fp32 512 x 4096 x 4096 139 / 240 / 283, in 4 parts by the last 100.
 struct Rate { float turn, step, more; };
 enum Kernel { kByDepth = 0, kMiddle = 1, kLarge = 2 };
 struct Plan {
@@ -1130,7 +1132,7 @@ Plan plan(const ProductArgs& a) {
       const int64_t groups = tiles * parts, turns = (groups + 255) / 256;
       const Rate& r = rates[k];
       float us = 1.5f + (float)turns * (r.turn + (float)per * (r.step + r.more * std::min(1.f, (float)groups / 256.f)));
-      if (parts > 1) us += 4.f + 4e-6f / 4.5f * (float)(groups * g.bi * g.bj);
+      if (parts > 1) us += 4.f + 4e-6f / 4.5f * (float)(groups * g.bi * g.bj) + (k == kByDepth ? .35f * (float)parts : 0.f);
       if (k + parts == 1 || us < least) {
         least = us;
         best.kernel = (Kernel)k;
@@ -1170,7 +1172,7 @@ bool whole_chunks(const void* p, int64_t ld, int64_t length) {
 template <typename T, int PRODUCT, bool DIRECT>
 hipError_t by_size(const ProductArgs& a, hipStream_t s) {
   const Plan p = plan<T, PRODUCT, DIRECT>(a);
-  if (p.tiles > INT32_MAX) return hipErrorInvalidValue;
+  if (p.tiles * p.sp.splits >= (int64_t(1) << 32) / 512) return hipErrorInvalidValue;      // threads of a launch: 2^32
   if constexpr (std::is_same_v<T, float>) {
     if (p.kernel == kLarge) return run_product<T, PRODUCT, Shape<256, 128, 4, 2, 32, 2>, DIRECT>(a, p, s);
     if (p.kernel == kMiddle) return run_product<T, PRODUCT, Shape<128, 128, 2, 2, 32, 2>, DIRECT>(a, p, s);
@@ -1218,25 +1220,39 @@ hipError_t launch_product(int product_kind, int type, const ProductArgs& a, hipS
   });
 }
 
+// A launch has fewer than 2^32 threads: longer tensors go in slabs of samples.
+template <typename F>
+hipError_t by_slabs(int64_t samples, uint32_t pieces, F&& launch) {
+  const int64_t slab = (int64_t(1) << 31) / pieces;
+  for (int64_t at = 0; at < samples; at += slab) {
+    const int64_t n = std::min(slab, samples - at);
+    hipError_t e = launch(at, n, (unsigned)((n * pieces + 255) / 256));
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 hipError_t launch_checkpoint_save(int type, int64_t samples, int32_t features, const void* x, int64_t ldx, Codes c, hipStream_t s) {
   const uint32_t pieces = (uint32_t)((features + kGroup - 1) / kGroup * (kGroup / kPiece));
-  const int64_t blocks = (samples * pieces + 255) / 256;
-  if (blocks > INT32_MAX) return hipErrorInvalidValue;
   return by_type(type, [&](auto zero) {
     using T = decltype(zero);
-    checkpoint_save_kernel<T><<<dim3((unsigned)blocks), 256, 0, s>>>(static_cast<const T*>(x), ldx, c, samples, features, pieces);
-    return hipGetLastError();
+    return by_slabs(samples, pieces, [&](int64_t at, int64_t n, unsigned blocks) {
+      const Codes part{c.codes + at * pieces * kPiece, c.exponents + at * (pieces >> 2)};
+      checkpoint_save_kernel<T><<<dim3(blocks), 256, 0, s>>>(static_cast<const T*>(x) + at * ldx, ldx, part, n, features, pieces);
+      return hipGetLastError();
+    });
   });
 }
 
 hipError_t launch_checkpoint_load(int type, int64_t samples, int32_t features, Codes c, void* x, int64_t ldx, hipStream_t s) {
   const uint32_t pieces = (uint32_t)((features + kGroup - 1) / kGroup * (kGroup / kPiece));
-  const int64_t blocks = (samples * pieces + 255) / 256;
-  if (blocks > INT32_MAX) return hipErrorInvalidValue;
   return by_type(type, [&](auto zero) {
     using T = decltype(zero);
-    checkpoint_load_kernel<T><<<dim3((unsigned)blocks), 256, 0, s>>>(static_cast<T*>(x), ldx, c, samples, features, pieces);
-    return hipGetLastError();
+    return by_slabs(samples, pieces, [&](int64_t at, int64_t n, unsigned blocks) {
+      const Codes part{c.codes + at * pieces * kPiece, c.exponents + at * (pieces >> 2)};
+      checkpoint_load_kernel<T><<<dim3(blocks), 256, 0, s>>>(static_cast<T*>(x) + at * ldx, ldx, part, n, features, pieces);
+      return hipGetLastError();
+    });
   });
 }
 

@@ -55,6 +55,7 @@ constexpr const char kNull[] = "a pointer that is needed is NULL";
 constexpr const char kBadType[] = "unknown type or activation";
 constexpr const char kBadSize[] = "samples, features or a stride out of range";
 constexpr const char kBadAlign[] = "a pointer is not aligned to its type";
+constexpr const char kOver[] = "an output lies over an input";
 constexpr const char kBadCodes[] = "a checkpoint needs both of its pointers, and codes aligned to 16 bytes";
 
 }  // namespace
@@ -144,6 +145,7 @@ int lqsgd_linear_forward(lqsgd_linear* c, int32_t type, int32_t act, int64_t sam
   const uintptr_t s = size_of(type);
   if (!aligned(x, s) || !aligned(w, s) || !aligned(bias, s) || !aligned(residual, s) || !aligned(y, s)) return fail(c, LQSGD_EINVAL, kBadAlign);
   if (!codes_ok(z_codes, z_exponents, true) || !codes_ok(y_codes, y_exponents, true)) return fail(c, LQSGD_EINVAL, kBadCodes);
+  if (y == x || y == w || y == bias) return fail(c, LQSGD_EINVAL, kOver);
   if (residual == y && ldr != ldy) return fail(c, LQSGD_EINVAL, "y is the residual, with another stride");
   ProductArgs a{};
   a.ni = rows; a.nj = samples; a.depth = cols;
@@ -167,6 +169,7 @@ int lqsgd_linear_activation_backward(lqsgd_linear* c, int32_t type, int32_t act,
     if (!codes_ok(z_codes, z_exponents, act == LQSGD_ACT_NONE)) return fail(c, LQSGD_EINVAL, kBadCodes);
   }
   if (!aligned(dy, size_of(type)) || !aligned(dz, size_of(type)) || !aligned(dbias, 4)) return fail(c, LQSGD_EINVAL, kBadAlign);
+  if (dz == dy && dz && lddz != lddy) return fail(c, LQSGD_EINVAL, "dz is dy, with another stride");
   if (samples == 0 && !dbias) return LQSGD_OK;
   const Codes held{const_cast<int8_t*>(z_codes), const_cast<uint8_t*>(z_exponents)};
   return done(c, launch_activation_backward(type, act, samples, rows, dy, lddy, held, dz, lddz, dbias, accumulate != 0, c->workspace, c->slopes, c->stream),
@@ -184,6 +187,7 @@ int lqsgd_linear_input_grad(lqsgd_linear* c, int32_t type, int64_t samples, int3
   if (!dz || !w || !dx) return fail(c, LQSGD_EINVAL, kNull);
   const uintptr_t s = size_of(type);
   if (!aligned(dz, s) || !aligned(w, s) || !aligned(dx, s)) return fail(c, LQSGD_EINVAL, kBadAlign);
+  if (dx == dz || dx == w) return fail(c, LQSGD_EINVAL, kOver);
   ProductArgs a{};
   a.ni = cols; a.nj = samples; a.depth = rows;
   a.a = w; a.lda = ldw; a.b = dz; a.ldb = lddz;
@@ -201,6 +205,7 @@ int lqsgd_linear_weight_grad(lqsgd_linear* c, int32_t type, int64_t samples, int
   if (!dw || (samples > 0 && !dz)) return fail(c, LQSGD_EINVAL, kNull);
   if (samples > 0 && !codes_ok(x_codes, x_exponents, false)) return fail(c, LQSGD_EINVAL, kBadCodes);
   if (!aligned(dz, size_of(type)) || !aligned(dw, size_of(grad_type))) return fail(c, LQSGD_EINVAL, kBadAlign);
+  if (dw == dz) return fail(c, LQSGD_EINVAL, kOver);
   if (samples == 0 && accumulate) return LQSGD_OK;
   ProductArgs a{};
   a.ni = cols; a.nj = rows; a.depth = samples;

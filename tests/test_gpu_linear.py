@@ -565,4 +565,13 @@ def test_refusals(ops):
                       (dict(zc=c.codes.data_ptr()), B.EINVAL), (dict(zc=c.codes.data_ptr() + 8, ze=c.exponents.data_ptr()), B.EINVAL)):
         assert call(**bad) == code, bad
         assert L.lqsgd_linear_last_error(h).decode()
+    # outputs over inputs
+    square = f(8, 8)
+    refused(B.EINVAL, lambda: ops.forward(square, f(8, 8), out=square))
+    refused(B.EINVAL, lambda: ops.forward(f(8, 8), square, out=square))
+    refused(B.EINVAL, lambda: ops.input_grad(square, f(8, 8), out=square))
+    refused(B.EINVAL, lambda: ops.input_grad(f(8, 8), square, out=square))
+    refused(B.EINVAL, lambda: ops.weight_grad(square, B.Checkpoint.empty(8, 8), out=square))
+    wide = f(8, 16)
+    refused(B.EINVAL, lambda: ops.activation_backward(wide[:, :8], dz=wide.view(-1)[:64].view(8, 8)))
     ops.synchronize()
