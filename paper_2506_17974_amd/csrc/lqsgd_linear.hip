@@ -192,7 +192,7 @@ __device__ inline void pack_codes(uint32_t (&w)[N / 4], const float (&v)[N], flo
 // ---------------------------------------------------------------------------
 // A thread takes a piece of 8 consecutive values, four lanes a group; a workgroup a run of 256 pieces of the whole tensor, rows end to
 // end, so that narrow tensors fill their lanes too.  Bound by memory: s + 33/32 bytes per value (four pieces a thread on their way at
-// once: no faster, small tensors 2.8 -> 3.9 us).
+// once: no faster, small tensors 2.8 -> 3.9 us).  8192 x 4096 bf16 values: saving 18 us (5.6 TB/s), loading 16 (6.2).
 constexpr int kPiece = 8;
 
 template <typename T>
@@ -254,7 +254,8 @@ __device__ inline void times_tabled_slope(float (&d)[8], uint2 w, uint32_t byte,
 // A workgroup takes a strip of 8 << lanes_log2 features and a run of samples; a lane keeps 8 features' sums and has 4 samples on
 // their way.  Lanes that the strip does not fill take further samples.  Strips' sums over runs go to `part` (runs x rows) where
 // there is more than one run.  TABLE: gelu or silu of many samples, slopes from LDS (by their formulas, 27 instructions a value, the
-// vector units took 54 us for 4096 x 11008 bfloat16 values, whose memory traffic takes 32).
+// vector units took 54 us for 4096 x 11008 bfloat16 values; now 42, and 58 a pass where the tensors come from HBM, 4 TB/s: bound by
+// memory).
 template <typename T, bool TABLE>
 __global__ __launch_bounds__(256) void activation_backward_kernel(const T* dy, int64_t lddy, Codes z, T* dz, int64_t lddz, float* dbias,
                                                                   int accumulate, float* part, const float* slopes, int64_t samples,
@@ -338,6 +339,8 @@ __global__ __launch_bounds__(256) void sum_runs_kernel(const float* part, float*
 // ---------------------------------------------------------------------------
 // products
 // ---------------------------------------------------------------------------
+// 4096 x 11008 values with gelu and both checkpoints take 374 us with the product, 330 without all that: 45 vector instructions a
+// value, whose time no product hides (a CU holds one 256 x 256 tile).
 // The end of a product: v holds D[j][i0 .. i0 + N - 1], i0 a multiple of N, and neighbouring lanes the rest of the group of 32.  All
 // lanes of the wavefront come here together; `there` is false for those that have no row j.  N: 16 bytes of what is written.
 template <typename T, int PRODUCT> constexpr int kRun = std::is_same_v<T, float> || PRODUCT == kWeightGrad ? 4 : 8;
@@ -860,6 +863,16 @@ __device__ inline void add_parts(float (&v)[N], const ProductArgs& a, const Spli
   }
 }
 
+// A tile of D to a workgroup, operands through LDS in steps of BK.  What bounds it: 32 x 32 x 16 matrix instructions at 1024 flops a
+// cycle and SIMD, whose pipes are busy 49 (weight gradient) to 65 % (input gradient) of the time at 1.8 to 1.9 GHz -- the card lowers
+// its clock for them -- and what LDS
+// has to deliver to them, which is why a wavefront has as large a part of the tile as its registers hold (128 x 64: 6 reads of 1 KiB
+// to 8 products).  Measured, back to back, bfloat16 256 x 256: forward 4096 x 4096 -> 11008 322 us (1.15 PFLOP/s; the library's
+// product 402), input gradient 4096 x 11008 -> 4096 290 us (1.27 PFLOP/s; library 260), weight gradient of 8192 samples, 4096 x 4096,
+// decoding included, 246 us (1.12 PFLOP/s; library, from a decoded operand, 227).  fp32 256 x 128: input gradient 2048 x 8192 -> 8192
+// 1.36 ms (202 TFLOP/s of fp32, 1.2 PFLOP/s of its six bfloat16 products; the fp32 matrix instructions reach 153 in the library).
+// Tried: two buffers and a full wait at the barrier (input gradient 385 us), four wavefronts of 128 x 128 (the compiler spills 130
+// registers: 1.3 ms), wavefront priorities around the products (310 against 296), fp32 in steps of 16 (1.6 ms).
 template <typename T, int PRODUCT, typename S, bool DIRECT>
 __global__ __launch_bounds__(S::threads, S::threads >= 512 ? 2 : 1) void product_kernel(ProductArgs a, Split sp) {
   using O = Operands<T, PRODUCT, S::BI, S::BJ, S::BK, S::threads, DIRECT>;
@@ -979,8 +992,11 @@ __global__ __launch_bounds__(S::threads, S::threads >= 512 ? 2 : 1) void product
   }
 }
 
-// The same for few tiles: a workgroup's 8 wavefronts (4 of fp32) each have the whole tile and every 8th step of the sum, in LDS of
-// their own, so that nothing waits for another wavefront before the end, where the sums are added up in LDS in the wavefronts' order.
+// The same for few tiles, down to single tokens: a workgroup's 8 wavefronts each have the whole tile and every 8th step of the sum, in
+// LDS of their own, so that nothing waits for another wavefront before the end, where the sums are added up in LDS in the wavefronts'
+// order.  Bound by the latency of a step (1.0 to 1.6 us for 8 x 64 values of r in 16-bit types, 1.7 for 8 x 16 in fp32, where
+// splitting takes as long as multiplying) and, for single tokens, by the weights' stream: 4096 -> 11008 bf16 17 us, 5.3 TB/s, where a
+// tile of 128 x 128 takes 40.  1024 x 1024 x 1024 bf16 8 us, fp32 21.  Two steps on their way, half as long each: 10 and 24 us.
 template <typename T, int PRODUCT, int BI, int BJ, int BK, int WAVES, bool DIRECT>
 __global__ __launch_bounds__(WAVES * 64) void product_by_depth_kernel(ProductArgs a, Split sp) {
   using O = Operands<T, PRODUCT, BI, BJ, BK, 64, DIRECT>;
