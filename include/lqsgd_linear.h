@@ -16,7 +16,7 @@
  *   q = v / 2^e rounded to nearest, ties to even, -127 <= q <= 127; it stands for q 2^e.  e is the smallest integer for which the
  *   group's largest magnitude is below 127.5 * 2^e, held to -126..121 (LQSGD_TYPE_F16: -24..9), so that every q 2^e is a number of
  *   the type it was saved from and reading a checkpoint back rounds nothing: |v - q 2^e| <= 2^e / 2, except where the upper bound
- *   of e takes effect (up to 2^e there).  A group that holds a NaN or an infinity is kept as NaN in all its values.
+ *   of e takes effect (up to 2^e there; a z beyond half's range is kept as 127 2^9).  A group that holds a NaN or an infinity is kept as NaN in all its values.
  *     codes      : int8, samples x lqsgd_checkpoint_stride(features), 16-byte aligned; the codes behind the last feature are 0
  *     exponents  : uint8, samples x lqsgd_checkpoint_stride(features) / 32: e + 127, or 255 for NaN
  *
@@ -30,8 +30,8 @@
  *     pointer, same ld).  An output at an input's address otherwise is refused (EINVAL).
  *   - Results are the same bits from run to run: nothing is added in an order that depends on timing.
  *   - NaN and infinities go the way of the formulas, with two exceptions.  LQSGD_TYPE_F32 products are made from operands split
- *     into three bfloat16 terms: an infinite operand may make the outputs it reaches NaN instead of infinite.  A checkpoint reads
- *     back as above.
+ *     into three bfloat16 terms: an infinite operand may make the outputs it reaches NaN instead of infinite, and operands are taken
+ *     to multiples of 2^-133 (magnitudes below 2^-109 lose their last bits).  A checkpoint reads back as above.
  *   - A call only enqueues kernels on the context's stream (it may be captured into a HIP graph); it neither allocates nor waits.
  */
 #ifndef LQSGD_LINEAR_H

@@ -260,6 +260,19 @@ def test_forward_of_values_that_are_not_finite(ops, kind, shape):
         assert not torch.isfinite(y[:, 7]).any() and torch.isfinite(y[:, rest]).all()
 
 
+@pytest.mark.parametrize("scale_x,scale_w", [(3.4e38, 1e-30), (1e-30, 1e30), (2.0 ** -112, 1e30), (2.0 ** -130, 1e35)])
+def test_fp32_operands_of_any_size(ops, scale_x, scale_w):
+    """The three terms of an fp32 operand reach from the largest numbers to multiples of 2^-133."""
+    _say("sizes", scale_x, scale_w)
+    rng = np.random.default_rng(23)
+    x, xv = _put((rng.random((70, 96)) * 0.5 + 0.5) * scale_x, "f32")
+    w, wv = _put(rng.standard_normal((80, 96)) * scale_w, "f32")
+    want = xv @ wv.T
+    tol = _sum_bound(xv, wv.T, 96) + 2.0 ** -133 * np.abs(wv).sum(1) + HALF_ULP["f32"][0] * np.abs(want)
+    _close(ops.forward(x, w), want, tol, "y")
+    _close(ops.input_grad(x, w.t().contiguous()), want, tol, "dx")
+
+
 # ---------------------------------------------------------------------------
 # backward
 # ---------------------------------------------------------------------------
