@@ -402,6 +402,7 @@ class Checkpoint:
 
     @classmethod
     def empty(cls, samples, features, device="cuda"):
+        """One whose values are yet to be written."""
         import torch
         self = cls(None, None, features)
         groups = -(-self.features // CHECKPOINT_GROUP)

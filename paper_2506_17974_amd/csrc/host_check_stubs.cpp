@@ -26,7 +26,7 @@ namespace linear {
 hipError_t launch_product(int, int, const ProductArgs&, hipStream_t) { return hipErrorNotSupported; }
 hipError_t launch_checkpoint_save(int, int64_t, int32_t, const void*, int64_t, Codes, hipStream_t) { return hipErrorNotSupported; }
 hipError_t launch_checkpoint_load(int, int64_t, int32_t, Codes, void*, int64_t, hipStream_t) { return hipErrorNotSupported; }
-hipError_t launch_slopes(float*, hipStream_t) { return hipErrorNotSupported; }
+hipError_t launch_prepare(float*, int*, hipStream_t) { return hipErrorNotSupported; }
 hipError_t launch_activation_backward(int, int, int64_t, int32_t, const void*, int64_t, Codes, void*, int64_t, float*, int, void*, const float*,
                                       hipStream_t) {
   return hipErrorNotSupported;

@@ -230,8 +230,12 @@ __global__ __launch_bounds__(256) void checkpoint_load_kernel(T* x, int64_t ldx,
 constexpr int kSlopeRows = 36, kSlopes = kSlopeRows * 128, kSlopeLow = -30;
 static_assert(2 * kSlopes == kSlopeFloats);
 
-__global__ __launch_bounds__(256) void slopes_kernel(float* table) {
+static_assert(kTiles <= kSlopeFloats);
+
+// What a context's memory has to hold before its first call: the slopes, and no part of any tile's sum.
+__global__ __launch_bounds__(256) void prepare_kernel(float* table, int* arrived) {
   const int at = (int)blockIdx.x * 256 + threadIdx.x;              // gelu's, then silu's
+  if (at < kTiles) arrived[at] = 0;
   const int act = at < kSlopes ? kGelu : kSilu, in = at % kSlopes;
   const float z[1] = {(float)(in & 127) * power_of_two(kSlopeLow + (in >> 7))};
   float d[1] = {1.f};
@@ -1272,8 +1276,8 @@ hipError_t launch_checkpoint_load(int type, int64_t samples, int32_t features, C
   });
 }
 
-hipError_t launch_slopes(float* slopes, hipStream_t s) {
-  slopes_kernel<<<dim3(kSlopeFloats / 256), 256, 0, s>>>(slopes);
+hipError_t launch_prepare(float* slopes, int* arrived, hipStream_t s) {
+  prepare_kernel<<<dim3(kSlopeFloats / 256), 256, 0, s>>>(slopes, arrived);
   return hipGetLastError();
 }
 

@@ -76,8 +76,7 @@ int lqsgd_linear_create(void* hip_stream, lqsgd_linear** out) {
   }
   c->arrived = reinterpret_cast<int*>(static_cast<char*>(c->workspace) + kWorkspaceBytes);
   c->slopes = reinterpret_cast<float*>(c->arrived + kTiles);
-  e = hipMemsetAsync(c->arrived, 0, kTiles * sizeof(int), c->stream);
-  if (e == hipSuccess) e = launch_slopes(c->slopes, c->stream);
+  e = launch_prepare(c->slopes, c->arrived, c->stream);
   if (e != hipSuccess) {
     (void)hipFree(c->workspace);
     delete c;

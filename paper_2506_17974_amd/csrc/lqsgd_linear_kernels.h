@@ -49,7 +49,7 @@ hipError_t launch_checkpoint_save(int type, int64_t samples, int32_t features, c
 hipError_t launch_checkpoint_load(int type, int64_t samples, int32_t features, Codes c, void* x, int64_t ldx, hipStream_t s);
 hipError_t launch_activation_backward(int type, int act, int64_t samples, int32_t rows, const void* dy, int64_t lddy, Codes z, void* dz,
                                       int64_t lddz, float* dbias, int accumulate, void* workspace, const float* slopes, hipStream_t s);
-hipError_t launch_slopes(float* slopes, hipStream_t s);       // kSlopeFloats of them, once for a context
+hipError_t launch_prepare(float* slopes, int* arrived, hipStream_t s);       // kSlopeFloats and kTiles of them, once for a context
 
 }  // namespace linear
 }  // namespace lqsgd
