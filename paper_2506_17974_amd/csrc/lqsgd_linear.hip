@@ -86,6 +86,16 @@ __device__ inline float normal_cdf(float z, float* density) {
 }
 __device__ inline float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950408889634f * z)); }
 
+// act'(z) of silu = s (1 + z (1 - s)), s = sigmoid(z), at -|z|, and 1 less that for z > 0: no difference of nearly equal numbers, so that the
+// slope is right relative to its size where it goes to 0 and to a few units in the last place where it goes to 1 (from s itself z (1 - s)
+// is off by z units).  exp(-|z|) as the square of its root: what is left of z exp(z) where exp(z) itself is below the floats stays.
+__device__ inline float silu_slope(float z) {
+  const float x = fabsf(z), root = __builtin_amdgcn_exp2f(-0.72134752044448170f * x);
+  const float c = __builtin_amdgcn_rcpf(fmaf(root, root, 1.f));           // 1 - s
+  const float t = root * (c * fmaf(-x, c, 1.f)) * root;
+  return z > 0.f ? 1.f - t : t;
+}
+
 // One branch for all values: which activation it is, is the same for the whole launch.
 template <int N>
 __device__ inline void activate_all(float (&v)[N], int act) {
@@ -118,10 +128,7 @@ __device__ inline void times_slope(float (&d)[N], const float (&z)[N], int act) 
     }
   } else if (act == kSilu) {
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
-      const float s = sigmoid(z[k]);
-      d[k] *= s * fmaf(z[k], 1.f - s, 1.f);
-    }
+    for (int k = 0; k < N; ++k) d[k] *= silu_slope(z[k]);
   }
 }
 
@@ -225,33 +232,32 @@ __global__ __launch_bounds__(256) void checkpoint_load_kernel(T* x, int64_t ldx,
 // ---------------------------------------------------------------------------
 // activation backward
 // ---------------------------------------------------------------------------
-// Slopes as a table: act'(z) for z = |q| 2^e has 128 values an exponent, and act'(-z) = 1 - act'(z) for gelu and silu.  Rows e = -30
-// (below, z is under 2^-23 and the slope 1/2) to 5 (above, it is 0 or 1 to 2^-24 but for q = 0), each entry act'(z) - 1/2.
-constexpr int kSlopeRows = 36, kSlopes = kSlopeRows * 128, kSlopeLow = -30;
-static_assert(2 * kSlopes == kSlopeFloats);
-
-static_assert(kTiles <= kSlopeFloats);
+// Slopes as a table: z = |q| 2^e has 128 values an exponent, and act'(z) = 1 - act'(-z) for gelu and silu.  Entries are act'(-|z|), so
+// that the slopes that go to 0 are held to a float's relative precision, as the formula has them.  Rows e = -32 (below, z is under 2^-25
+// and the slope 1/2 to half a unit in its last place) to 7 (above, the slope is 0 or 1 for every |q| >= 1).
+constexpr int kSlopes = kSlopeRows * 128, kSlopeLow = -32;
+static_assert(kTiles <= kSlopeFloats && kSlopeFloats % 256 == 0);
 
 // What a context's memory has to hold before its first call: the slopes, and no part of any tile's sum.
 __global__ __launch_bounds__(256) void prepare_kernel(float* table, int* arrived) {
   const int at = (int)blockIdx.x * 256 + threadIdx.x;              // gelu's, then silu's
   if (at < kTiles) arrived[at] = 0;
   const int act = at < kSlopes ? kGelu : kSilu, in = at % kSlopes;
-  const float z[1] = {(float)(in & 127) * power_of_two(kSlopeLow + (in >> 7))};
+  const float z[1] = {-(float)(in & 127) * power_of_two(kSlopeLow + (in >> 7))};
   float d[1] = {1.f};
   times_slope(d, z, act);
-  table[at] = d[0] - 0.5f;
+  table[at] = d[0];
 }
 
 // d *= act'(z) of 8 codes of a group.
 __device__ inline void times_tabled_slope(float (&d)[8], uint2 w, uint32_t byte, const float* table) {
   const float* row = table + min(max((int)byte - 127 - kSlopeLow, 0), kSlopeRows - 1) * 128;
-  const float half = byte == 255u ? __builtin_nanf("") : 0.5f;
+  const float zero = byte == 255u ? __builtin_nanf("") : 0.f, one = byte == 255u ? __builtin_nanf("") : 1.f;
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     const int q = (int8_t)((k < 4 ? w.x : w.y) >> (8 * (k & 3)));
-    const float s = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, row[abs(q) & 127]) ^ ((uint32_t)q & 0x80000000u));
-    d[k] *= s + half;
+    const float t = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, row[abs(q) & 127]) ^ (~(uint32_t)q & 0x80000000u));
+    d[k] *= (q < 0 ? zero : one) + t;
   }
 }
 

@@ -11,7 +11,8 @@ namespace linear {
 
 constexpr int kGroup = 32;                        // features that share an exponent in a checkpoint
 constexpr size_t kWorkspaceBytes = 64ull << 20;   // sums of parts, at most
-constexpr int kSlopeFloats = 2 * 36 * 128;        // slopes of gelu and silu for every code and exponent that needs one
+constexpr int kSlopeRows = 40;                    // exponents whose codes' slopes are not all 1/2, or 0 and 1
+constexpr int kSlopeFloats = 2 * kSlopeRows * 128;       // slopes of gelu and silu for every code of those
 constexpr int kTiles = 8192;                      // tiles whose sum is in parts, at most (64 x 32, two parts)
 
 enum Type { kF32 = 0, kBF16 = 1, kF16 = 2 };
