@@ -58,7 +58,8 @@ typedef struct lqsgd_linear lqsgd_linear;
 
 #define LQSGD_LINEAR_MAX_FEATURES (1 << 20)  /* rows, cols              */
 #define LQSGD_LINEAR_MAX_STRIDE (1 << 21)    /* ld*, in elements        */
-#define LQSGD_LINEAR_MAX_SAMPLES (1 << 30)
+#define LQSGD_LINEAR_MAX_SAMPLES (1 << 30)       /* and an output of forward, input_grad or weight_grad that is longer than 2^36
+                                                     values may be refused (ESHAPE) */
 
 /* A context on the current HIP device: the stream its calls run on (a hipStream_t, NULL = the default stream) and 64 MiB of
  * workspace, which the calls share: work of one context is ordered by its stream.  Not thread-safe.  Errors: EINVAL, ENOMEM, EHIP. */

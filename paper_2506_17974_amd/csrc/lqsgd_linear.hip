@@ -3,6 +3,7 @@
 //
 // Sums have a fixed order: results are bit-identical run to run.
 #include "lqsgd_linear_kernels.h"
+#include "lqsgd_linear_plan.h"
 
 #include <algorithm>
 #include <cstdint>
@@ -706,12 +707,6 @@ __device__ inline Where where(int tiles_i, int tiles_j, int tiles, int splits) {
   return Where{in / high, band * kBand + in % high, split};
 }
 
-// A tile's sum in `splits` parts.
-struct Split {
-  int tiles_i, tiles_j, splits;
-  int64_t steps;         // values of r of a split, a multiple of BK
-};
-
 // Types and operands of a product whose workgroups (or wavefronts: THREADS = 64) have a tile of BI x BJ, BK deep.
 template <typename T, int PRODUCT, int BI, int BJ, int BK, int THREADS, bool DIRECT>
 struct Operands {
@@ -1125,59 +1120,6 @@ __global__ __launch_bounds__(256) void join_kernel(ProductArgs a, Split sp) {
   finish<T, PRODUCT>(v, bias, a, j, i, j < a.nj);
 }
 
-// ---- which kernel a product takes ----
-// Three kernels serve a product: by depth (64 x 64 tiles, the sum shared out among a workgroup's wavefronts), 128 x 128 tiles and
-// the largest ones, each with the sum whole or in parts that are added up at the end.  The one with the least expected time is taken:
-//   1.5 us + turns (turn + steps (step + more w)) + [parts > 1] (4 us + what the join writes and reads at 4.5 TB/s)
-// for `turns` rounds of 256 workgroups of `steps` steps each and w = the share of the CUs that have one; by depth, where one workgroup
-// adds up a tile, 0.35 us a part more.  The figures are fits to the three kernels' times over 120 products from 64 x 1024 x 64 to
-// 8192 x 2048 x 1024 in bfloat16 and fp32; taken by them the products cost 2 % more than each one's best.  E.g. (bf16,
-// ni x nj x depth: by depth / 128 x 128 / 256 x 256) 1024 x 1024 x 1024 8 / 16 / 29 us, 2048 x 2048 x 2048 39 / 28 / 50,
-// 4096 x 4096 x 512 72 / 28 / 23; fp32 512 x 4096 x 4096 139 / 240 / 283, in 4 parts by the last 100.
-struct Rate { float turn, step, more; };
-enum Kernel { kByDepth = 0, kMiddle = 1, kLarge = 2 };
-struct Plan {
-  Kernel kernel;
-  Split sp;
-  int64_t tiles;
-};
-struct Geometry { int bi, bj, step; };
-
-template <typename T, int PRODUCT, bool DIRECT>
-Plan plan(const ProductArgs& a) {
-  constexpr bool kWide = std::is_same_v<T, float>, kGrad = PRODUCT == kWeightGrad;
-  constexpr Rate rates[3] = {kWide ? kGrad ? Rate{2.8f, 1.15f, .2f} : Rate{3.2f, 1.65f, .35f}
-                             : DIRECT ? kGrad ? Rate{3.6f, 1.5f, .35f} : Rate{3.4f, 1.f, .45f} : Rate{3.6f, 2.2f, .6f},
-                             kWide ? kGrad ? Rate{6.f, 1.35f, .05f} : Rate{8.f, 1.85f, .05f}
-                             : DIRECT ? kGrad ? Rate{4.f, .58f, .12f} : Rate{2.8f, .34f, 0.f} : Rate{5.f, .9f, .1f},
-                             kWide ? kGrad ? Rate{6.5f, 1.36f, .1f} : Rate{8.f, 2.f, .5f}
-                             : DIRECT ? kGrad ? Rate{9.f, .78f, .22f} : Rate{9.f, .62f, .25f} : Rate{8.f, .8f, .1f}};
-  const Geometry shapes[3] = {{64, a.nj <= 32 ? 32 : 64, kWide ? a.nj <= 32 ? 256 : 128 : 512}, {128, 128, 32}, {256, !kWide && DIRECT ? 256 : 128, 32}};
-  Plan best{};
-  float least = 0.f;
-  for (int k = 0; k < 3; ++k) {
-    const Geometry& g = shapes[k];
-    const int64_t ti = (a.ni + g.bi - 1) / g.bi, tj = (a.nj + g.bj - 1) / g.bj, tiles = ti * tj, steps = (a.depth + g.step - 1) / g.step;
-    const int64_t fit = (int64_t)(kWorkspaceBytes / (sizeof(float) * g.bi * g.bj)) / tiles;
-    for (int64_t parts = 1; parts <= 16; ++parts) {
-      if (parts > 1 && (parts > steps || parts > fit)) break;
-      const int64_t per = parts > 1 ? (steps + parts - 1) / parts : steps;
-      if (parts > 1 && (steps + per - 1) / per != parts) continue;         // as many steps a part as with fewer parts
-      const int64_t groups = tiles * parts, turns = (groups + 255) / 256;
-      const Rate& r = rates[k];
-      float us = 1.5f + (float)turns * (r.turn + (float)per * (r.step + r.more * std::min(1.f, (float)groups / 256.f)));
-      if (parts > 1) us += 4.f + 4e-6f / 4.5f * (float)(groups * g.bi * g.bj) + (k == kByDepth ? .35f * (float)parts : 0.f);
-      if (k + parts == 1 || us < least) {
-        least = us;
-        best.kernel = (Kernel)k;
-        best.sp = Split{(int)ti, (int)std::min<int64_t>(tj, INT32_MAX), (int)parts, std::max<int64_t>(1, per) * g.step};
-        best.tiles = tiles;
-      }
-    }
-  }
-  return best;
-}
-
 template <typename T, int PRODUCT, typename P, int BI, int BJ>
 hipError_t join(const ProductArgs& a, const Plan& p, hipStream_t s) {
   static_assert(P::pieces % 4 == 0);
@@ -1205,8 +1147,8 @@ bool whole_chunks(const void* p, int64_t ld, int64_t length) {
 
 template <typename T, int PRODUCT, bool DIRECT>
 hipError_t by_size(const ProductArgs& a, hipStream_t s) {
-  const Plan p = plan<T, PRODUCT, DIRECT>(a);
-  if (p.tiles * p.sp.splits >= (int64_t(1) << 32) / 512) return hipErrorInvalidValue;      // threads of a launch: 2^32
+  const Plan p = plan_product(PRODUCT, std::is_same_v<T, float>, DIRECT, a.ni, a.nj, a.depth);
+  if (p.tiles == 0) return hipErrorInvalidValue;
   if constexpr (std::is_same_v<T, float>) {
     if (p.kernel == kLarge) return run_product<T, PRODUCT, Shape<256, 128, 4, 2, 32, 2>, DIRECT>(a, p, s);
     if (p.kernel == kMiddle) return run_product<T, PRODUCT, Shape<128, 128, 2, 2, 32, 2>, DIRECT>(a, p, s);

@@ -44,6 +44,9 @@ uintptr_t size_of(int32_t t) { return t == LQSGD_TYPE_F32 ? 4 : 2; }
 bool aligned(const void* p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 bool features_ok(int32_t n) { return n >= 1 && n <= LQSGD_LINEAR_MAX_FEATURES; }
 bool samples_ok(int64_t n) { return n >= 0 && n <= LQSGD_LINEAR_MAX_SAMPLES; }
+// An output of ni x nj values that the kernels of 128 x 128 tiles can be launched for (of any shape up to 2^36 values): as many threads
+// as one launch has.
+bool output_ok(int64_t ni, int64_t nj) { return ((ni + 127) / 128) * ((nj + 127) / 128) * 256 < int64_t(1) << 32; }
 bool stride_ok(int64_t ld, int32_t n) { return ld >= n && ld <= LQSGD_LINEAR_MAX_STRIDE; }
 // A checkpoint's two pointers: both or neither (neither only if it is optional).
 bool codes_ok(const void* codes, const void* exponents, bool optional) {
@@ -139,6 +142,7 @@ int lqsgd_linear_forward(lqsgd_linear* c, int32_t type, int32_t act, int64_t sam
   if (!samples_ok(samples) || !features_ok(rows) || !features_ok(cols) || !stride_ok(ldx, cols) || !stride_ok(ldw, cols) ||
       !stride_ok(ldy, rows) || (residual && !stride_ok(ldr, rows)))
     return fail(c, LQSGD_ESHAPE, kBadSize);
+  if (!output_ok(rows, samples)) return fail(c, LQSGD_ESHAPE, kBadSize);
   if (samples == 0) return LQSGD_OK;
   if (!x || !w || !y) return fail(c, LQSGD_EINVAL, kNull);
   const uintptr_t s = size_of(type);
@@ -182,6 +186,7 @@ int lqsgd_linear_input_grad(lqsgd_linear* c, int32_t type, int64_t samples, int3
   if (!samples_ok(samples) || !features_ok(rows) || !features_ok(cols) || !stride_ok(lddz, rows) || !stride_ok(ldw, cols) ||
       !stride_ok(lddx, cols))
     return fail(c, LQSGD_ESHAPE, kBadSize);
+  if (!output_ok(cols, samples)) return fail(c, LQSGD_ESHAPE, kBadSize);
   if (samples == 0) return LQSGD_OK;
   if (!dz || !w || !dx) return fail(c, LQSGD_EINVAL, kNull);
   const uintptr_t s = size_of(type);
@@ -201,6 +206,7 @@ int lqsgd_linear_weight_grad(lqsgd_linear* c, int32_t type, int64_t samples, int
   if (!known_type(type) || (grad_type != LQSGD_TYPE_F32 && grad_type != LQSGD_TYPE_BF16)) return fail(c, LQSGD_EINVAL, kBadType);
   if (!samples_ok(samples) || !features_ok(rows) || !features_ok(cols) || !stride_ok(lddz, rows) || !stride_ok(lddw, cols))
     return fail(c, LQSGD_ESHAPE, kBadSize);
+  if (!output_ok(cols, rows)) return fail(c, LQSGD_ESHAPE, kBadSize);
   if (!dw || (samples > 0 && !dz)) return fail(c, LQSGD_EINVAL, kNull);
   if (samples > 0 && !codes_ok(x_codes, x_exponents, false)) return fail(c, LQSGD_EINVAL, kBadCodes);
   if (!aligned(dz, size_of(type)) || !aligned(dw, size_of(grad_type))) return fail(c, LQSGD_EINVAL, kBadAlign);

@@ -6,14 +6,14 @@
 #include <cstddef>
 #include <cstdint>
 
+#include "lqsgd_linear_plan.h"
+
 namespace lqsgd {
 namespace linear {
 
 constexpr int kGroup = 32;                        // features that share an exponent in a checkpoint
-constexpr size_t kWorkspaceBytes = 64ull << 20;   // sums of parts, at most
 constexpr int kSlopeRows = 40;                    // exponents whose codes' slopes are not all 1/2, or 0 and 1
 constexpr int kSlopeFloats = 2 * kSlopeRows * 128;       // slopes of gelu and silu for every code of those
-constexpr int kTiles = 8192;                      // tiles whose sum is in parts, at most (64 x 32, two parts)
 
 enum Type { kF32 = 0, kBF16 = 1, kF16 = 2 };
 enum Act { kNone = 0, kRelu = 1, kGelu = 2, kSilu = 3 };
@@ -23,13 +23,7 @@ struct Codes {                                    // a checkpoint's memory; code
   uint8_t* exponents;
 };
 
-// A product D[j][i] = sum over r < depth of A[i][r] B[j][r], i < ni contiguous in the output's rows, j < nj its rows:
-//   forward       i = output feature  A = w    (r contiguous)   j = sample          B = x  (r contiguous)   r = input feature
-//   input grad    i = input feature   A = w    (i contiguous)   j = sample          B = dz (r contiguous)   r = output feature
-//   weight grad   i = input feature   A = x^   (i contiguous)   j = output feature  B = dz (j contiguous)   r = sample
-enum Product { kForward = 0, kInputGrad = 1, kWeightGrad = 2 };
-
-struct ProductArgs {
+struct ProductArgs {                              // sizes as in lqsgd_linear_plan.h
   int64_t nj, depth;
   int32_t ni;
   const void* a; int64_t lda;                     // kWeightGrad: unused, the operand is `held`
