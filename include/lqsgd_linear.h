@@ -27,7 +27,8 @@
  *     fp32, bias, activation, residual and sums are fp32, and each output is rounded once (to nearest even).
  *   - samples may be 0: nothing is written then, except that sums over no samples are 0.
  *   - Outputs must not overlap inputs or each other, with two exceptions: y may be the residual itself and dz may be dy itself (same
- *     pointer, same ld).  An output at an input's address otherwise is refused (EINVAL).
+ *     pointer, same ld).  An output that starts where an input or another output does is refused otherwise (EINVAL; checkpoints' codes and
+ *     exponents are inputs and outputs too); an overlap of another kind is not looked for.
  *   - Results are the same bits from run to run: nothing is added in an order that depends on timing.
  *   - NaN and infinities go the way of the formulas, with two exceptions.  LQSGD_TYPE_F32 products are made from operands split
  *     into three bfloat16 terms: an infinite operand may make the outputs it reaches NaN instead of infinite, and operands are taken
@@ -76,7 +77,7 @@ int64_t lqsgd_checkpoint_stride(int32_t features);
 
 /* x (samples x features, of `type`) into a checkpoint, and back; loading into a type other than the one it was saved from rounds
  * to nearest.  Errors of these and of the calls below: EINVAL (NULL, unknown type or activation, pointers that are not aligned to
- * their type, codes not aligned to 16 bytes, an output at an input's address), ESHAPE (sizes or strides out of range), EHIP. */
+ * their type, codes not aligned to 16 bytes, an output at the address of an input or another output), ESHAPE (sizes or strides out of range), EHIP. */
 int lqsgd_checkpoint_save(lqsgd_linear* ctx, int32_t type, int64_t samples, int32_t features, const void* x, int64_t ldx,
                           int8_t* codes, uint8_t* exponents);
 int lqsgd_checkpoint_load(lqsgd_linear* ctx, int32_t type, int64_t samples, int32_t features, const int8_t* codes,

@@ -3,6 +3,7 @@
 
 #include <cstdint>
 #include <cstdio>
+#include <initializer_list>
 #include <new>
 #include <string>
 
@@ -54,11 +55,23 @@ bool codes_ok(const void* codes, const void* exponents, bool optional) {
   return aligned(codes, 16);
 }
 
+// Whether an output starts where an input or another output does (NULL: not there).
+bool lies_over(std::initializer_list<const void*> outputs, std::initializer_list<const void*> inputs) {
+  for (auto o = outputs.begin(); o != outputs.end(); ++o) {
+    if (!*o) continue;
+    for (const void* i : inputs)
+      if (*o == i) return true;
+    for (auto p = o + 1; p != outputs.end(); ++p)
+      if (*o == *p) return true;
+  }
+  return false;
+}
+
 constexpr const char kNull[] = "a pointer that is needed is NULL";
 constexpr const char kBadType[] = "unknown type or activation";
 constexpr const char kBadSize[] = "samples, features or a stride out of range";
 constexpr const char kBadAlign[] = "a pointer is not aligned to its type";
-constexpr const char kOver[] = "an output lies over an input";
+constexpr const char kOver[] = "an output lies over an input or another output";
 constexpr const char kBadCodes[] = "a checkpoint needs both of its pointers, and codes aligned to 16 bytes";
 
 }  // namespace
@@ -118,6 +131,7 @@ int lqsgd_checkpoint_save(lqsgd_linear* c, int32_t type, int64_t samples, int32_
   if (!x) return fail(c, LQSGD_EINVAL, kNull);
   if (!aligned(x, size_of(type))) return fail(c, LQSGD_EINVAL, kBadAlign);
   if (!codes_ok(codes, exponents, false)) return fail(c, LQSGD_EINVAL, kBadCodes);
+  if (lies_over({codes, exponents}, {x})) return fail(c, LQSGD_EINVAL, kOver);
   return done(c, launch_checkpoint_save(type, samples, features, x, ldx, Codes{codes, exponents}, c->stream), "lqsgd_checkpoint_save");
 }
 
@@ -130,6 +144,7 @@ int lqsgd_checkpoint_load(lqsgd_linear* c, int32_t type, int64_t samples, int32_
   if (!x) return fail(c, LQSGD_EINVAL, kNull);
   if (!aligned(x, size_of(type))) return fail(c, LQSGD_EINVAL, kBadAlign);
   if (!codes_ok(codes, exponents, false)) return fail(c, LQSGD_EINVAL, kBadCodes);
+  if (lies_over({x}, {codes, exponents})) return fail(c, LQSGD_EINVAL, kOver);
   const Codes held{const_cast<int8_t*>(codes), const_cast<uint8_t*>(exponents)};
   return done(c, launch_checkpoint_load(type, samples, features, held, x, ldx, c->stream), "lqsgd_checkpoint_load");
 }
@@ -148,7 +163,9 @@ int lqsgd_linear_forward(lqsgd_linear* c, int32_t type, int32_t act, int64_t sam
   const uintptr_t s = size_of(type);
   if (!aligned(x, s) || !aligned(w, s) || !aligned(bias, s) || !aligned(residual, s) || !aligned(y, s)) return fail(c, LQSGD_EINVAL, kBadAlign);
   if (!codes_ok(z_codes, z_exponents, true) || !codes_ok(y_codes, y_exponents, true)) return fail(c, LQSGD_EINVAL, kBadCodes);
-  if (y == x || y == w || y == bias) return fail(c, LQSGD_EINVAL, kOver);
+  if (lies_over({y, z_codes, z_exponents, y_codes, y_exponents}, {x, w, bias}) ||
+      lies_over({z_codes, z_exponents, y_codes, y_exponents}, {residual}))
+    return fail(c, LQSGD_EINVAL, kOver);
   if (residual == y && ldr != ldy) return fail(c, LQSGD_EINVAL, "y is the residual, with another stride");
   ProductArgs a{};
   a.ni = rows; a.nj = samples; a.depth = cols;
@@ -172,6 +189,11 @@ int lqsgd_linear_activation_backward(lqsgd_linear* c, int32_t type, int32_t act,
     if (!codes_ok(z_codes, z_exponents, act == LQSGD_ACT_NONE)) return fail(c, LQSGD_EINVAL, kBadCodes);
   }
   if (!aligned(dy, size_of(type)) || !aligned(dz, size_of(type)) || !aligned(dbias, 4)) return fail(c, LQSGD_EINVAL, kBadAlign);
+  if (samples > 0) {
+    const bool reads_z = act != LQSGD_ACT_NONE;
+    if (lies_over({dz, dbias}, {reads_z ? z_codes : nullptr, reads_z ? z_exponents : nullptr}) || lies_over({dbias}, {dy}))
+      return fail(c, LQSGD_EINVAL, kOver);
+  }
   if (dz == dy && dz && lddz != lddy) return fail(c, LQSGD_EINVAL, "dz is dy, with another stride");
   if (samples == 0 && !dbias) return LQSGD_OK;
   const Codes held{const_cast<int8_t*>(z_codes), const_cast<uint8_t*>(z_exponents)};
@@ -191,7 +213,7 @@ int lqsgd_linear_input_grad(lqsgd_linear* c, int32_t type, int64_t samples, int3
   if (!dz || !w || !dx) return fail(c, LQSGD_EINVAL, kNull);
   const uintptr_t s = size_of(type);
   if (!aligned(dz, s) || !aligned(w, s) || !aligned(dx, s)) return fail(c, LQSGD_EINVAL, kBadAlign);
-  if (dx == dz || dx == w) return fail(c, LQSGD_EINVAL, kOver);
+  if (lies_over({dx}, {dz, w})) return fail(c, LQSGD_EINVAL, kOver);
   ProductArgs a{};
   a.ni = cols; a.nj = samples; a.depth = rows;
   a.a = w; a.lda = ldw; a.b = dz; a.ldb = lddz;
@@ -210,7 +232,7 @@ int lqsgd_linear_weight_grad(lqsgd_linear* c, int32_t type, int64_t samples, int
   if (!dw || (samples > 0 && !dz)) return fail(c, LQSGD_EINVAL, kNull);
   if (samples > 0 && !codes_ok(x_codes, x_exponents, false)) return fail(c, LQSGD_EINVAL, kBadCodes);
   if (!aligned(dz, size_of(type)) || !aligned(dw, size_of(grad_type))) return fail(c, LQSGD_EINVAL, kBadAlign);
-  if (dw == dz) return fail(c, LQSGD_EINVAL, kOver);
+  if (lies_over({dw}, {dz, x_codes, x_exponents})) return fail(c, LQSGD_EINVAL, kOver);
   if (samples == 0 && accumulate) return LQSGD_OK;
   ProductArgs a{};
   a.ni = cols; a.nj = rows; a.depth = samples;
