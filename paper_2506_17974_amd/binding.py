@@ -440,11 +440,40 @@ class Checkpoint:
         return self.samples * -(-self.features // CHECKPOINT_GROUP) * (CHECKPOINT_GROUP + 1)
 
 
+_no_backward = None
+
+
+def _without_autograd(out, *inputs):
+    """`out`, a result that was just made from `inputs`.  Where autograd records and one of them has to have a gradient, `out` becomes
+    part of the graph with a backward pass that raises: the gradient is not left out in silence."""
+    global _no_backward
+    import torch
+    if not torch.is_grad_enabled() or not any(t is not None and t.requires_grad for t in inputs):
+        return out
+    if _no_backward is None:
+        class NoBackward(torch.autograd.Function):
+            @staticmethod
+            def forward(ctx, out, *inputs):
+                ctx.mark_dirty(out)
+                return out
+
+            @staticmethod
+            def backward(ctx, *grads):
+                raise LqsgdError(EINVAL, "autograd does not pass through the linear layer's calls: their gradients are made by "
+                                         "activation_backward, input_grad and weight_grad")
+        _no_backward = NoBackward
+    return _no_backward.apply(out, *inputs)
+
+
 class LinearOps:
     """One lqsgd_linear context: the forward and backward passes of linear layers on torch CUDA tensors (float32, bfloat16 or float16;
     two-dimensional, the elements of a row contiguous, rows at any stride).  Every call checks shapes, types and devices on the host
     and enqueues kernels on the stream that was current at construction; it raises where another stream is current, since the outputs
-    that it allocates would belong to that one.  Tensors made on other streams are the caller's to order, as with torch's own calls."""
+    that it allocates would belong to that one.  Tensors made on other streams are the caller's to order, as with torch's own calls.
+
+    The calls are a layer's passes, made by hand; autograd does not go through them.  A new tensor that a call returns, made from tensors that
+    require a gradient while autograd records, raises where a backward() reaches it.  Checkpoints, and tensors given for the
+    results, are plain memory: nothing is recorded for those."""
 
     def __init__(self):
         import torch
@@ -569,6 +598,7 @@ class LinearOps:
         if act not in ACTS:
             raise LqsgdError(EINVAL, "unknown activation %r" % (act,))
         b = self._vector("bias", bias, T, n) if bias is not None else None
+        new = out is None
         r, ldr = (residual.data_ptr(), self._matrix("residual", residual, T, m, n)[2]) if residual is not None else (None, 0)
         if out is None:
             out, ldy = self._empty(m, n, dtype=T, device=self.device), n
@@ -578,6 +608,8 @@ class LinearOps:
         yc, ye = self._held("save_y", save_y, m, n) if save_y is not None else (None, None)
         self._check(self._L.lqsgd_linear_forward(self._h, self._types[T], ACTS[act], m, n, k, x.data_ptr(), ldx, w.data_ptr(), ldw,
                                                  b, r, ldr, out.data_ptr(), ldy, zc, ze, yc, ye))
+        if new and (x.requires_grad or w.requires_grad or (b and bias.requires_grad) or (r and residual.requires_grad)):
+            return _without_autograd(out, x, w, bias, residual)
         return out
 
     # -- backward --------------------------------------------------------
@@ -592,6 +624,7 @@ class LinearOps:
             raise LqsgdError(EINVAL, "the activation's backward needs the checkpoint of z")
         zc, ze = self._held("z", z, m, n) if z is not None else (None, None)
         pz, lddz = None, 0
+        new_dz, new_db = dz is None, dbias is None
         if dz is not None:
             pz, lddz = dz.data_ptr(), self._matrix("dz", dz, T, m, n)[2]
         elif want_dz:
@@ -604,6 +637,11 @@ class LinearOps:
         db = self._vector("dbias", dbias, self._f32, n) if dbias is not None else None
         self._check(self._L.lqsgd_linear_activation_backward(self._h, self._types[T], ACTS[act], m, n, dy.data_ptr(), lddy, zc, ze, pz, lddz,
                                                              db, 1 if accumulate else 0))
+        if dy.requires_grad:
+            if new_dz and dz is not None:
+                dz = _without_autograd(dz, dy)
+            if new_db and dbias is not None:
+                dbias = _without_autograd(dbias, dy)
         return dz, dbias
 
     def input_grad(self, dz, w, out=None):
@@ -612,12 +650,15 @@ class LinearOps:
         m, n, lddz = self._matrix("dz", dz)
         T = dz.dtype
         _, k, ldw = self._matrix("w", w, T, n, None)
-        if out is None:
+        new = out is None
+        if new:
             out, lddx = self._empty(m, k, dtype=T, device=self.device), k
         else:
             lddx = self._matrix("out", out, T, m, k)[2]
         self._check(self._L.lqsgd_linear_input_grad(self._h, self._types[T], m, n, k, dz.data_ptr(), lddz, w.data_ptr(), ldw, out.data_ptr(),
                                                     lddx))
+        if new and (dz.requires_grad or w.requires_grad):
+            return _without_autograd(out, dz, w)
         return out
 
     def weight_grad(self, dz, x, out=None, dtype=None, accumulate=False):
@@ -628,7 +669,8 @@ class LinearOps:
             raise LqsgdError(EINVAL, "x has to be a Checkpoint")
         k = x.features
         xc, xe = self._held("x", x, m, k)
-        if out is None:
+        new = out is None
+        if new:
             if accumulate:
                 raise LqsgdError(EINVAL, "accumulate needs the gradient to add to")
             dtype, lddw = dtype or self._f32, k
@@ -639,4 +681,6 @@ class LinearOps:
             lddw = self._matrix("out", out, dtype, n, k)[2]
         self._check(self._L.lqsgd_linear_weight_grad(self._h, self._types[dz.dtype], m, n, k, dz.data_ptr(), lddz, xc, xe,
                                                      self._types[out.dtype], out.data_ptr(), lddw, 1 if accumulate else 0))
+        if new and dz.requires_grad:
+            return _without_autograd(out, dz)
         return out
