@@ -33,7 +33,10 @@
  *   - NaN and infinities go the way of the formulas, with two exceptions.  LQSGD_TYPE_F32 products are made from operands split
  *     into three bfloat16 terms: an infinite operand may make the outputs it reaches NaN instead of infinite, and operands are taken
  *     to multiples of 2^-133 (magnitudes below 2^-109 lose their last bits).  A checkpoint reads back as above.
- *   - A call only enqueues kernels on the context's stream (it may be captured into a HIP graph); it neither allocates nor waits.
+ *   - A call only enqueues kernels on the context's stream; it neither allocates nor waits.  It may be captured into a HIP graph, whose
+ *     replays use the context's workspace like the call itself: order replays, on whatever stream they run, with one another and with
+ *     the context's other calls.  Work that is to run side by side takes a context each (two users of one workspace at a time add up
+ *     each other's sums).
  */
 #ifndef LQSGD_LINEAR_H
 #define LQSGD_LINEAR_H
@@ -63,7 +66,8 @@ typedef struct lqsgd_linear lqsgd_linear;
                                                      values may be refused (ESHAPE) */
 
 /* A context on the current HIP device: the stream its calls run on (a hipStream_t, NULL = the default stream) and 64 MiB of
- * workspace, which the calls share: work of one context is ordered by its stream.  Not thread-safe.  Errors: EINVAL, ENOMEM, EHIP. */
+ * workspace, which the calls share: work of one context is ordered by its stream, replays of graphs by the caller.  Not thread-safe.
+ * Errors: EINVAL, ENOMEM, EHIP. */
 int lqsgd_linear_create(void* hip_stream, lqsgd_linear** out);
 /* Waits for the stream and frees everything; NULL is accepted. */
 int lqsgd_linear_destroy(lqsgd_linear* ctx);

@@ -470,6 +470,8 @@ class LinearOps:
     two-dimensional, the elements of a row contiguous, rows at any stride).  Every call checks shapes, types and devices on the host
     and enqueues kernels on the stream that was current at construction; it raises where another stream is current, since the outputs
     that it allocates would belong to that one.  Tensors made on other streams are the caller's to order, as with torch's own calls.
+    So are the replays of a graph that the calls were captured into (on this stream: torch.cuda.graph(g, stream=...)): they use the context's
+    workspace, and may run neither beside each other nor beside its other calls.  What is to run side by side takes a LinearOps each.
 
     The calls are a layer's passes, made by hand; autograd does not go through them.  A new tensor that a call returns, made from tensors that
     require a gradient while autograd records, raises where a backward() reaches it.  Checkpoints, and tensors given for the
