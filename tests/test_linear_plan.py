@@ -51,3 +51,23 @@ def test_what_no_launch_holds_is_said(exe):
     assert [p[5] for p in lp.plans(exe, [("forward", "f32", top, 1 << 20, 1), ("input_grad", "bf16", top, 1, 1 << 20)])] == [0, 0]
     narrow = lp.plans(exe, [("forward", "bf16", top, 16, 16), ("forward", "f32", top, 64, 64)])
     assert [p[0] for p in narrow] == ["128 x 128"] * 2 and [p[5] for p in narrow] == [1 << 23] * 2
+
+
+def test_the_gpu_tests_reach_every_kernel(exe):
+    """The products of lp.CASES are served by the kernels that they are listed for, and every one of those is there."""
+    asked = [(product, "f32" if operands == "f32" else "bf16", m, n, k) for product, operands, m, n, k, _, _ in lp.CASES]
+    covered = set()
+    for case, a, p in zip(lp.CASES, asked, lp.plans(exe, asked)):
+        product, operands, m, n, k, kernel, in_parts = case
+        assert operands == ("f32" if a[1] == "f32" else "direct" if lp.is_direct(*a) else "any"), case
+        assert (p[0], p[1] > 1) == (kernel, in_parts), (case, p)
+        _check(a, p)
+        nj = {"forward": m, "input_grad": m, "weight_grad": n}[product]
+        depth = {"forward": k, "input_grad": n, "weight_grad": m}[product]
+        if kernel != "by depth":
+            assert min(p[4], depth) > 5 * 32, (case, p)         # more steps than there are buffers
+        covered.add((product, operands, kernel, in_parts, kernel == "by depth" and nj <= 32))
+    every = {(product, operands, kernel, parts, narrow) for product in lp.PRODUCTS for operands in ("f32", "direct", "any")
+             for kernel in lp.KERNELS for parts in (False, True) for narrow in (False, True) if kernel == "by depth" or not narrow}
+    assert covered == every, every ^ covered
+    assert lp.plans(exe, [("input_grad", "bf16", 700000, 256, 4096)])[0][0] == "large"         # the long tensors' product
