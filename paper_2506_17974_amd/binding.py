@@ -469,7 +469,8 @@ class LinearOps:
     """One lqsgd_linear context: the forward and backward passes of linear layers on torch CUDA tensors (float32, bfloat16 or float16;
     two-dimensional, the elements of a row contiguous, rows at any stride).  Every call checks shapes, types and devices on the host
     and enqueues kernels on the stream that was current at construction; it raises where another stream is current, since the outputs
-    that it allocates would belong to that one.  Tensors made on other streams are the caller's to order, as with torch's own calls.
+    that it allocates would belong to that one, and where another device is, since kernels would be launched there.
+    Tensors made on other streams are the caller's to order, as with torch's own calls.
     So are the replays of a graph that the calls were captured into (on this stream: torch.cuda.graph(g, stream=...)): they use the context's
     workspace, and may run neither beside each other nor beside its other calls.  What is to run side by side takes a LinearOps each.
 
@@ -489,6 +490,8 @@ class LinearOps:
         self.device = torch.device("cuda", self._index)
         # the current stream's handle, without the Stream object around it where torch has that
         self._stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+        # kernels go to the current device: which that is has to be asked only where there are others
+        self._current_device = torch.cuda.current_device if torch.cuda.device_count() > 1 else None
         self.stream_handle = int(self._stream(self._index))
         self._L = lib()
         rc = self._L.lqsgd_linear_create(C.c_void_p(self.stream_handle), C.byref(self._h))
@@ -504,6 +507,8 @@ class LinearOps:
     def _begin(self):
         if not self._h:
             raise LqsgdError(ESTATE, "the context is closed")
+        if self._current_device is not None and self._current_device() != self._index:
+            raise LqsgdError(ESTATE, "the current device is not the one this context was made on, %s" % self.device)
         if self._stream(self._index) != self.stream_handle:
             raise LqsgdError(ESTATE, "the current stream is not the one this context was made on")
 
