@@ -36,7 +36,7 @@
  *   - A call only enqueues kernels on the context's stream; it neither allocates nor waits.  It may be captured into a HIP graph, whose
  *     replays use the context's workspace like the call itself: order replays, on whatever stream they run, with one another and with
  *     the context's other calls.  Work that is to run side by side takes a context each (two users of one workspace at a time add up
- *     each other's sums).
+ *     each other's sums).  A context has to live as long as the graphs that hold calls of it are replayed.
  */
 #ifndef LQSGD_LINEAR_H
 #define LQSGD_LINEAR_H
@@ -69,7 +69,7 @@ typedef struct lqsgd_linear lqsgd_linear;
  * workspace, which the calls share: work of one context is ordered by its stream, replays of graphs by the caller.  Not thread-safe.
  * Errors: EINVAL, ENOMEM, EHIP. */
 int lqsgd_linear_create(void* hip_stream, lqsgd_linear** out);
-/* Waits for the stream and frees everything; NULL is accepted. */
+/* Waits for the stream and frees everything, also what graphs of its calls would use; NULL is accepted. */
 int lqsgd_linear_destroy(lqsgd_linear* ctx);
 /* Waits for the context's stream. */
 int lqsgd_linear_synchronize(lqsgd_linear* ctx);

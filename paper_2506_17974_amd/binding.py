@@ -472,7 +472,8 @@ class LinearOps:
     that it allocates would belong to that one, and where another device is, since kernels would be launched there.
     Tensors made on other streams are the caller's to order, as with torch's own calls.
     So are the replays of a graph that the calls were captured into (on this stream: torch.cuda.graph(g, stream=...)): they use the context's
-    workspace, and may run neither beside each other nor beside its other calls.  What is to run side by side takes a LinearOps each.
+    workspace, and may run neither beside each other nor beside its other calls, nor after close() or the end of this object.  What is to run
+    side by side takes a LinearOps each.
 
     The calls are a layer's passes, made by hand; autograd does not go through them.  A new tensor that a call returns, made from tensors that
     require a gradient while autograd records, raises where a backward() reaches it.  Checkpoints, and tensors given for the
