@@ -272,9 +272,9 @@ __device__ inline void times_tabled_slope(float (&d)[8], uint2 w, uint32_t byte,
 
 // A workgroup takes a strip of 8 << lanes_log2 features and a run of samples; a lane keeps 8 features' sums and has 4 samples on
 // their way.  Lanes that the strip does not fill take further samples.  Strips' sums over runs go to `part` (runs x rows) where
-// there is more than one run.  TABLE: gelu or silu of many samples, slopes from LDS (by their formulas, 27 instructions a value, the
-// vector units took 54 us for 4096 x 11008 bfloat16 values; now 42, and 58 a pass where the tensors come from HBM, 4 TB/s: bound by
-// memory).
+// there is more than one run.  TABLE: gelu or silu of many samples, slopes from LDS (by formulas of 27 instructions a value the
+// vector units took 54 us for 4096 x 11008 bfloat16 values; now 42, and 58.6 a pass where the tensors come from HBM: 3.9 TB/s, where plain
+// streams of this mix reach 6.2 -- pieces of 1 KiB lie 22 KB apart, and 60 % of the table reads' LDS cycles are bank conflicts).
 template <typename T, bool TABLE>
 __global__ __launch_bounds__(256) void activation_backward_kernel(const T* dy, int64_t lddy, Codes z, T* dz, int64_t lddz, float* dbias,
                                                                   int accumulate, float* part, const float* slopes, int64_t samples,
@@ -358,7 +358,7 @@ __global__ __launch_bounds__(256) void sum_runs_kernel(const float* part, float*
 // ---------------------------------------------------------------------------
 // products
 // ---------------------------------------------------------------------------
-// 4096 x 11008 values with gelu and both checkpoints take 374 us with the product, 330 without all that: 45 vector instructions a
+// 4096 x 11008 values with gelu and both checkpoints take 381 us with the product, 330 without all that: 50 vector instructions a
 // value, whose time no product hides (a CU holds one 256 x 256 tile).
 // The end of a product: v holds D[j][i0 .. i0 + N - 1], i0 a multiple of N, and neighbouring lanes the rest of the group of 32.  All
 // lanes of the wavefront come here together; `there` is false for those that have no row j.  N: 16 bytes of what is written.
@@ -877,13 +877,12 @@ __device__ inline void add_parts(float (&v)[N], const ProductArgs& a, const Spli
 }
 
 // A tile of D to a workgroup, operands through LDS in steps of BK.  What bounds it: 32 x 32 x 16 matrix instructions at 1024 flops a
-// cycle and SIMD, whose pipes are busy 49 (weight gradient) to 65 % (input gradient) of the time at 1.8 to 1.9 GHz -- the card lowers
-// its clock for them -- and what LDS
+// cycle and SIMD, whose pipes are busy 47 (forward with its epilogue) to 65 % (input gradient) of the time, at 1.8 to 2.0 GHz, and what LDS
 // has to deliver to them, which is why a wavefront has as large a part of the tile as its registers hold (128 x 64: 6 reads of 1 KiB
-// to 8 products).  Measured, back to back, bfloat16 256 x 256: forward 4096 x 4096 -> 11008 322 us (1.15 PFLOP/s; the library's
-// product 402), input gradient 4096 x 11008 -> 4096 290 us (1.27 PFLOP/s; library 260), weight gradient of 8192 samples, 4096 x 4096,
-// decoding included, 246 us (1.12 PFLOP/s; library, from a decoded operand, 227).  fp32 256 x 128: input gradient 2048 x 8192 -> 8192
-// 1.36 ms (202 TFLOP/s of fp32, 1.2 PFLOP/s of its six bfloat16 products; the fp32 matrix instructions reach 153 in the library).
+// to 8 products).  Measured, back to back, bfloat16 256 x 256: forward 4096 x 4096 -> 11008 338 us (1.09 PFLOP/s; the library's
+// product 406), input gradient 4096 x 11008 -> 4096 290 us (1.27 PFLOP/s; library 261), weight gradient of 8192 samples, 4096 x 4096,
+// decoding included, 265 us (1.04 PFLOP/s; library, from a decoded operand, 223).  fp32 256 x 128: input gradient 2048 x 8192 -> 8192
+// 1.33 ms (206 TFLOP/s of fp32, 1.24 PFLOP/s of its six bfloat16 products; the fp32 matrix instructions reach 153 in the library).
 // Tried: two buffers and a full wait at the barrier (input gradient 385 us), four wavefronts of 128 x 128 (the compiler spills 130
 // registers: 1.3 ms), wavefront priorities around the products (310 against 296), fp32 in steps of 16 (1.6 ms).
 template <typename T, int PRODUCT, typename S, bool DIRECT>
