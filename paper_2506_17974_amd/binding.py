@@ -1,5 +1,5 @@
-"""ctypes binding of include/lqsgd.h and include/lqsgd_linear.h.  Argument marshalling only: every step of
-the compressor and of the linear layer runs in the HIP library.  torch is used for device memory and
+"""ctypes binding of include/lqsgd.h, include/lqsgd_linear.h and include/lqsgd_block.h.  Argument marshalling only: every step of
+the compressor, of the linear layer and of what stands around it runs in the HIP library.  torch is used for device memory and
 the stream handle, nothing else."""
 from __future__ import annotations
 
@@ -37,9 +37,12 @@ LINEAR_SYMBOLS = [
     "lqsgd_checkpoint_save", "lqsgd_checkpoint_load", "lqsgd_linear_forward", "lqsgd_linear_activation_backward",
     "lqsgd_linear_input_grad", "lqsgd_linear_weight_grad",
 ]
+# ... and lqsgd_block.h
+BLOCK_SYMBOLS = ["lqsgd_rows_save", "lqsgd_rows_load", "lqsgd_rms_norm", "lqsgd_rms_norm_backward", "lqsgd_int8_forward", "lqsgd_dropout"]
 TYPE_F32, TYPE_BF16, TYPE_F16 = range(3)
 ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 CHECKPOINT_GROUP = 32
+INT8_MAX_COLS = 131040
 
 
 class LqsgdError(RuntimeError):
@@ -124,6 +127,12 @@ def lib():
     L.lqsgd_linear_activation_backward.argtypes = [vp, i32, i32, i64, i32, vp, i64, vp, vp, vp, i64, vp, i32]
     L.lqsgd_linear_input_grad.argtypes = [vp, i32, i64, i32, i32, vp, i64, vp, i64, vp, i64]
     L.lqsgd_linear_weight_grad.argtypes = [vp, i32, i64, i32, i32, vp, i64, vp, vp, i32, vp, i64, i32]
+    L.lqsgd_rows_save.argtypes = [vp, i32, i64, i32, vp, i64, vp, vp]
+    L.lqsgd_rows_load.argtypes = [vp, i32, i64, i32, vp, vp, vp, i64]
+    L.lqsgd_rms_norm.argtypes = [vp, i32, i64, i32, C.c_double, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, vp, vp, vp, vp]
+    L.lqsgd_rms_norm_backward.argtypes = [vp, i32, i64, i32, vp, i64, vp, i64, vp, vp, vp, vp, vp, i64, vp, i64, vp, i32]
+    L.lqsgd_int8_forward.argtypes = [vp, i32, i32, i64, i32, i32, vp, vp, vp, vp, vp, vp, i64, vp, i64]
+    L.lqsgd_dropout.argtypes = [vp, i32, i64, i32, C.c_double, C.c_uint64, C.c_uint64, vp, vp, i64, vp, i64, vp, i64, vp, vp]
     _lib = L
     return L
 
@@ -440,6 +449,53 @@ class Checkpoint:
         return self.samples * -(-self.features // CHECKPOINT_GROUP) * (CHECKPOINT_GROUP + 1)
 
 
+class RowCodes:
+    """A samples x features tensor kept in 8 bits with a scale a row, as include/lqsgd_block.h lays it out: `codes` (int8, samples x the
+    features rounded up to groups of 32) and `scales` (float32, samples).  Made of those two, or by empty() with both in one allocation."""
+    __slots__ = ("features", "_codes", "_scales", "_both", "_at")
+
+    def __init__(self, codes, scales, features):
+        self.features, self._codes, self._scales = int(features), codes, scales
+        self._both = self._at = None
+
+    @classmethod
+    def empty(cls, samples, features, device="cuda"):
+        """One whose values are yet to be written."""
+        import torch
+        self = cls(None, None, features)
+        n = samples * -(-self.features // CHECKPOINT_GROUP) * CHECKPOINT_GROUP
+        self._both = torch.empty(n + 4 * samples, dtype=torch.uint8, device=device)
+        at = self._both.data_ptr()
+        self._at = (samples, self._both.get_device(), at, at + n, self.features)       # what LinearOps would find out about the two
+        return self
+
+    def _parts(self):
+        import torch
+        samples, stride = self._at[0], -(-self._at[4] // CHECKPOINT_GROUP) * CHECKPOINT_GROUP
+        self._codes = self._both[:samples * stride].view(torch.int8).view(samples, stride)
+        self._scales = self._both[samples * stride:].view(torch.float32)
+
+    @property
+    def codes(self):
+        if self._codes is None:
+            self._parts()
+        return self._codes
+
+    @property
+    def scales(self):
+        if self._scales is None:
+            self._parts()
+        return self._scales
+
+    @property
+    def samples(self):
+        return self._at[0] if self._at else self._codes.shape[0]
+
+    @property
+    def nbytes(self):
+        return self.samples * (-(-self.features // CHECKPOINT_GROUP) * CHECKPOINT_GROUP + 4)
+
+
 _no_backward = None
 
 
@@ -460,13 +516,14 @@ def _without_autograd(out, *inputs):
             @staticmethod
             def backward(ctx, *grads):
                 raise LqsgdError(EINVAL, "autograd does not pass through the linear layer's calls: their gradients are made by "
-                                         "activation_backward, input_grad and weight_grad")
+                                         "activation_backward, input_grad, weight_grad, rms_norm_backward and dropout")
         _no_backward = NoBackward
     return _no_backward.apply(out, *inputs)
 
 
 class LinearOps:
-    """One lqsgd_linear context: the forward and backward passes of linear layers on torch CUDA tensors (float32, bfloat16 or float16;
+    """One lqsgd_linear context: the forward and backward passes of linear layers, and of the norms, 8-bit rows and dropout around them, on
+    torch CUDA tensors (float32, bfloat16 or float16;
     two-dimensional, the elements of a row contiguous, rows at any stride).  Every call checks shapes, types and devices on the host
     and enqueues kernels on the stream that was current at construction; it raises where another stream is current, since the outputs
     that it allocates would belong to that one, and where another device is, since kernels would be launched there.
@@ -553,6 +610,23 @@ class LinearOps:
                 not exps.is_contiguous():
             self._bad("%s: contiguous uint8 exponents of %d x %d wanted" % (what, samples, groups), exps)
         return codes.data_ptr(), exps.data_ptr()
+
+    def _rows(self, what, c, samples=None, features=None):
+        if not isinstance(c, RowCodes):
+            raise LqsgdError(EINVAL, "%s has to be RowCodes" % what)
+        if features is not None and c.features != features:
+            raise LqsgdError(ESHAPE, "%s has %d features, %d wanted" % (what, c.features, features))
+        if samples is None:
+            samples = c.samples
+        at = c._at
+        if at is not None and at[0] == samples and at[1] == self._index and at[4] == c.features:
+            return at[2], at[3]
+        stride = -(-c.features // CHECKPOINT_GROUP) * CHECKPOINT_GROUP
+        codes, scales = c.codes, c.scales
+        if codes.dtype is not self._codes_type or codes.shape != (samples, stride) or codes.get_device() != self._index or \
+                not codes.is_contiguous():
+            self._bad("%s: contiguous int8 codes of %d x %d wanted" % (what, samples, stride), codes)
+        return codes.data_ptr(), self._vector("%s's scales" % what, scales, self._f32, samples)
 
     def close(self):
         if self._h:
@@ -691,4 +765,153 @@ class LinearOps:
                                                      self._types[out.dtype], out.data_ptr(), lddw, 1 if accumulate else 0))
         if new and dz.requires_grad:
             return _without_autograd(out, dz)
+        return out
+
+    # -- around the layer --------------------------------------------------
+    def quantize(self, x, out=None):
+        """x as 8-bit rows with a scale each."""
+        self._begin()
+        m, n, ld = self._matrix("x", x)
+        if out is None:
+            out = RowCodes.empty(m, n, self.device)
+        codes, scales = self._rows("out", out, m, n)
+        self._check(self._L.lqsgd_rows_save(self._h, self._types[x.dtype], m, n, x.data_ptr(), ld, codes, scales))
+        return out
+
+    def dequantize(self, rows, dtype=None, out=None):
+        """The tensor that 8-bit rows stand for, in `dtype` (default: out's, else bfloat16)."""
+        self._begin()
+        codes, scales = self._rows("rows", rows)
+        m, n = rows.samples, rows.features
+        if out is None:
+            dtype, ld = dtype or self._torch.bfloat16, n
+            if dtype not in self._types:
+                raise LqsgdError(EINVAL, "8-bit rows are not read back as %s" % (dtype,))
+            out = self._empty(m, n, dtype=dtype, device=self.device)
+        else:
+            ld = self._matrix("out", out, dtype, m, n)[2]
+        self._check(self._L.lqsgd_rows_load(self._h, self._types[out.dtype], m, n, codes, scales, out.data_ptr(), ld))
+        return out
+
+    def rms_norm(self, x, gain=None, residual=None, eps=1e-6, h=None, out=None, rstd=None, save_y=None, quantize_y=None, want_h=True,
+                 want_y=True, want_rstd=False):
+        """(y, h, rstd): h = x + residual (None without a residual, and where it is not wanted), y = h gain / sqrt(mean h^2 + eps), and
+        rstd, which the backward pass needs.  save_y: a Checkpoint that receives y as well; quantize_y: RowCodes that do.  h may be x or the
+        residual."""
+        self._begin()
+        m, n, ldx = self._matrix("x", x)
+        T = x.dtype
+        g = self._vector("gain", gain, T, n) if gain is not None else None
+        new_h, new_y, new_rstd = h is None, out is None, rstd is None
+        r, ldr, ph, ldh, py, ldy = None, 0, None, 0, None, 0
+        if residual is not None:
+            r, ldr = residual.data_ptr(), self._matrix("residual", residual, T, m, n)[2]
+            if new_h and want_h:
+                h, ldh = self._empty(m, n, dtype=T, device=self.device), n
+                ph = h.data_ptr()
+        if not new_h:
+            if residual is None:
+                raise LqsgdError(EINVAL, "h is wanted without a residual: it is x")
+            ph, ldh = h.data_ptr(), self._matrix("h", h, T, m, n)[2]
+        if not new_y:
+            py, ldy = out.data_ptr(), self._matrix("out", out, T, m, n)[2]
+        elif want_y:
+            out, ldy = self._empty(m, n, dtype=T, device=self.device), n
+            py = out.data_ptr()
+        if new_rstd and want_rstd:
+            rstd = self._empty(m, dtype=self._f32, device=self.device)
+        ps = self._vector("rstd", rstd, self._f32, m) if rstd is not None else None
+        yc, ye = self._held("save_y", save_y, m, n) if save_y is not None else (None, None)
+        qc, qs = self._rows("quantize_y", quantize_y, m, n) if quantize_y is not None else (None, None)
+        self._check(self._L.lqsgd_rms_norm(self._h, self._types[T], m, n, eps, x.data_ptr(), ldx, r, ldr, g, ph, ldh, py, ldy, ps, yc, ye, qc, qs))
+        if x.requires_grad or (g and gain.requires_grad) or (r and residual.requires_grad):
+            out, h, rstd = (_without_autograd(t, x, gain, residual) if new and t is not None else t
+                            for new, t in ((new_y, out), (new_h, h), (new_rstd, rstd)))
+        return out, h, rstd
+
+    def rms_norm_backward(self, dy, h, rstd, gain=None, dh=None, dx=None, dgain=None, accumulate=False, want_dx=True, want_dgain=True):
+        """(dx, dgain) of dy and of dh, which came to h past the norm: dx is the gradient of rms_norm's x and of its residual alike.  h: the
+        tensor that the norm was taken of (x without a residual), or a Checkpoint of it.  What is not wanted is None.  dx may be dy or dh."""
+        self._begin()
+        m, n, lddy = self._matrix("dy", dy)
+        T = dy.dtype
+        if isinstance(h, Checkpoint):
+            ph, ldh = None, 0
+            hc, he = self._held("h", h, m, n)
+        else:
+            ldh = self._matrix("h", h, T, m, n)[2]
+            ph, hc, he = h.data_ptr(), None, None
+        ps = self._vector("rstd", rstd, self._f32, m)
+        g = self._vector("gain", gain, T, n) if gain is not None else None
+        pdh, lddh = (dh.data_ptr(), self._matrix("dh", dh, T, m, n)[2]) if dh is not None else (None, 0)
+        new_dx, new_dg = dx is None, dgain is None
+        pdx, lddx = None, 0
+        if not new_dx:
+            pdx, lddx = dx.data_ptr(), self._matrix("dx", dx, T, m, n)[2]
+        elif want_dx:
+            dx, lddx = self._empty(m, n, dtype=T, device=self.device), n
+            pdx = dx.data_ptr()
+        if new_dg and want_dgain:
+            if accumulate:
+                raise LqsgdError(EINVAL, "accumulate needs the dgain to add to")
+            dgain = self._empty(n, dtype=self._f32, device=self.device)
+        pdg = self._vector("dgain", dgain, self._f32, n) if dgain is not None else None
+        self._check(self._L.lqsgd_rms_norm_backward(self._h, self._types[T], m, n, dy.data_ptr(), lddy, ph, ldh, hc, he, ps, g, pdh, lddh,
+                                                    pdx, lddx, pdg, 1 if accumulate else 0))
+        inputs = (dy, None if hc else h, rstd, gain, dh)
+        if any(t is not None and t.requires_grad for t in inputs):
+            dx, dgain = (_without_autograd(t, *inputs) if new and t is not None else t for new, t in ((new_dx, dx), (new_dg, dgain)))
+        return dx, dgain
+
+    def int8_forward(self, x, w, bias=None, residual=None, act="none", dtype=None, out=None):
+        """act(x w^T + bias) + residual of RowCodes x and w, in `dtype` (default: out's, the residual's or the bias', else bfloat16)."""
+        self._begin()
+        if act not in ACTS:
+            raise LqsgdError(EINVAL, "unknown activation %r" % (act,))
+        xc, xs = self._rows("x", x)
+        m, k = x.samples, x.features
+        wc, ws = self._rows("w", w, None, k)
+        n = w.samples
+        new = out is None
+        T = dtype or next((t.dtype for t in (out, residual, bias) if isinstance(t, self._Tensor)), self._torch.bfloat16)
+        if T not in self._types:
+            raise LqsgdError(EINVAL, "a product is not written as %s" % (T,))
+        b = self._vector("bias", bias, T, n) if bias is not None else None
+        r, ldr = (residual.data_ptr(), self._matrix("residual", residual, T, m, n)[2]) if residual is not None else (None, 0)
+        if new:
+            out, ldy = self._empty(m, n, dtype=T, device=self.device), n
+        else:
+            ldy = self._matrix("out", out, T, m, n)[2]
+        self._check(self._L.lqsgd_int8_forward(self._h, self._types[T], ACTS[act], m, n, k, xc, xs, wc, ws, b, r, ldr, out.data_ptr(), ldy))
+        if new and ((b and bias.requires_grad) or (r and residual.requires_grad)):
+            return _without_autograd(out, bias, residual)
+        return out
+
+    def dropout(self, x, p, seed, offset=0, residual=None, out=None, save_y=None, more_offset=None):
+        """x with a share p of its values dropped and the others divided by 1 - p (p to a multiple of 2^-16), plus residual.  Which, is
+        decided by seed, offset (64 bits each) and the place in the tensor: the gradient of x is dropout(dy, p, seed, offset).  out may be x or the
+        residual; save_y: a Checkpoint that receives the result as well.  more_offset: an int64 tensor of one element on the device
+        that is added to offset when the call runs: a graph that counts it up has another mask at each replay."""
+        self._begin()
+        m, n, ldx = self._matrix("x", x)
+        T = x.dtype
+        if not 0 <= seed < 1 << 64 or not 0 <= offset < 1 << 64:
+            raise LqsgdError(EINVAL, "seed and offset have 64 bits")
+        more = None
+        if more_offset is not None:
+            if not isinstance(more_offset, self._Tensor) or more_offset.get_device() != self._index or more_offset.dtype is not self._torch.int64 or \
+                    more_offset.numel() != 1:
+                self._bad("more_offset has to be one int64 on %s" % self.device, more_offset)
+            more = more_offset.data_ptr()
+        new = out is None
+        r, ldr = (residual.data_ptr(), self._matrix("residual", residual, T, m, n)[2]) if residual is not None else (None, 0)
+        if new:
+            out, ldy = self._empty(m, n, dtype=T, device=self.device), n
+        else:
+            ldy = self._matrix("out", out, T, m, n)[2]
+        yc, ye = self._held("save_y", save_y, m, n) if save_y is not None else (None, None)
+        self._check(self._L.lqsgd_dropout(self._h, self._types[T], m, n, p, seed, offset, more, x.data_ptr(), ldx, r, ldr, out.data_ptr(), ldy,
+                                          yc, ye))
+        if new and (x.requires_grad or (r and residual.requires_grad)):
+            return _without_autograd(out, x, residual)
         return out

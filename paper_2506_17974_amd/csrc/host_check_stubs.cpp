@@ -1,6 +1,7 @@
 // Stand-ins for the kernel launchers, for the host-only sanitizer build: the planner and the
 // argument checking of the C ABI are linked without any device code.  Nothing here is part of
 // the library; every launcher reports that it cannot run.
+#include "lqsgd_block_kernels.h"
 #include "lqsgd_kernels.h"
 #include "lqsgd_linear_kernels.h"
 
@@ -31,6 +32,12 @@ hipError_t launch_activation_backward(int, int, int64_t, int32_t, const void*, i
                                       hipStream_t) {
   return hipErrorNotSupported;
 }
+hipError_t launch_rows_save(int, int64_t, int32_t, const void*, int64_t, Rows, hipStream_t) { return hipErrorNotSupported; }
+hipError_t launch_rows_load(int, int64_t, int32_t, Rows, void*, int64_t, hipStream_t) { return hipErrorNotSupported; }
+hipError_t launch_rms_norm(int, const NormArgs&, hipStream_t) { return hipErrorNotSupported; }
+hipError_t launch_rms_norm_backward(int, const NormBackwardArgs&, hipStream_t) { return hipErrorNotSupported; }
+hipError_t launch_dropout(int, const DropoutArgs&, hipStream_t) { return hipErrorNotSupported; }
+hipError_t launch_int8_product(int, const Int8Args&, hipStream_t) { return hipErrorNotSupported; }
 
 }  // namespace linear
 }  // namespace lqsgd
