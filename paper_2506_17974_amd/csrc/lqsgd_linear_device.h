@@ -230,10 +230,11 @@ hipError_t by_slabs(int64_t samples, uint32_t pieces, F&& launch) {
 }
 
 // Features' sums over `runs` runs of samples, in the runs' order by four.
-__global__ __launch_bounds__(256) void sum_runs_kernel(const float* part, float* dbias, int accumulate, int rows, int runs) {
-  __shared__ float sums[4][64];
+template <typename Sum>
+__global__ __launch_bounds__(256) void sum_runs_kernel(const Sum* part, Sum* dbias, int accumulate, int rows, int runs) {
+  __shared__ Sum sums[4][64];
   const int f = (int)blockIdx.x * 64 + (threadIdx.x & 63), w = threadIdx.x >> 6;
-  float s = 0.f;
+  Sum s = 0;
   if (f < rows) {
 #pragma unroll 8
     for (int k = w; k < runs; k += 4) s += part[(int64_t)k * rows + f];
