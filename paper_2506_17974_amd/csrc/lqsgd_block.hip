@@ -14,43 +14,6 @@ namespace {
 // ---------------------------------------------------------------------------
 // a row shared out among lanes
 // ---------------------------------------------------------------------------
-// What all 64 lanes have, put together by `op` (commutative): every lane gets the same bits.  Lanes are exchanged within 4, 8 and 16,
-// then rows of 16 and halves of 32 change places.
-template <typename V, typename Op>
-__device__ inline V over_wave(V v, Op op) {
-  constexpr int kWords = sizeof(V) / 4;
-  auto moved = [&](auto control) {
-    uint32_t w[kWords];
-    __builtin_memcpy(w, &v, sizeof v);
-#pragma unroll
-    for (int k = 0; k < kWords; ++k) w[k] = (uint32_t)__builtin_amdgcn_mov_dpp((int)w[k], decltype(control)::value, 0xf, 0xf, true);
-    V o;
-    __builtin_memcpy(&o, w, sizeof o);
-    return o;
-  };
-  v = op(v, moved(std::integral_constant<int, 0xb1>{}));           // lane ^ 1
-  v = op(v, moved(std::integral_constant<int, 0x4e>{}));           // lane ^ 2
-  v = op(v, moved(std::integral_constant<int, 0x141>{}));          // 7 - lane, of 8
-  v = op(v, moved(std::integral_constant<int, 0x140>{}));          // 15 - lane, of 16
-  auto halves = [&](auto swap) {
-    uint32_t w[kWords], a[kWords], b[kWords];
-    __builtin_memcpy(w, &v, sizeof v);
-#pragma unroll
-    for (int k = 0; k < kWords; ++k) {
-      const auto r = swap(w[k]);
-      a[k] = r[0], b[k] = r[1];
-    }
-    V x, y;
-    __builtin_memcpy(&x, a, sizeof x);
-    __builtin_memcpy(&y, b, sizeof y);
-    return op(x, y);
-  };
-  v = halves([](uint32_t w) { return __builtin_amdgcn_permlane16_swap(w, w, false, false); });
-  return halves([](uint32_t w) { return __builtin_amdgcn_permlane32_swap(w, w, false, false); });
-}
-struct Plus { template <typename V> __device__ V operator()(V a, V b) const { return a + b; } };
-struct Larger { __device__ float operator()(float a, float b) const { return __builtin_elementwise_maximum(a, b); } };     // NaN if one is
-
 // 8-bit rows: the step of a row whose largest magnitude is absmax (NaN if that is none).
 __device__ inline float row_step(float absmax) {
   return absmax < __builtin_inff() ? fmaxf(absmax / 127.f, 0x1p-126f) : __builtin_nanf("");

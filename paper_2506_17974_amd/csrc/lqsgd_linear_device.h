@@ -169,16 +169,18 @@ __device__ inline void stream_out(void* p, const void* from) {
 }
 template <int N, typename T>
 __device__ inline void store_values(T* p, const float (&v)[N], int n) {
-  if (n >= N) {
-    T t[N];
+  T t[N];
+  if constexpr (sizeof t >= 4) {
+    if (n >= N) {
 #pragma unroll
-    for (int k = 0; k < N; ++k) t[k] = narrow<T>(v[k]);
-    stream_out<sizeof t>(p, t);
-  } else {
-#pragma unroll
-    for (int k = 0; k < N; ++k)
-      if (k < n) p[k] = narrow<T>(v[k]);
+      for (int k = 0; k < N; ++k) t[k] = narrow<T>(v[k]);
+      stream_out<sizeof t>(p, t);
+      return;
+    }
   }
+#pragma unroll
+  for (int k = 0; k < N; ++k)
+    if (k < n) p[k] = narrow<T>(v[k]);
 }
 
 // N values of one group quantised and packed, four to a word; `absmax` is the whole group's.  v 2^-e + 1.5 2^23 rounds to the
@@ -203,6 +205,46 @@ __device__ inline void pack_codes(uint32_t (&w)[N / 4], const float (&v)[N], flo
 }
 
 constexpr int kPiece = 8;                         // values that a thread takes at once
+
+// ---------------------------------------------------------------------------
+// a wavefront's lanes put together
+// ---------------------------------------------------------------------------
+// What all 64 lanes have, put together by `op` (commutative): every lane gets the same bits.  Lanes are exchanged within 4, 8 and 16,
+// then rows of 16 and halves of 32 change places.
+template <typename V, typename Op>
+__device__ inline V over_wave(V v, Op op) {
+  constexpr int kWords = sizeof(V) / 4;
+  auto moved = [&](auto control) {
+    uint32_t w[kWords];
+    __builtin_memcpy(w, &v, sizeof v);
+#pragma unroll
+    for (int k = 0; k < kWords; ++k) w[k] = (uint32_t)__builtin_amdgcn_mov_dpp((int)w[k], decltype(control)::value, 0xf, 0xf, true);
+    V o;
+    __builtin_memcpy(&o, w, sizeof o);
+    return o;
+  };
+  v = op(v, moved(std::integral_constant<int, 0xb1>{}));           // lane ^ 1
+  v = op(v, moved(std::integral_constant<int, 0x4e>{}));           // lane ^ 2
+  v = op(v, moved(std::integral_constant<int, 0x141>{}));          // 7 - lane, of 8
+  v = op(v, moved(std::integral_constant<int, 0x140>{}));          // 15 - lane, of 16
+  auto halves = [&](auto swap) {
+    uint32_t w[kWords], a[kWords], b[kWords];
+    __builtin_memcpy(w, &v, sizeof v);
+#pragma unroll
+    for (int k = 0; k < kWords; ++k) {
+      const auto r = swap(w[k]);
+      a[k] = r[0], b[k] = r[1];
+    }
+    V x, y;
+    __builtin_memcpy(&x, a, sizeof x);
+    __builtin_memcpy(&y, b, sizeof y);
+    return op(x, y);
+  };
+  v = halves([](uint32_t w) { return __builtin_amdgcn_permlane16_swap(w, w, false, false); });
+  return halves([](uint32_t w) { return __builtin_amdgcn_permlane32_swap(w, w, false, false); });
+}
+struct Plus { template <typename V> __device__ V operator()(V a, V b) const { return a + b; } };
+struct Larger { __device__ float operator()(float a, float b) const { return __builtin_elementwise_maximum(a, b); } };     // NaN if one is
 
 // ---------------------------------------------------------------------------
 // launches
@@ -267,7 +309,12 @@ struct Strips {
   __device__ static inline int row(int piece, int lane) {
     return (piece / per_wave / WI * FJ + piece / turns % FJ) * 32 + piece % turns * rows + lane / lanes;
   }
-  __device__ static inline int place(int row, int chunk) { return (row * chunks + (chunk ^ (row & (chunks - 1)))) * 16; }
+  // A lane that takes two chunks back finds the even ones in the first half of a row and the odd ones in the second: neighbouring
+  // lanes read neighbouring places.
+  __device__ static inline int place(int row, int chunk) {
+    const int at = N == 4 ? chunk : (chunk >> 1) + (chunk & 1) * (chunks / 2);
+    return (row * chunks + (at ^ (row & (chunks - 1)))) * 16;
+  }
   __device__ static inline void put(lds_char* strip, int k, const f32x16& block, int lane) {
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
@@ -286,14 +333,9 @@ struct Strips {
       const s16x8 x = *reinterpret_cast<const lds_s16x8*>(strip + place(row, u));
       __builtin_memcpy(v, &x, 16);
     } else {
-      const int second = (u >> 2 ^ u >> 3) & 1;           // which of the two is read first
-      const s16x8 x = *reinterpret_cast<const lds_s16x8*>(strip + place(row, 2 * u + second));
-      const s16x8 y = *reinterpret_cast<const lds_s16x8*>(strip + place(row, 2 * u + 1 - second));
-      float p[4], q[4];
-      __builtin_memcpy(p, &x, 16);
-      __builtin_memcpy(q, &y, 16);
-#pragma unroll
-      for (int c = 0; c < 4; ++c) v[c] = second ? q[c] : p[c], v[4 + c] = second ? p[c] : q[c];
+      const s16x8 x = *reinterpret_cast<const lds_s16x8*>(strip + place(row, 2 * u)), y = *reinterpret_cast<const lds_s16x8*>(strip + place(row, 2 * u + 1));
+      __builtin_memcpy(v, &x, 16);
+      __builtin_memcpy(v + 4, &y, 16);
     }
   }
 };
