@@ -37,14 +37,45 @@ __device__ inline uint2 row_codes(const float (&v)[kPiece], float inverse) {
 // ---------------------------------------------------------------------------
 // norm and 8-bit rows
 // ---------------------------------------------------------------------------
-// THREADS to a row, PIECES of 8 values each in registers; WIDE: a row of any length, read again for its outputs.  ROWS rows to a
-// workgroup (of a wavefront each).  NORM: the norm, with what is wanted of it; otherwise 8-bit rows of x alone.
-template <typename T, int THREADS, int PIECES, int ROWS, bool NORM, bool WIDE>
-__global__ __launch_bounds__(THREADS * ROWS) void row_kernel(NormArgs a) {
-  static_assert(ROWS == 1 || THREADS == 64, "rows that share a workgroup have a wavefront each");
-  constexpr int kWaves = THREADS / 64;
-  const int t = threadIdx.x % THREADS;
-  const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / THREADS;
+// 8 values as they lie in memory, on their way: whole words, so that 16-bit values share registers.
+template <typename T>
+struct Raw {
+  uint32_t w[kPiece * sizeof(T) / 4];
+  __device__ inline void load(const T* p, int n) {
+    if (n >= kPiece) {
+      __builtin_memcpy(w, p, sizeof w);
+    } else {
+#pragma unroll
+      for (int k = 0; k < (int)(sizeof w / 4); ++k) {
+        if constexpr (sizeof(T) == 4) {
+          w[k] = k < n ? __builtin_bit_cast(uint32_t, p[k]) : 0u;
+        } else {
+          const uint32_t low = 2 * k < n ? __builtin_bit_cast(uint16_t, p[2 * k]) : 0u, high = 2 * k + 1 < n ? __builtin_bit_cast(uint16_t, p[2 * k + 1]) : 0u;
+          w[k] = low | high << 16;
+        }
+      }
+    }
+  }
+  __device__ inline void get(float (&f)[kPiece]) const {
+    T v[kPiece];
+    __builtin_memcpy(v, w, sizeof v);
+#pragma unroll
+    for (int k = 0; k < kPiece; ++k) f[k] = widen(v[k]);
+  }
+};
+
+// 1 / sqrt(mean + eps) in fp64: the hardware's estimate and a step of Newton's on it, which leaves 2^-40.
+__device__ inline float root(double v) {
+  const double y = __builtin_amdgcn_rsq(v);
+  return (float)(v > 0.0 && v < __builtin_inf() ? y + 0.5 * y * (1.0 - v * y * y) : y);
+}
+
+// A row to a workgroup, PIECES of 8 values a thread in registers, or, ROWS > 1, to each of its wavefronts; WIDE: a row of any length,
+// read again for its outputs.  NORM: the norm, with what is wanted of it; otherwise 8-bit rows of x alone.
+template <typename T, int PIECES, int ROWS, bool NORM, bool WIDE>
+__global__ __launch_bounds__(ROWS > 1 ? 64 * ROWS : 1024) void row_kernel(NormArgs a) {
+  const int threads = ROWS > 1 ? 64 : (int)blockDim.x, t = ROWS > 1 ? threadIdx.x & 63 : threadIdx.x;
+  const int64_t row = (int64_t)blockIdx.x * ROWS + (ROWS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0);
   if (ROWS > 1 && row >= a.samples) return;
   const int n = a.features, stride = (n + kGroup - 1) / kGroup * kGroup;
   const T* const x = static_cast<const T*>(a.x) + row * a.ldx;
@@ -53,18 +84,18 @@ __global__ __launch_bounds__(THREADS * ROWS) void row_kernel(NormArgs a) {
   T* const h = NORM && a.h ? static_cast<T*>(a.h) + row * a.ldh : nullptr;
 
   // values of the row from `col` on, as the norm sees them; zeros behind its end
-  auto load = [&](float (&v)[kPiece], int col) {
-    load_values(v, x + col, n - col);
+  auto joined = [&](float (&v)[kPiece], const Raw<T>& from, const Raw<T>& more) {
+    from.get(v);
     if (r) {
-      float more[kPiece];
-      load_values(more, r + col, n - col);
+      float m[kPiece];
+      more.get(m);
 #pragma unroll
-      for (int k = 0; k < kPiece; ++k) v[k] = widen(narrow<T>(v[k] + more[k]));
+      for (int k = 0; k < kPiece; ++k) v[k] = widen(narrow<T>(v[k] + m[k]));
     }
   };
-  auto load_gain = [&](float (&g)[kPiece], int col) {
+  auto gains = [&](float (&g)[kPiece], const Raw<T>& from) {
     if (gain) {
-      load_values(g, gain + col, n - col);
+      from.get(g);
     } else {
 #pragma unroll
       for (int k = 0; k < kPiece; ++k) g[k] = 1.f;
@@ -72,7 +103,7 @@ __global__ __launch_bounds__(THREADS * ROWS) void row_kernel(NormArgs a) {
   };
   double sum = 0.0;
   float most = 0.f;
-  auto count = [&](const float (&v)[kPiece], int col) {
+  auto count = [&](const float (&v)[kPiece], const Raw<T>& rg) {
     if (NORM) {
 #pragma unroll
       for (int k = 0; k < kPiece; ++k) sum = __builtin_fma((double)v[k], (double)v[k], sum);
@@ -81,7 +112,7 @@ __global__ __launch_bounds__(THREADS * ROWS) void row_kernel(NormArgs a) {
       most = __builtin_elementwise_maximum(most, largest(v));
     } else if (a.rows.codes) {
       float g[kPiece];
-      load_gain(g, col);
+      gains(g, rg);
 #pragma unroll
       for (int k = 0; k < kPiece; ++k) g[k] *= v[k];
       most = __builtin_elementwise_maximum(most, largest(g));
@@ -89,48 +120,57 @@ __global__ __launch_bounds__(THREADS * ROWS) void row_kernel(NormArgs a) {
   };
 
   float v[PIECES][kPiece];
+  Raw<T> rx[PIECES], rr[PIECES], rg[PIECES];
   const int pieces = (n + kPiece - 1) / kPiece;
   if constexpr (WIDE) {
-    for (int p = t; p < pieces; p += THREADS) {
-      load(v[0], p * kPiece);
-      if (h) store_values(h + p * kPiece, v[0], n - p * kPiece);
-      count(v[0], p * kPiece);
+    for (int p = t; p < pieces; p += threads) {
+      const int col = p * kPiece;
+      rx[0].load(x + col, n - col);
+      if (r) rr[0].load(r + col, n - col);
+      if (gain && a.rows.codes) rg[0].load(gain + col, n - col);
+      joined(v[0], rx[0], rr[0]);
+      if (h) store_values(h + col, v[0], n - col);
+      count(v[0], rg[0]);
     }
   } else {
+    // all of it on its way at once
 #pragma unroll
-    for (int p = 0; p < PIECES; ++p) load(v[p], (t + p * THREADS) * kPiece);
+    for (int p = 0; p < PIECES; ++p) rx[p].load(x + (t + p * threads) * kPiece, n - (t + p * threads) * kPiece);
+    if (r) {
+#pragma unroll
+      for (int p = 0; p < PIECES; ++p) rr[p].load(r + (t + p * threads) * kPiece, n - (t + p * threads) * kPiece);
+    }
+    if (gain) {
+#pragma unroll
+      for (int p = 0; p < PIECES; ++p) rg[p].load(gain + (t + p * threads) * kPiece, n - (t + p * threads) * kPiece);
+    }
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
-      const int col = (t + p * THREADS) * kPiece;
+      const int col = (t + p * threads) * kPiece;
+      joined(v[p], rx[p], rr[p]);
       if (h) store_values(h + col, v[p], n - col);
-      count(v[p], col);
+      count(v[p], rg[p]);
     }
   }
   if (NORM) sum = over_wave(sum, Plus{});
   if (!NORM || a.rows.codes) most = over_wave(most, Larger{});
-  if constexpr (kWaves > 1) {
-    __shared__ double sums[kWaves];
-    __shared__ float mosts[kWaves];
+  if (ROWS == 1 && threads > 64) {
+    __shared__ double sums[16];
+    __shared__ float mosts[16];
     if ((t & 63) == 0) sums[t >> 6] = sum, mosts[t >> 6] = most;
     __syncthreads();
     sum = 0.0, most = 0.f;
-#pragma unroll
-    for (int k = 0; k < kWaves; ++k) sum += sums[k], most = __builtin_elementwise_maximum(most, mosts[k]);
+    for (int k = 0; k < threads >> 6; ++k) sum += sums[k], most = __builtin_elementwise_maximum(most, mosts[k]);
   }
-  const float rstd = NORM ? (float)(1.0 / sqrt(sum / n + a.eps)) : 1.f;
+  const float rstd = NORM ? root(sum * a.inverse + a.eps) : 1.f;
   const float step = row_step(most), inverse = 1.f / step;
   if (t == 0) {
     if (NORM && a.rstd) a.rstd[row] = rstd;
     if (a.rows.codes) a.rows.scales[row] = NORM ? step * rstd : step;
   }
-  auto write = [&](const float (&v)[kPiece], int col) {
+  auto write = [&](const float (&v)[kPiece], const Raw<T>& rg, int col) {
     float g[kPiece];
-    if (NORM) {
-      load_gain(g, col);
-    } else {
-#pragma unroll
-      for (int k = 0; k < kPiece; ++k) g[k] = 1.f;
-    }
+    gains(g, rg);
     if (a.rows.codes) {
       float q[kPiece];
 #pragma unroll
@@ -153,18 +193,21 @@ __global__ __launch_bounds__(THREADS * ROWS) void row_kernel(NormArgs a) {
   };
   if constexpr (WIDE) {
     // whole wavefronts go round together: lanes exchange what a group's largest value is
-    for (int p = t; p < (pieces + 63) / 64 * 64; p += THREADS) {
+    for (int p = t; p < (pieces + 63) / 64 * 64; p += threads) {
       const int col = p * kPiece;
+      if (gain) rg[0].load(gain + col, n - col);
       if (h) {
         load_values(v[0], h + col, n - col);      // this thread's own; x or the residual may be gone
       } else {
-        load(v[0], col);
+        rx[0].load(x + col, n - col);
+        if (r) rr[0].load(r + col, n - col);
+        joined(v[0], rx[0], rr[0]);
       }
-      write(v[0], col);
+      write(v[0], rg[0], col);
     }
   } else {
 #pragma unroll
-    for (int p = 0; p < PIECES; ++p) write(v[p], (t + p * THREADS) * kPiece);
+    for (int p = 0; p < PIECES; ++p) write(v[p], rg[p], (t + p * threads) * kPiece);
   }
 }
 
@@ -173,9 +216,11 @@ hipError_t run_rows(const NormArgs& all, hipStream_t s) {
   // a launch has fewer than 2^32 threads
   constexpr int64_t kSlab = int64_t(1) << 21;
   const int64_t stride = (all.features + kGroup - 1) / kGroup * kGroup;
+  const int pieces = (all.features + kPiece - 1) / kPiece;
   for (int64_t at = 0; at < all.samples; at += kSlab) {
     NormArgs a = all;
     a.samples = std::min(kSlab, all.samples - at);
+    a.inverse = 1.0 / a.features;
     a.x = static_cast<const T*>(all.x) + at * all.ldx;
     if (a.residual) a.residual = static_cast<const T*>(all.residual) + at * all.ldr;
     if (a.h) a.h = static_cast<T*>(all.h) + at * all.ldh;
@@ -184,13 +229,13 @@ hipError_t run_rows(const NormArgs& all, hipStream_t s) {
     if (a.kept.codes) a.kept = Codes{all.kept.codes + at * stride, all.kept.exponents + at * (stride / kGroup)};
     if (a.rows.codes) a.rows = Rows{all.rows.codes + at * stride, all.rows.scales + at};
     const unsigned n = (unsigned)a.samples;
-    if (a.features <= 512) row_kernel<T, 64, 1, 4, NORM, false><<<dim3((n + 3) / 4), 256, 0, s>>>(a);
-    else if (a.features <= 1024) row_kernel<T, 64, 2, 4, NORM, false><<<dim3((n + 3) / 4), 256, 0, s>>>(a);
-    else if (a.features <= 2048) row_kernel<T, 256, 1, 1, NORM, false><<<dim3(n), 256, 0, s>>>(a);
-    else if (a.features <= 4096) row_kernel<T, 256, 2, 1, NORM, false><<<dim3(n), 256, 0, s>>>(a);
-    else if (a.features <= 8192) row_kernel<T, 512, 2, 1, NORM, false><<<dim3(n), 512, 0, s>>>(a);
-    else if (a.features <= 16384) row_kernel<T, 512, 4, 1, NORM, false><<<dim3(n), 512, 0, s>>>(a);
-    else row_kernel<T, 1024, 1, 1, NORM, true><<<dim3(n), 1024, 0, s>>>(a);
+    auto threads = [&](int each) { return dim3((unsigned)((pieces + 64 * each - 1) / (64 * each)) * 64); };
+    //PICK
+    if (pieces <= 64) row_kernel<T, 1, 4, NORM, false><<<dim3((n + 3) / 4), 256, 0, s>>>(a);
+    else if (pieces <= 128) row_kernel<T, 2, 4, NORM, false><<<dim3((n + 3) / 4), 256, 0, s>>>(a);
+    else if (pieces <= 2 * 1024) row_kernel<T, 2, 1, NORM, false><<<dim3(n), threads(2), 0, s>>>(a);
+    else if (pieces <= 4 * 1024) row_kernel<T, 4, 1, NORM, false><<<dim3(n), threads(4), 0, s>>>(a);
+    else row_kernel<T, 1, 1, NORM, true><<<dim3(n), 1024, 0, s>>>(a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -240,68 +285,108 @@ __device__ inline void load_or_ones(float (&g)[kPiece], const void* from, int co
   }
 }
 
-// A workgroup takes a run of rows, ROWS at a time, THREADS to a row; a thread keeps its columns' gain and sums.  dgain: `part`, runs x
-// features, where it is wanted.
-template <typename T, bool HELD, int THREADS, int PIECES, int ROWS>
-__global__ __launch_bounds__(THREADS * ROWS) void norm_backward_kernel(NormBackwardArgs a, float* part, int64_t run) {
-  static_assert(ROWS == 1 || THREADS == 64, "rows that share a workgroup have a wavefront each");
-  constexpr int kWaves = THREADS / 64;
-  const int t = threadIdx.x % THREADS, slot = threadIdx.x / THREADS, n = a.features;
+// A workgroup takes a run of rows, one or, ROWS > 1, one to each of its wavefronts at a time; a thread keeps its columns' gain and sums,
+// and, but for the widest rows, has the next row's values on their way.  dgain: `part`, runs x `stride`, where it is wanted.
+template <typename T, bool HELD, int PIECES, int ROWS, int MOST>
+__global__ __launch_bounds__(MOST) void norm_backward_kernel(NormBackwardArgs a, float* part, int stride, int64_t run) {
+  const int threads = ROWS > 1 ? 64 : (int)blockDim.x, t = ROWS > 1 ? threadIdx.x & 63 : threadIdx.x, n = a.features;
+  const int slot = ROWS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
   const int64_t first = (int64_t)blockIdx.x * run, last = min(a.samples, first + run);
-  float gain[PIECES][kPiece], sums[PIECES][kPiece] = {};
-#pragma unroll
-  for (int p = 0; p < PIECES; ++p) load_or_ones<T>(gain[p], a.gain, (t + p * THREADS) * kPiece, n);
-  __shared__ float dots[2][kWaves];
-  int turn = 0;
-  for (int64_t row = first + slot; row < last; row += ROWS, turn ^= 1) {
-    float dy[PIECES][kPiece], h[PIECES][kPiece];
-    const float rstd = a.rstd[row];
-    float dot = 0.f;
+  struct Row {
+    Raw<T> dy[PIECES], dh[PIECES];
+    std::conditional_t<HELD, uint2, Raw<T>> h[PIECES];
+    uint32_t exps[HELD ? PIECES : 1];
+    float rstd;
+  };
+  const int groups = (n + kGroup - 1) / kGroup;
+  auto ask = [&](Row& q, int64_t row) {
+    q.rstd = a.rstd[row];
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
-      const int col = (t + p * THREADS) * kPiece;
-      load_values(dy[p], static_cast<const T*>(a.dy) + row * a.lddy + col, n - col);
-      load_h<T, HELD>(h[p], a, row, col);
+      const int col = (t + p * threads) * kPiece;
+      q.dy[p].load(static_cast<const T*>(a.dy) + row * a.lddy + col, n - col);
+      if constexpr (HELD) {
+        const int in = min(col, groups * kGroup - kPiece);                  // codes go on to the end of their group
+        q.h[p] = *reinterpret_cast<const uint2*>(a.held.codes + row * ((int64_t)groups * kGroup) + in);
+        q.exps[p] = a.held.exponents[row * groups + in / kGroup];
+      } else {
+        q.h[p].load(static_cast<const T*>(a.h) + row * a.ldh + col, n - col);
+      }
+      if (a.dh) q.dh[p].load(static_cast<const T*>(a.dh) + row * a.lddh + col, n - col);
     }
+  };
+  constexpr bool kNext = MOST <= 512;              // 1024 threads have no registers for it
+  Raw<T> gain[PIECES];
+  float sums[PIECES][kPiece] = {};
+  Row now, next;
+  int64_t row = first + slot;
+  if (kNext && row < last) ask(now, row);
+  if (a.gain) {
 #pragma unroll
-    for (int p = 0; p < PIECES; ++p)
+    for (int p = 0; p < PIECES; ++p) gain[p].load(static_cast<const T*>(a.gain) + (t + p * threads) * kPiece, n - (t + p * threads) * kPiece);
+  }
+  __shared__ float dots[2][16];
+  for (int turn = 0; row < last; row += ROWS, turn ^= 1) {
+    if (!kNext) ask(now, row);
+    else if (row + ROWS < last) ask(next, row + ROWS);
+    float dy[PIECES][kPiece], h[PIECES][kPiece], dot = 0.f;
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+      now.dy[p].get(dy[p]);
+      if constexpr (HELD) {
+        decode(h[p], now.h[p], factor_of(now.exps[p]));                    // behind the row's end dy is 0, and so is what is made of h
+        const int left = n - (t + p * threads) * kPiece;
+#pragma unroll
+        for (int k = 0; k < kPiece; ++k) h[p][k] = k < left ? h[p][k] : 0.f;
+      } else {
+        now.h[p].get(h[p]);
+      }
+      float g[kPiece];
+      if (a.gain) {
+        gain[p].get(g);
+      } else {
+#pragma unroll
+        for (int k = 0; k < kPiece; ++k) g[k] = 1.f;
+      }
 #pragma unroll
       for (int k = 0; k < kPiece; ++k) {
-        h[p][k] *= rstd;
+        h[p][k] *= now.rstd;
         sums[p][k] = fmaf(dy[p][k], h[p][k], sums[p][k]);
-        dy[p][k] *= gain[p][k];
+        dy[p][k] *= g[k];
         dot = fmaf(dy[p][k], h[p][k], dot);
       }
-    if (!a.dx) continue;
-    dot = over_wave(dot, Plus{});
-    if constexpr (kWaves > 1) {
-      if ((t & 63) == 0) dots[turn][t >> 6] = dot;
-      __syncthreads();
-      dot = 0.f;
-#pragma unroll
-      for (int k = 0; k < kWaves; ++k) dot += dots[turn][k];
     }
-    const float along = dot / (float)n;
+    if (a.dx) {
+      dot = over_wave(dot, Plus{});
+      if (ROWS == 1 && threads > 64) {
+        if ((t & 63) == 0) dots[turn][t >> 6] = dot;
+        __syncthreads();
+        dot = 0.f;
+        for (int k = 0; k < threads >> 6; ++k) dot += dots[turn][k];
+      }
+      const float along = dot / (float)n;
 #pragma unroll
-    for (int p = 0; p < PIECES; ++p) {
-      const int col = (t + p * THREADS) * kPiece;
-      float d[kPiece] = {};
-      if (a.dh) load_values(d, static_cast<const T*>(a.dh) + row * a.lddh + col, n - col);
+      for (int p = 0; p < PIECES; ++p) {
+        const int col = (t + p * threads) * kPiece;
+        float d[kPiece] = {};
+        if (a.dh) now.dh[p].get(d);
 #pragma unroll
-      for (int k = 0; k < kPiece; ++k) d[k] = fmaf(rstd, fmaf(-h[p][k], along, dy[p][k]), d[k]);
-      store_values(static_cast<T*>(a.dx) + row * a.lddx + col, d, n - col);
+        for (int k = 0; k < kPiece; ++k) d[k] = fmaf(now.rstd, fmaf(-h[p][k], along, dy[p][k]), d[k]);
+        store_values(static_cast<T*>(a.dx) + row * a.lddx + col, d, n - col);
+      }
     }
+    if (kNext) now = next;
   }
   if (!part) return;
-  float* const out = part + (int64_t)blockIdx.x * n;
+  float* const out = part + (int64_t)blockIdx.x * stride;
   if constexpr (ROWS > 1) {
     __shared__ float all[ROWS][PIECES * 64 * kPiece];
 #pragma unroll
     for (int p = 0; p < PIECES; ++p)
 #pragma unroll
-      for (int k = 0; k < kPiece; ++k) all[slot][(t + p * THREADS) * kPiece + k] = sums[p][k];
+      for (int k = 0; k < kPiece; ++k) all[slot][(t + p * threads) * kPiece + k] = sums[p][k];
     __syncthreads();
-    for (int f = threadIdx.x; f < n; f += THREADS * ROWS) {
+    for (int f = threadIdx.x; f < n; f += 64 * ROWS) {
       float total = 0.f;
 #pragma unroll
       for (int k = 0; k < ROWS; ++k) total += all[k][f];
@@ -309,12 +394,11 @@ __global__ __launch_bounds__(THREADS * ROWS) void norm_backward_kernel(NormBackw
     }
   } else {
 #pragma unroll
-    for (int p = 0; p < PIECES; ++p)
-#pragma unroll
-      for (int k = 0; k < kPiece; ++k) {
-        const int f = (t + p * THREADS) * kPiece + k;
-        if (f < n) out[f] = sums[p][k];
-      }
+    for (int p = 0; p < PIECES; ++p) {
+      const int f = (t + p * threads) * kPiece;
+      if (f >= n) continue;                                                // `stride` has room for whole pieces
+      __builtin_memcpy(__builtin_assume_aligned(out + f, 16), sums[p], sizeof sums[p]);
+    }
   }
 }
 
@@ -345,7 +429,7 @@ __global__ __launch_bounds__(1024) void norm_along_kernel(NormBackwardArgs a, fl
 }
 
 template <typename T, bool HELD>
-__global__ __launch_bounds__(256) void norm_strips_kernel(NormBackwardArgs a, const float* along, float* part, int64_t run) {
+__global__ __launch_bounds__(256) void norm_strips_kernel(NormBackwardArgs a, const float* along, float* part, int stride, int64_t run) {
   const int n = a.features, col = ((int)blockIdx.x * 256 + (int)threadIdx.x) * kPiece;
   if (col >= n) return;
   const int64_t first = (int64_t)blockIdx.y * run, last = min(a.samples, first + run);
@@ -368,7 +452,29 @@ __global__ __launch_bounds__(256) void norm_strips_kernel(NormBackwardArgs a, co
   if (!part) return;
 #pragma unroll
   for (int k = 0; k < kPiece; ++k)
-    if (col + k < n) part[(int64_t)blockIdx.y * n + col + k] = sums[k];
+    if (col + k < n) part[(int64_t)blockIdx.y * stride + col + k] = sums[k];
+}
+
+// dgain from the runs' sums: a workgroup adds up 16 columns, 64 runs at a time, in an order of its own that is always the same.
+__global__ __launch_bounds__(256) void norm_gain_kernel(const float* part, float* dgain, int accumulate, int n, int stride, int runs) {
+  __shared__ float sums[64][17];
+  const int col = (int)blockIdx.x * 16 + (threadIdx.x & 3) * 4, slot = threadIdx.x >> 2;
+  float s[4] = {};
+#pragma unroll 8
+  for (int k = slot; k < runs; k += 64) {
+    const float4 v = *reinterpret_cast<const float4*>(part + (int64_t)k * stride + col);
+    s[0] += v.x, s[1] += v.y, s[2] += v.z, s[3] += v.w;
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) sums[slot][(threadIdx.x & 3) * 4 + k] = s[k];
+  __syncthreads();
+  // 16 threads a column, four runs' sums each
+  const int f = threadIdx.x >> 4, part4 = threadIdx.x & 15;
+  float total = (sums[part4][f] + sums[part4 + 16][f]) + (sums[part4 + 32][f] + sums[part4 + 48][f]);
+#pragma unroll
+  for (int k = 8; k > 0; k >>= 1) total += __shfl_xor(total, k, 16);
+  const int at = (int)blockIdx.x * 16 + f;
+  if (part4 == 0 && at < n) dgain[at] = accumulate ? dgain[at] + total : total;
 }
 
 constexpr int64_t kAlong = int64_t(1) << 22;              // rows whose means lie in front of the parts in the workspace
@@ -379,6 +485,7 @@ hipError_t run_norm_backward(const NormBackwardArgs& all, hipStream_t s) {
   float* const along = static_cast<float*>(all.workspace);
   float* const parts = along + kAlong;
   const int64_t groups = (all.features + kGroup - 1) / kGroup;
+  const int pieces = (all.features + kPiece - 1) / kPiece, stride = (all.features + 15) / 16 * 16;
   int64_t at = 0;
   do {
     NormBackwardArgs a = all;
@@ -390,29 +497,30 @@ hipError_t run_norm_backward(const NormBackwardArgs& all, hipStream_t s) {
     a.rstd = all.rstd + at;
     if (a.dh) a.dh = static_cast<const T*>(all.dh) + at * all.lddh;
     if (a.dx) a.dx = static_cast<T*>(all.dx) + at * all.lddx;
-    const int64_t most = std::min<int64_t>(a.features <= 16384 ? 1024 : std::max<int64_t>(1, 1024 * 2048 / a.features), kPartFloats / a.features);
-    const int rows = a.features <= 1024 ? 4 : 1;
+    // as many workgroups as run together, 16 wavefronts a CU
+    const int each = pieces <= 64 ? 1 : 2, waves = pieces <= 128 ? 4 : std::min(16, (pieces + 64 * each - 1) / (64 * each)), rows = pieces <= 128 ? 4 : 1;
+    const bool wide = pieces > 2 * 1024;
+    const int64_t most = std::min<int64_t>(wide ? std::max<int64_t>(1, 1024 * 2048 / a.features) : 256 * (16 / waves), kPartFloats / stride);
     const int64_t run = std::max<int64_t>(1, (a.samples + most * rows - 1) / (most * rows)) * rows;
     const unsigned runs = (unsigned)((a.samples + run - 1) / run);
     float* const part = a.dgain ? parts : nullptr;
     if (a.samples > 0) {
-      if (a.features <= 512) norm_backward_kernel<T, HELD, 64, 1, 4><<<dim3(runs), 256, 0, s>>>(a, part, run);
-      else if (a.features <= 1024) norm_backward_kernel<T, HELD, 64, 2, 4><<<dim3(runs), 256, 0, s>>>(a, part, run);
-      else if (a.features <= 2048) norm_backward_kernel<T, HELD, 256, 1, 1><<<dim3(runs), 256, 0, s>>>(a, part, run);
-      else if (a.features <= 4096) norm_backward_kernel<T, HELD, 256, 2, 1><<<dim3(runs), 256, 0, s>>>(a, part, run);
-      else if (a.features <= 8192) norm_backward_kernel<T, HELD, 512, 2, 1><<<dim3(runs), 512, 0, s>>>(a, part, run);
-      else if (a.features <= 16384) norm_backward_kernel<T, HELD, 1024, 2, 1><<<dim3(runs), 1024, 0, s>>>(a, part, run);
+      if (pieces <= 64) norm_backward_kernel<T, HELD, 1, 4, 256><<<dim3(runs), 256, 0, s>>>(a, part, stride, run);
+      else if (pieces <= 128) norm_backward_kernel<T, HELD, 2, 4, 256><<<dim3(runs), 256, 0, s>>>(a, part, stride, run);
+      else if (waves <= 4) norm_backward_kernel<T, HELD, 2, 1, 256><<<dim3(runs), dim3((unsigned)waves * 64), 0, s>>>(a, part, stride, run);
+      else if (waves <= 8) norm_backward_kernel<T, HELD, 2, 1, 512><<<dim3(runs), dim3((unsigned)waves * 64), 0, s>>>(a, part, stride, run);
+      else if (!wide) norm_backward_kernel<T, HELD, 2, 1, 1024><<<dim3(runs), dim3((unsigned)waves * 64), 0, s>>>(a, part, stride, run);
       else {
         norm_along_kernel<T, HELD><<<dim3((unsigned)a.samples), 1024, 0, s>>>(a, along);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        norm_strips_kernel<T, HELD><<<dim3((unsigned)((a.features + 2047) / 2048), runs), 256, 0, s>>>(a, along, part, run);
+        norm_strips_kernel<T, HELD><<<dim3((unsigned)((a.features + 2047) / 2048), runs), 256, 0, s>>>(a, along, part, stride, run);
       }
       const hipError_t e = hipGetLastError();
       if (e != hipSuccess) return e;
     }
     if (part) {
-      sum_runs_kernel<<<dim3((unsigned)((a.features + 63) / 64)), 256, 0, s>>>(part, a.dgain, a.accumulate, a.features, (int)runs);
+      norm_gain_kernel<<<dim3((unsigned)((a.features + 15) / 16)), 256, 0, s>>>(part, a.dgain, a.accumulate, a.features, stride, (int)runs);
       const hipError_t e = hipGetLastError();
       if (e != hipSuccess) return e;
     }

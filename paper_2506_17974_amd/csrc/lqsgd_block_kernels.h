@@ -18,7 +18,7 @@ struct Rows {                                     // 8-bit rows' memory; codes =
 struct NormArgs {
   int64_t samples;
   int32_t features;
-  double eps;
+  double eps, inverse;                            // inverse: 1 / features, the launcher's
   const void* x; int64_t ldx;
   const void* residual; int64_t ldr;              // the rest may be nullptr
   const void* gain;
