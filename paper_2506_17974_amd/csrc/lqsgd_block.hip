@@ -41,9 +41,20 @@ __device__ inline uint2 row_codes(const float (&v)[kPiece], float inverse) {
 template <typename T>
 struct Raw {
   uint32_t w[kPiece * sizeof(T) / 4];
+  // PAST: past the caches.
+  template <bool PAST = false>
   __device__ inline void load(const T* p, int n) {
     if (n >= kPiece) {
-      __builtin_memcpy(w, p, sizeof w);
+      if constexpr (PAST) {
+        typedef uint32_t Words __attribute__((ext_vector_type(4), aligned(1)));
+#pragma unroll
+        for (int k = 0; k < (int)(sizeof w / 16); ++k) {
+          const Words v = __builtin_nontemporal_load(reinterpret_cast<const Words*>(p) + k);
+          __builtin_memcpy(w + 4 * k, &v, 16);
+        }
+      } else {
+        __builtin_memcpy(w, p, sizeof w);
+      }
     } else {
 #pragma unroll
       for (int k = 0; k < (int)(sizeof w / 4); ++k) {
@@ -71,8 +82,11 @@ __device__ inline float root(double v) {
 }
 
 // A row to a workgroup, PIECES of 8 values a thread in registers, or, ROWS > 1, to each of its wavefronts; WIDE: a row of any length,
-// read again for its outputs.  NORM: the norm, with what is wanted of it; otherwise 8-bit rows of x alone.
-template <typename T, int PIECES, int ROWS, bool NORM, bool WIDE>
+// read again for its outputs.  NORM: the norm, with what is wanted of it; otherwise 8-bit rows of x alone.  PAST: inputs past the caches.
+// Bound by memory: 8192 x 4096 bfloat16 norm with residual, checkpoint and h 53 us (5.7 TB/s), with 8-bit rows instead 42 (5.6), rows alone 18 (5.6).
+// Tried: workgroups that stay, keep the gain and have the next row on their way (norm alone 25 -> 29 us, single rows 0.2 us more: fewer
+// wavefronts fit).
+template <typename T, int PIECES, int ROWS, bool NORM, bool WIDE, bool PAST>
 __global__ __launch_bounds__(ROWS > 1 ? 64 * ROWS : 1024) void row_kernel(NormArgs a) {
   const int threads = ROWS > 1 ? 64 : (int)blockDim.x, t = ROWS > 1 ? threadIdx.x & 63 : threadIdx.x;
   const int64_t row = (int64_t)blockIdx.x * ROWS + (ROWS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0);
@@ -135,10 +149,10 @@ __global__ __launch_bounds__(ROWS > 1 ? 64 * ROWS : 1024) void row_kernel(NormAr
   } else {
     // all of it on its way at once
 #pragma unroll
-    for (int p = 0; p < PIECES; ++p) rx[p].load(x + (t + p * threads) * kPiece, n - (t + p * threads) * kPiece);
+    for (int p = 0; p < PIECES; ++p) rx[p].template load<PAST>(x + (t + p * threads) * kPiece, n - (t + p * threads) * kPiece);
     if (r) {
 #pragma unroll
-      for (int p = 0; p < PIECES; ++p) rr[p].load(r + (t + p * threads) * kPiece, n - (t + p * threads) * kPiece);
+      for (int p = 0; p < PIECES; ++p) rr[p].template load<PAST>(r + (t + p * threads) * kPiece, n - (t + p * threads) * kPiece);
     }
     if (gain) {
 #pragma unroll
@@ -211,7 +225,11 @@ __global__ __launch_bounds__(ROWS > 1 ? 64 * ROWS : 1024) void row_kernel(NormAr
   }
 }
 
-template <typename T, bool NORM>
+// Inputs of this size and more are read past the caches (bfloat16 8192 x 4096: norm with residual and checkpoint 58.8 -> 53.3 us, backward 65.6 ->
+// 59.8, rows 19.7 -> 18.1; of half the size the norm 25.4 -> 30.2), but not by the norm of a single input (25.6 -> 29.5).
+constexpr int64_t kPastBytes = int64_t(1) << 26;
+
+template <typename T, bool NORM, bool PAST>
 hipError_t run_rows(const NormArgs& all, hipStream_t s) {
   // a launch has fewer than 2^32 threads
   constexpr int64_t kSlab = int64_t(1) << 21;
@@ -230,16 +248,22 @@ hipError_t run_rows(const NormArgs& all, hipStream_t s) {
     if (a.rows.codes) a.rows = Rows{all.rows.codes + at * stride, all.rows.scales + at};
     const unsigned n = (unsigned)a.samples;
     auto threads = [&](int each) { return dim3((unsigned)((pieces + 64 * each - 1) / (64 * each)) * 64); };
-    //PICK
-    if (pieces <= 64) row_kernel<T, 1, 4, NORM, false><<<dim3((n + 3) / 4), 256, 0, s>>>(a);
-    else if (pieces <= 128) row_kernel<T, 2, 4, NORM, false><<<dim3((n + 3) / 4), 256, 0, s>>>(a);
-    else if (pieces <= 2 * 1024) row_kernel<T, 2, 1, NORM, false><<<dim3(n), threads(2), 0, s>>>(a);
-    else if (pieces <= 4 * 1024) row_kernel<T, 4, 1, NORM, false><<<dim3(n), threads(4), 0, s>>>(a);
-    else row_kernel<T, 1, 1, NORM, true><<<dim3(n), 1024, 0, s>>>(a);
+    // the norm by one piece a thread where that goes: the more wavefronts, the sooner a row is there (two pieces: 1 x 4096 4.4 us, not 3.6;
+    // 8192 x 4096 57.7, not 54.9); rows of more than 14 wavefronts by four pieces, so that two fit a CU (2000 x 16384 28.8 us, not 32.9)
+    if (pieces <= 64) row_kernel<T, 1, 4, NORM, false, PAST><<<dim3((n + 3) / 4), 256, 0, s>>>(a);
+    else if (NORM && pieces <= 1024) row_kernel<T, 1, 1, NORM, false, PAST><<<dim3(n), threads(1), 0, s>>>(a);
+    else if (pieces <= 2 * 64 * 14) row_kernel<T, 2, 1, NORM, false, PAST><<<dim3(n), threads(2), 0, s>>>(a);
+    else if (pieces <= 4096) row_kernel<T, 4, 1, NORM, false, PAST><<<dim3(n), threads(4), 0, s>>>(a);
+    else row_kernel<T, 1, 1, NORM, true, false><<<dim3(n), 1024, 0, s>>>(a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
+}
+template <typename T, bool NORM>
+hipError_t run_rows(const NormArgs& a, hipStream_t s) {
+  const bool past = (!NORM || a.residual) && a.samples * a.features * (int64_t)sizeof(T) >= kPastBytes;
+  return past ? run_rows<T, NORM, true>(a, s) : run_rows<T, NORM, false>(a, s);
 }
 
 template <typename T>
@@ -285,13 +309,13 @@ __device__ inline void load_or_ones(float (&g)[kPiece], const void* from, int co
   }
 }
 
-// A workgroup takes a run of rows, one or, ROWS > 1, one to each of its wavefronts at a time; a thread keeps its columns' gain and sums,
+// A workgroup takes a row or, ROWS > 1, one to each of its wavefronts at a time, those that run together neighbouring ones; a thread keeps its columns' gain and sums,
 // and, but for the widest rows, has the next row's values on their way.  dgain: `part`, runs x `stride`, where it is wanted.
-template <typename T, bool HELD, int PIECES, int ROWS, int MOST>
-__global__ __launch_bounds__(MOST) void norm_backward_kernel(NormBackwardArgs a, float* part, int stride, int64_t run) {
+template <typename T, bool HELD, int PIECES, int ROWS, int MOST, bool PAST>
+__global__ __launch_bounds__(MOST) void norm_backward_kernel(NormBackwardArgs a, float* part, int stride) {
   const int threads = ROWS > 1 ? 64 : (int)blockDim.x, t = ROWS > 1 ? threadIdx.x & 63 : threadIdx.x, n = a.features;
   const int slot = ROWS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
-  const int64_t first = (int64_t)blockIdx.x * run, last = min(a.samples, first + run);
+  const int64_t step = (int64_t)gridDim.x * ROWS, last = a.samples;
   struct Row {
     Raw<T> dy[PIECES], dh[PIECES];
     std::conditional_t<HELD, uint2, Raw<T>> h[PIECES];
@@ -304,31 +328,31 @@ __global__ __launch_bounds__(MOST) void norm_backward_kernel(NormBackwardArgs a,
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
       const int col = (t + p * threads) * kPiece;
-      q.dy[p].load(static_cast<const T*>(a.dy) + row * a.lddy + col, n - col);
+      q.dy[p].template load<PAST>(static_cast<const T*>(a.dy) + row * a.lddy + col, n - col);
       if constexpr (HELD) {
         const int in = min(col, groups * kGroup - kPiece);                  // codes go on to the end of their group
         q.h[p] = *reinterpret_cast<const uint2*>(a.held.codes + row * ((int64_t)groups * kGroup) + in);
         q.exps[p] = a.held.exponents[row * groups + in / kGroup];
       } else {
-        q.h[p].load(static_cast<const T*>(a.h) + row * a.ldh + col, n - col);
+        q.h[p].template load<PAST>(static_cast<const T*>(a.h) + row * a.ldh + col, n - col);
       }
-      if (a.dh) q.dh[p].load(static_cast<const T*>(a.dh) + row * a.lddh + col, n - col);
+      if (a.dh) q.dh[p].template load<PAST>(static_cast<const T*>(a.dh) + row * a.lddh + col, n - col);
     }
   };
   constexpr bool kNext = MOST <= 512;              // 1024 threads have no registers for it
   Raw<T> gain[PIECES];
   float sums[PIECES][kPiece] = {};
   Row now, next;
-  int64_t row = first + slot;
+  int64_t row = (int64_t)blockIdx.x * ROWS + slot;
   if (kNext && row < last) ask(now, row);
   if (a.gain) {
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) gain[p].load(static_cast<const T*>(a.gain) + (t + p * threads) * kPiece, n - (t + p * threads) * kPiece);
   }
   __shared__ float dots[2][16];
-  for (int turn = 0; row < last; row += ROWS, turn ^= 1) {
+  for (int turn = 0; row < last; row += step, turn ^= 1) {
     if (!kNext) ask(now, row);
-    else if (row + ROWS < last) ask(next, row + ROWS);
+    else if (row + step < last) ask(next, row + step);
     float dy[PIECES][kPiece], h[PIECES][kPiece], dot = 0.f;
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
@@ -480,7 +504,7 @@ __global__ __launch_bounds__(256) void norm_gain_kernel(const float* part, float
 constexpr int64_t kAlong = int64_t(1) << 22;              // rows whose means lie in front of the parts in the workspace
 constexpr int64_t kPartFloats = (int64_t)(kWorkspaceBytes / 4) - kAlong;
 
-template <typename T, bool HELD>
+template <typename T, bool HELD, bool PAST>
 hipError_t run_norm_backward(const NormBackwardArgs& all, hipStream_t s) {
   float* const along = static_cast<float*>(all.workspace);
   float* const parts = along + kAlong;
@@ -497,19 +521,26 @@ hipError_t run_norm_backward(const NormBackwardArgs& all, hipStream_t s) {
     a.rstd = all.rstd + at;
     if (a.dh) a.dh = static_cast<const T*>(all.dh) + at * all.lddh;
     if (a.dx) a.dx = static_cast<T*>(all.dx) + at * all.lddx;
-    // as many workgroups as run together, 16 wavefronts a CU
-    const int each = pieces <= 64 ? 1 : 2, waves = pieces <= 128 ? 4 : std::min(16, (pieces + 64 * each - 1) / (64 * each)), rows = pieces <= 128 ? 4 : 1;
+    // A row takes a workgroup about 1.25 us, and a run's sums their time to be written, read and joined: the rows of a run grow with the
+    // root of their number (bfloat16, us: 512 x 4096 by 1, 2, 4, 8 rows 16.7, 13.3, 13.4, 17.9; 8192 x 4096 by 4, 8, 16, 32 69.8, 65.9, 56.6, 63.9;
+    // 8192 x 512, four wavefronts a row each, by 4, 8, 16, 32 17.4, 12.8, 11.9, 12.3).
+    const int waves = pieces <= 128 ? 4 : std::min(16, (pieces + 127) / 128), rows = pieces <= 128 ? 4 : 1;
     const bool wide = pieces > 2 * 1024;
-    const int64_t most = std::min<int64_t>(wide ? std::max<int64_t>(1, 1024 * 2048 / a.features) : 256 * (16 / waves), kPartFloats / stride);
-    const int64_t run = std::max<int64_t>(1, (a.samples + most * rows - 1) / (most * rows)) * rows;
+    int64_t run = wide ? std::max<int64_t>(1, a.samples * a.features / (1024 * 2048)) : rows;
+    while (!wide && (run / rows + 1) * (run / rows + 1) * (rows > 1 ? 512 : 32) <= a.samples) run += rows;
+    // no more runs than workgroups run together, 12 wavefronts a CU
+    const int64_t together = 256 * std::max(1, 12 / waves);
+    if (!wide && run * together < a.samples) run = (a.samples + together * rows - 1) / (together * rows) * rows;
+    const int64_t least = (a.samples + kPartFloats / stride - 1) / (kPartFloats / stride);
+    if (run < least) run = (least + rows - 1) / rows * rows;
     const unsigned runs = (unsigned)((a.samples + run - 1) / run);
     float* const part = a.dgain ? parts : nullptr;
     if (a.samples > 0) {
-      if (pieces <= 64) norm_backward_kernel<T, HELD, 1, 4, 256><<<dim3(runs), 256, 0, s>>>(a, part, stride, run);
-      else if (pieces <= 128) norm_backward_kernel<T, HELD, 2, 4, 256><<<dim3(runs), 256, 0, s>>>(a, part, stride, run);
-      else if (waves <= 4) norm_backward_kernel<T, HELD, 2, 1, 256><<<dim3(runs), dim3((unsigned)waves * 64), 0, s>>>(a, part, stride, run);
-      else if (waves <= 8) norm_backward_kernel<T, HELD, 2, 1, 512><<<dim3(runs), dim3((unsigned)waves * 64), 0, s>>>(a, part, stride, run);
-      else if (!wide) norm_backward_kernel<T, HELD, 2, 1, 1024><<<dim3(runs), dim3((unsigned)waves * 64), 0, s>>>(a, part, stride, run);
+      if (pieces <= 64) norm_backward_kernel<T, HELD, 1, 4, 256, PAST><<<dim3(runs), 256, 0, s>>>(a, part, stride);
+      else if (pieces <= 128) norm_backward_kernel<T, HELD, 2, 4, 256, PAST><<<dim3(runs), 256, 0, s>>>(a, part, stride);
+      else if (waves <= 4) norm_backward_kernel<T, HELD, 2, 1, 256, PAST><<<dim3(runs), dim3((unsigned)waves * 64), 0, s>>>(a, part, stride);
+      else if (waves <= 8) norm_backward_kernel<T, HELD, 2, 1, 512, PAST><<<dim3(runs), dim3((unsigned)waves * 64), 0, s>>>(a, part, stride);
+      else if (!wide) norm_backward_kernel<T, HELD, 2, 1, 1024, PAST><<<dim3(runs), dim3((unsigned)waves * 64), 0, s>>>(a, part, stride);
       else {
         norm_along_kernel<T, HELD><<<dim3((unsigned)a.samples), 1024, 0, s>>>(a, along);
         const hipError_t e = hipGetLastError();
@@ -603,7 +634,9 @@ hipError_t launch_rms_norm(int type, const NormArgs& a, hipStream_t s) {
 hipError_t launch_rms_norm_backward(int type, const NormBackwardArgs& a, hipStream_t s) {
   return by_type(type, [&](auto zero) {
     using T = decltype(zero);
-    return a.held.codes ? run_norm_backward<T, true>(a, s) : run_norm_backward<T, false>(a, s);
+    const bool past = a.samples * a.features * (int64_t)sizeof(T) >= kPastBytes;
+    if (a.held.codes) return past ? run_norm_backward<T, true, true>(a, s) : run_norm_backward<T, true, false>(a, s);
+    return past ? run_norm_backward<T, false, true>(a, s) : run_norm_backward<T, false, false>(a, s);
   });
 }
 
