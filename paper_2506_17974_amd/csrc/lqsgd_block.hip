@@ -266,16 +266,24 @@ hipError_t run_rows(const NormArgs& a, hipStream_t s) {
   return past ? run_rows<T, NORM, true>(a, s) : run_rows<T, NORM, false>(a, s);
 }
 
+// 16 bytes of x a thread: neighbouring threads store whole lines (fp32 by 32 bytes a thread, half a line with each store past the caches, took
+// 8192 x 4096 45 us; bfloat16 17, 6.0 TB/s).
+template <typename T> constexpr int kWide = 16 / (int)sizeof(T);
+
 template <typename T>
 __global__ __launch_bounds__(256) void rows_load_kernel(T* x, int64_t ldx, Rows rows, int64_t samples, int features, uint32_t pieces) {
+  constexpr int N = kWide<T>;
   const int64_t first = (int64_t)blockIdx.x * 256, row0 = first / pieces;
   const uint32_t at = (uint32_t)(first - row0 * pieces) + threadIdx.x, piece = at % pieces;
   const int64_t row = row0 + at / pieces;
   if (row >= samples) return;
-  const uint2 w = *reinterpret_cast<const uint2*>(rows.codes + row * ((int64_t)pieces * kPiece) + piece * kPiece);
-  float v[kPiece];
-  decode(v, w, rows.scales[row]);
-  store_values(x + row * ldx + piece * kPiece, v, features - (int)(piece * kPiece));
+  int8_t q[N];
+  __builtin_memcpy(q, __builtin_assume_aligned(rows.codes + row * ((int64_t)pieces * N) + piece * N, N), N);
+  const float scale = rows.scales[row];
+  float v[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) v[k] = (float)q[k] * scale;
+  store_values(x + row * ldx + piece * N, v, features - (int)(piece * N));
 }
 
 // ---------------------------------------------------------------------------
@@ -575,36 +583,39 @@ __device__ inline uint4 philox(uint4 c, uint2 key) {
   return c;
 }
 
-// A thread takes 8 consecutive values, whose bits are one block of the generator, a workgroup a run of 256 such pieces of the whole
-// tensor.  pieces: of a row; whole groups of 32 values where a checkpoint is kept.
+// A thread takes 16 bytes: 8 values, whose bits are one block of the generator, or in fp32 half of them (two threads make the block: a
+// thread that takes all 8 stores half lines).  A workgroup has a run of 256 such pieces of the whole tensor.  pieces: of a row; whole groups
+// of 32 values where a checkpoint is kept.
 template <typename T>
 __global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a, int64_t row_first, uint32_t pieces) {
+  constexpr int N = kWide<T>, kParts = 8 / N, kGroupPieces = kGroup / N;
   const int64_t first = (int64_t)blockIdx.x * 256, row0 = first / pieces;
   const uint32_t at = (uint32_t)(first - row0 * pieces) + threadIdx.x, piece = at % pieces;
   const int64_t row = row0 + at / pieces;
   const bool there = row < a.samples;
-  const int col = (int)piece * kPiece, n = there ? a.features - col : 0;
-  float v[kPiece], r[kPiece] = {};
+  const int col = (int)piece * N, n = there ? a.features - col : 0;
+  float v[N], r[N] = {};
   load_values(v, static_cast<const T*>(a.x) + row * a.ldx + col, n);
   if (a.residual) load_values(r, static_cast<const T*>(a.residual) + row * a.ldr + col, n);
   const uint64_t offset = a.offset + (a.more_offset ? *a.more_offset : 0);
-  const uint4 bits = philox(make_uint4(piece, (uint32_t)(row_first + row), (uint32_t)offset, (uint32_t)(offset >> 32)),
+  const uint4 bits = philox(make_uint4(piece / kParts, (uint32_t)(row_first + row), (uint32_t)offset, (uint32_t)(offset >> 32)),
                             make_uint2((uint32_t)a.seed, (uint32_t)(a.seed >> 32)));
-  const uint32_t words[4] = {bits.x, bits.y, bits.z, bits.w};
+  const bool high = kParts > 1 && piece % kParts;
+  const uint32_t words[4] = {high ? bits.z : bits.x, high ? bits.w : bits.y, bits.z, bits.w};
 #pragma unroll
-  for (int k = 0; k < kPiece; ++k) {
+  for (int k = 0; k < N; ++k) {
     const uint32_t b = k & 1 ? words[k >> 1] >> 16 : words[k >> 1] & 0xffffu;
     v[k] = (b >= a.least ? v[k] * a.factor : 0.f) + r[k];
   }
   store_values(static_cast<T*>(a.y) + row * a.ldy + col, v, n);
   if (!a.kept.codes) return;
 #pragma unroll
-  for (int k = 0; k < kPiece; ++k) v[k] = k < n ? widen(narrow<T>(v[k])) : 0.f;
-  uint32_t w[2], byte;
-  pack_codes<T>(w, v, group_largest<kPiece>(largest(v)), &byte);
+  for (int k = 0; k < N; ++k) v[k] = k < n ? widen(narrow<T>(v[k])) : 0.f;
+  uint32_t w[N / 4], byte;
+  pack_codes<T>(w, v, group_largest<N>(largest(v)), &byte);
   if (!there) return;
-  *reinterpret_cast<uint2*>(a.kept.codes + row * ((int64_t)pieces * kPiece) + col) = make_uint2(w[0], w[1]);
-  if ((piece & 3u) == 0) a.kept.exponents[row * (pieces >> 2) + (piece >> 2)] = (uint8_t)byte;
+  __builtin_memcpy(__builtin_assume_aligned(a.kept.codes + row * ((int64_t)pieces * N) + col, N), w, N);
+  if (piece % kGroupPieces == 0) a.kept.exponents[row * (pieces / kGroupPieces) + piece / kGroupPieces] = (uint8_t)byte;
 }
 
 }  // namespace
@@ -616,11 +627,11 @@ hipError_t launch_rows_save(int type, int64_t samples, int32_t features, const v
 }
 
 hipError_t launch_rows_load(int type, int64_t samples, int32_t features, Rows rows, void* x, int64_t ldx, hipStream_t s) {
-  const uint32_t pieces = (uint32_t)((features + kGroup - 1) / kGroup * (kGroup / kPiece));
   return by_type(type, [&](auto zero) {
     using T = decltype(zero);
+    const uint32_t pieces = (uint32_t)((features + kGroup - 1) / kGroup * (kGroup / kWide<T>));
     return by_slabs(samples, pieces, [&](int64_t at, int64_t n, unsigned blocks) {
-      const Rows part{rows.codes + at * pieces * kPiece, rows.scales + at};
+      const Rows part{rows.codes + at * pieces * kWide<T>, rows.scales + at};
       rows_load_kernel<T><<<dim3(blocks), 256, 0, s>>>(static_cast<T*>(x) + at * ldx, ldx, part, n, features, pieces);
       return hipGetLastError();
     });
@@ -641,16 +652,17 @@ hipError_t launch_rms_norm_backward(int type, const NormBackwardArgs& a, hipStre
 }
 
 hipError_t launch_dropout(int type, const DropoutArgs& all, hipStream_t s) {
-  const uint32_t pieces = (uint32_t)(all.kept.codes ? (all.features + kGroup - 1) / kGroup * (kGroup / kPiece) : (all.features + kPiece - 1) / kPiece);
   return by_type(type, [&](auto zero) {
     using T = decltype(zero);
+    constexpr int N = kWide<T>;
+    const uint32_t pieces = (uint32_t)(all.kept.codes ? (all.features + kGroup - 1) / kGroup * (kGroup / N) : (all.features + N - 1) / N);
     return by_slabs(all.samples, pieces, [&](int64_t at, int64_t n, unsigned blocks) {
       DropoutArgs a = all;
       a.samples = n;
       a.x = static_cast<const T*>(all.x) + at * all.ldx;
       if (a.residual) a.residual = static_cast<const T*>(all.residual) + at * all.ldr;
       a.y = static_cast<T*>(all.y) + at * all.ldy;
-      if (a.kept.codes) a.kept = Codes{all.kept.codes + at * pieces * kPiece, all.kept.exponents + at * (pieces >> 2)};
+      if (a.kept.codes) a.kept = Codes{all.kept.codes + at * pieces * N, all.kept.exponents + at * (pieces / (kGroup / N))};
       dropout_kernel<T><<<dim3(blocks), 256, 0, s>>>(a, at, pieces);
       return hipGetLastError();
     });
