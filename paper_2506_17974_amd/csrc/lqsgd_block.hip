@@ -37,14 +37,14 @@ __device__ inline uint2 row_codes(const float (&v)[kPiece], float inverse) {
 // ---------------------------------------------------------------------------
 // norm and 8-bit rows
 // ---------------------------------------------------------------------------
-// 8 values as they lie in memory, on their way: whole words, so that 16-bit values share registers.
-template <typename T>
+// N values as they lie in memory, on their way: whole words, so that 16-bit values share registers.
+template <typename T, int N = kPiece>
 struct Raw {
-  uint32_t w[kPiece * sizeof(T) / 4];
+  uint32_t w[N * sizeof(T) / 4];
   // PAST: past the caches.
   template <bool PAST = false>
   __device__ inline void load(const T* p, int n) {
-    if (n >= kPiece) {
+    if (n >= N) {
       if constexpr (PAST) {
         typedef uint32_t Words __attribute__((ext_vector_type(4), aligned(1)));
 #pragma unroll
@@ -67,11 +67,11 @@ struct Raw {
       }
     }
   }
-  __device__ inline void get(float (&f)[kPiece]) const {
-    T v[kPiece];
+  __device__ inline void get(float (&f)[N]) const {
+    T v[N];
     __builtin_memcpy(v, w, sizeof v);
 #pragma unroll
-    for (int k = 0; k < kPiece; ++k) f[k] = widen(v[k]);
+    for (int k = 0; k < N; ++k) f[k] = widen(v[k]);
   }
 };
 
@@ -226,7 +226,8 @@ __global__ __launch_bounds__(ROWS > 1 ? 64 * ROWS : 1024) void row_kernel(NormAr
 }
 
 // Inputs of this size and more are read past the caches (bfloat16 8192 x 4096: norm with residual and checkpoint 58.8 -> 53.3 us, backward 65.6 ->
-// 59.8, rows 19.7 -> 18.1; of half the size the norm 25.4 -> 30.2), but not by the norm of a single input (25.6 -> 29.5).
+// 59.8, rows 19.7 -> 18.1, dropout with residual 38.4 -> 33.9; of half the size the norm 25.4 -> 30.2), but not by the norm and dropout of a single input
+// (25.6 -> 29.5, 24.3 -> 25.7).
 constexpr int64_t kPastBytes = int64_t(1) << 26;
 
 template <typename T, bool NORM, bool PAST>
@@ -411,6 +412,13 @@ __global__ __launch_bounds__(MOST) void norm_backward_kernel(NormBackwardArgs a,
   }
   if (!part) return;
   float* const out = part + (int64_t)blockIdx.x * stride;
+  const bool joins = a.arrived != nullptr, whole = joins && gridDim.x == 1;
+  auto put = [&](int f, float v) {
+    if (f >= n) return;
+    if (whole) a.dgain[f] = a.accumulate ? a.dgain[f] + v : v;
+    else if (joins) __hip_atomic_store(out + f, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    else out[f] = v;
+  };
   if constexpr (ROWS > 1) {
     __shared__ float all[ROWS][PIECES * 64 * kPiece];
 #pragma unroll
@@ -422,15 +430,56 @@ __global__ __launch_bounds__(MOST) void norm_backward_kernel(NormBackwardArgs a,
       float total = 0.f;
 #pragma unroll
       for (int k = 0; k < ROWS; ++k) total += all[k][f];
-      out[f] = total;
+      put(f, total);
     }
   } else {
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
       const int f = (t + p * threads) * kPiece;
       if (f >= n) continue;                                                // `stride` has room for whole pieces
-      __builtin_memcpy(__builtin_assume_aligned(out + f, 16), sums[p], sizeof sums[p]);
+      if (joins) {
+#pragma unroll
+        for (int k = 0; k < kPiece; ++k) put(f + k, sums[p][k]);
+      } else {
+        __builtin_memcpy(__builtin_assume_aligned(out + f, 16), sums[p], sizeof sums[p]);
+      }
     }
+  }
+  if (!joins || whole) return;
+  // The workgroup that comes last joins the runs' sums, in the runs' order, whichever it is.  They are stored and read with agent-scope
+  // atomics, which go past the caches that the XCDs do not share: every store has arrived when vmcnt says so, and the barrier puts all of the
+  // workgroup's before its count.
+  __shared__ int last_one;
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0);
+  asm volatile("" ::: "memory");
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    last_one = __hip_atomic_fetch_add(a.arrived, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.x - 1;
+    if (last_one) __hip_atomic_store(a.arrived, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);        // for the next launch
+  }
+  __syncthreads();
+  if (!last_one) return;
+  // two columns and 16 runs at a time
+  for (int f = 2 * (int)threadIdx.x; f < n; f += 2 * (int)blockDim.x) {
+    float total[2] = {};
+    for (int k = 0; k < (int)gridDim.x; k += 16) {
+      uint64_t x[16];
+#pragma unroll
+      for (int u = 0; u < 16; ++u)
+        x[u] = __hip_atomic_load(reinterpret_cast<const uint64_t*>(part + (int64_t)min(k + u, (int)gridDim.x - 1) * stride + f), __ATOMIC_RELAXED,
+                                 __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+      for (int u = 0; u < 16; ++u) {
+        float v[2];
+        __builtin_memcpy(v, &x[u], sizeof v);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) total[c] += k + u < (int)gridDim.x ? v[c] : 0.f;
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+      if (f + c < n) a.dgain[f + c] = a.accumulate ? a.dgain[f + c] + total[c] : total[c];
   }
 }
 
@@ -543,6 +592,9 @@ hipError_t run_norm_backward(const NormBackwardArgs& all, hipStream_t s) {
     if (run < least) run = (least + rows - 1) / rows * rows;
     const unsigned runs = (unsigned)((a.samples + run - 1) / run);
     float* const part = a.dgain ? parts : nullptr;
+    // few sums are joined in the kernel itself: no second launch (64 x 1024 fp32 6.5 us, not 6.1, but 3.5 less on the host; 300 x 513 11.3, not 7.1)
+    const bool joins = part && !wide && a.samples > 0 && (int64_t)runs * stride <= int64_t(1) << 14;
+    if (!joins) a.arrived = nullptr;
     if (a.samples > 0) {
       if (pieces <= 64) norm_backward_kernel<T, HELD, 1, 4, 256, PAST><<<dim3(runs), 256, 0, s>>>(a, part, stride);
       else if (pieces <= 128) norm_backward_kernel<T, HELD, 2, 4, 256, PAST><<<dim3(runs), 256, 0, s>>>(a, part, stride);
@@ -558,7 +610,7 @@ hipError_t run_norm_backward(const NormBackwardArgs& all, hipStream_t s) {
       const hipError_t e = hipGetLastError();
       if (e != hipSuccess) return e;
     }
-    if (part) {
+    if (part && !joins) {
       norm_gain_kernel<<<dim3((unsigned)((a.features + 15) / 16)), 256, 0, s>>>(part, a.dgain, a.accumulate, a.features, stride, (int)runs);
       const hipError_t e = hipGetLastError();
       if (e != hipSuccess) return e;
@@ -586,7 +638,7 @@ __device__ inline uint4 philox(uint4 c, uint2 key) {
 // A thread takes 16 bytes: 8 values, whose bits are one block of the generator, or in fp32 half of them (two threads make the block: a
 // thread that takes all 8 stores half lines).  A workgroup has a run of 256 such pieces of the whole tensor.  pieces: of a row; whole groups
 // of 32 values where a checkpoint is kept.
-template <typename T>
+template <typename T, bool PAST>
 __global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a, int64_t row_first, uint32_t pieces) {
   constexpr int N = kWide<T>, kParts = 8 / N, kGroupPieces = kGroup / N;
   const int64_t first = (int64_t)blockIdx.x * 256, row0 = first / pieces;
@@ -595,13 +647,16 @@ __global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a, int64_t row
   const bool there = row < a.samples;
   const int col = (int)piece * N, n = there ? a.features - col : 0;
   float v[N], r[N] = {};
-  load_values(v, static_cast<const T*>(a.x) + row * a.ldx + col, n);
-  if (a.residual) load_values(r, static_cast<const T*>(a.residual) + row * a.ldr + col, n);
+  Raw<T, N> rx, rr;
+  rx.template load<PAST>(static_cast<const T*>(a.x) + row * a.ldx + col, n);
+  if (a.residual) rr.template load<PAST>(static_cast<const T*>(a.residual) + row * a.ldr + col, n);
   const uint64_t offset = a.offset + (a.more_offset ? *a.more_offset : 0);
   const uint4 bits = philox(make_uint4(piece / kParts, (uint32_t)(row_first + row), (uint32_t)offset, (uint32_t)(offset >> 32)),
                             make_uint2((uint32_t)a.seed, (uint32_t)(a.seed >> 32)));
   const bool high = kParts > 1 && piece % kParts;
   const uint32_t words[4] = {high ? bits.z : bits.x, high ? bits.w : bits.y, bits.z, bits.w};
+  rx.get(v);
+  if (a.residual) rr.get(r);
 #pragma unroll
   for (int k = 0; k < N; ++k) {
     const uint32_t b = k & 1 ? words[k >> 1] >> 16 : words[k >> 1] & 0xffffu;
@@ -656,6 +711,7 @@ hipError_t launch_dropout(int type, const DropoutArgs& all, hipStream_t s) {
     using T = decltype(zero);
     constexpr int N = kWide<T>;
     const uint32_t pieces = (uint32_t)(all.kept.codes ? (all.features + kGroup - 1) / kGroup * (kGroup / N) : (all.features + N - 1) / N);
+    const bool past = all.residual && all.samples * all.features * (int64_t)sizeof(T) >= kPastBytes;
     return by_slabs(all.samples, pieces, [&](int64_t at, int64_t n, unsigned blocks) {
       DropoutArgs a = all;
       a.samples = n;
@@ -663,7 +719,8 @@ hipError_t launch_dropout(int type, const DropoutArgs& all, hipStream_t s) {
       if (a.residual) a.residual = static_cast<const T*>(all.residual) + at * all.ldr;
       a.y = static_cast<T*>(all.y) + at * all.ldy;
       if (a.kept.codes) a.kept = Codes{all.kept.codes + at * pieces * N, all.kept.exponents + at * (pieces / (kGroup / N))};
-      dropout_kernel<T><<<dim3(blocks), 256, 0, s>>>(a, at, pieces);
+      if (past) dropout_kernel<T, true><<<dim3(blocks), 256, 0, s>>>(a, at, pieces);
+      else dropout_kernel<T, false><<<dim3(blocks), 256, 0, s>>>(a, at, pieces);
       return hipGetLastError();
     });
   });

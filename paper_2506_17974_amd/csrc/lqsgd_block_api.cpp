@@ -106,7 +106,7 @@ int lqsgd_rms_norm_backward(lqsgd_linear* c, int32_t type, int64_t samples, int3
   a.dy = dy; a.lddy = lddy; a.h = h; a.ldh = ldh;
   a.held = Codes{const_cast<int8_t*>(h_codes), const_cast<uint8_t*>(h_exponents)};
   a.rstd = rstd; a.gain = gain; a.dh = dh; a.lddh = lddh; a.dx = dx; a.lddx = lddx;
-  a.dgain = dgain; a.accumulate = accumulate != 0; a.workspace = c->workspace;
+  a.dgain = dgain; a.accumulate = accumulate != 0; a.workspace = c->workspace; a.arrived = c->arrived;
   return done(c, launch_rms_norm_backward(type, a, c->stream), "lqsgd_rms_norm_backward");
 }
 

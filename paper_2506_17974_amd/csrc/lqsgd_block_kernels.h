@@ -42,6 +42,7 @@ struct NormBackwardArgs {
   float* dgain;
   int32_t accumulate;
   void* workspace;
+  int* arrived;                                   // as in ProductArgs; the kernel: nullptr where another joins the runs' sums
 };
 
 struct DropoutArgs {
