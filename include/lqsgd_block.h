@@ -10,8 +10,8 @@
  *   dropout             y = keep x / (1 - p) + residual
  *
  * 8-bit rows
- *   A tensor's row v is kept as integers and one scale s: s = max|v| / 127, at least 2^-126, and a value's code is v (1 / s) rounded to
- *   the nearest integer, ties to even, with 1 / s and the product rounded to fp32: |v - q s| <= (1/2 + 2^-16) s.  A row that holds a NaN or an
+ *   A tensor's row v is kept as integers and one scale s: s = max|v| (1 / 127), at least 2^-126, and a value's code is v (1 / s) rounded
+ *   to the nearest integer, ties to even, with 1 / 127, 1 / s and both products rounded to fp32: |v - q s| <= (1/2 + 2^-16) s.  A row that holds a NaN or an
  *   infinity has a scale of NaN and codes of 0.  As the weight of a linear layer that is a scale an output feature, as its input a
  *   scale a sample.
  *     codes  : int8, samples x lqsgd_checkpoint_stride(features), 16-byte aligned; the codes behind the last feature are 0

@@ -2,7 +2,7 @@
 
     rms norm      h = x + residual;  rstd = 1 / sqrt(mean h^2 + eps);  y = h rstd gain
     its backward  v = dy gain;  dx = rstd (v - h rstd^2 mean(v h)) + dh;  dgain = sum dy h rstd
-    8-bit rows    s = max(max|v| / 127, 2^-126);  q = rint(v (1 / s)), each step in fp32
+    8-bit rows    s = max(max|v| (1 / 127), 2^-126);  q = rint(v (1 / s)), each step in fp32
     8-bit layer   z = s_x s_w (sum q_x q_w) + bias
     dropout       y = keep x 65536 / (65536 - t) + residual;  keep: 16 bits of Philox 4x32-10 are t or more
 """
@@ -37,7 +37,7 @@ def rows_save(v):
     fine = np.isfinite(v).all(1)
     w = np.where(fine[:, None], v, np.float32(0))
     with np.errstate(under="ignore"):
-        s = np.maximum(np.abs(w).max(1) / np.float32(127), np.float32(2.0 ** -126)).astype(np.float32)
+        s = np.maximum(np.abs(w).max(1) * (np.float32(1) / np.float32(127)), np.float32(2.0 ** -126)).astype(np.float32)
         q = np.rint((w * (np.float32(1) / s)[:, None]).astype(np.float32))
     codes = np.zeros((samples, -(-features // GROUP) * GROUP), np.int8)
     codes[:, :features] = q

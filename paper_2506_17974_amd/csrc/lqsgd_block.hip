@@ -16,7 +16,7 @@ namespace {
 // ---------------------------------------------------------------------------
 // 8-bit rows: the step of a row whose largest magnitude is absmax (NaN if that is none).
 __device__ inline float row_step(float absmax) {
-  return absmax < __builtin_inff() ? fmaxf(absmax / 127.f, 0x1p-126f) : __builtin_nanf("");
+  return absmax < __builtin_inff() ? fmaxf(absmax * (1.f / 127.f), 0x1p-126f) : __builtin_nanf("");
 }
 // Codes of 8 values, `inverse` = 1 / step; 0 where that is NaN.  |v| inverse is 127 (1 + 2^-22) at most, which rounds to 127; the product is
 // rounded before the sum that rounds it to an integer, as the definition has it.
