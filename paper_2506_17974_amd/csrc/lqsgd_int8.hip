@@ -13,10 +13,10 @@ namespace lqsgd {
 namespace linear {
 namespace {
 
-// v_mfma_i32_32x32x32_i8: a lane holds 16 consecutive r of operand row (lane mod 32), r0 = 16 (lane / 32); D comes back with
-// i = 8 (v / 4) + 4 (lane / 32) + v mod 4 in register v, j = lane mod 32.
+// v_mfma_i32_16x16x64_i8: a lane holds 16 consecutive r of operand row (lane mod 16), r0 = 16 (lane / 16); D comes back with
+// i = 4 (lane / 16) + register, j = lane mod 16.  (32 x 32 x 32 does as much a cycle, but the card gives it less power's worth: on random codes
+// 3.4 POPS in a loop of nothing else, this one 4.0.)
 typedef int i32x4 __attribute__((ext_vector_type(4)));
-typedef int i32x16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) i32x4 lds_i32x4;
 
 // The end of a product for D[j][i0 .. i0 + N - 1]: what it reads, which few samples' kernels ask for before their sums, and what it does.
@@ -46,8 +46,8 @@ struct End {
 };
 
 // A part of an operand in LDS: N rows x 128 codes, in chunks of 16, rows end to end: whole lines of memory (with rows of 64 codes the
-// requests to L2 were what bounded the largest products: 4096 x 11008 -> 4096 185 us).  Chunks change places within a row so that the 32
-// rows that one instruction reads a chunk of lie in different banks.
+// requests to L2 were what bounded the largest products: 4096 x 11008 -> 4096 185 us).  Chunks change places within a row so that the
+// 16 rows that one instruction reads a chunk of lie in different banks.
 constexpr int kRowChunks = kDeep / 16;
 __device__ inline int moved(int row) { return (row & 7) ^ (row >> 3 & 1); }
 __device__ inline int place(int row, int chunk) { return (row * kRowChunks + (chunk ^ moved(row))) * 16; }
@@ -93,7 +93,7 @@ struct Operand {
 // What a kernel's workgroups look like: B_ x B_ of D, WI x WJ wavefronts, operands of AHEAD steps in LDS.
 template <int B_, int WI_, int WJ_, int AHEAD>
 struct Shape {
-  static constexpr int B = B_, WI = WI_, WJ = WJ_, threads = 64 * WI * WJ, FI = B / WI / 32, FJ = B / WJ / 32;
+  static constexpr int B = B_, WI = WI_, WJ = WJ_, threads = 64 * WI * WJ, FI = B / WI / 16, FJ = B / WJ / 16;
   static constexpr int ahead = AHEAD, units = 2 * AHEAD + 1, unit = B * kDeep;
 };
 
@@ -108,9 +108,9 @@ __device__ inline Where where(int tiles_i, int tiles_j, int splits) {
   return Where{in / high, band * kBand + in % high, split};
 }
 
-// A tile of D to a workgroup, operands through LDS in steps of 128 codes.  LDS holds five units, each a step of one operand: those of
-// this step and the next, and the weight's of the step behind.  A step has four parts, whose products run from registers; the reads
-// of the next part and the fetches are issued among them, one behind each product.
+// A tile of D to a workgroup, operands through LDS in steps of 128 codes.  LDS holds the units (a step of one operand each) of `ahead` steps
+// and the weight's of the step behind them.  A step has two parts, whose products run from registers; the reads of the next part and
+// the fetches are issued among them, a weight's fragment read again as soon as its products are.
 template <typename T, typename S>
 __global__ __launch_bounds__(S::threads, S::threads >= 512 ? 2 : 1) void int8_product_kernel(Int8Args a, Split sp) {
   using O = Operand<S::B, S::threads>;
@@ -125,39 +125,21 @@ __global__ __launch_bounds__(S::threads, S::threads >= 512 ? 2 : 1) void int8_pr
   oa.prepare(a.a, i0, a.ni, a.stride, t);
   ob.prepare(a.b, j0, a.nj, a.stride, t);
   const uint32_t start = (uint32_t)(uintptr_t)all;
-  // rows of the tile that this wavefront multiplies, as bytes of a unit, and where in it a lane finds its chunks of the four parts
-  const int wi = wave % S::WI * (S::FI * 32) * kDeep, wj = wave / S::WI * (S::FJ * 32) * kDeep;
-  int mine[4];
-#pragma unroll
-  for (int k = 0; k < 4; ++k) mine[k] = place(lane & 31, 2 * k + (lane >> 5));
+  // rows of the tile that this wavefront multiplies, as bytes of a unit, and where in it a lane finds its chunks of the two parts
+  const int wi = wave % S::WI * (S::FI * 16) * kDeep, wj = wave / S::WI * (S::FJ * 16) * kDeep;
+  const int mine[2] = {place(lane & 15, lane >> 4), place(lane & 15, 4 + (lane >> 4))};
 
   // scales and bias of the tile's rows and columns, one a thread: for its end
   float of_a = 0.f, of_b = 0.f, of_bias = 0.f;
   if (t < S::B && i0 + t < a.ni) of_a = a.scales_a[i0 + t], of_bias = a.bias ? widen(static_cast<const T*>(a.bias)[i0 + t]) : 0.f;
   if (t < S::B && j0 + t < a.nj) of_b = a.scales_b[j0 + t];
 
-  i32x16 acc[S::FI][S::FJ] = {};
-  struct Fragments { i32x4 a[S::FI], b[S::FJ]; } now, next;
-  constexpr int kReads = S::FI + S::FJ, kProducts = S::FI * S::FJ;
-  constexpr int kAtOnce = (kReads + std::max(1, kProducts - 2) - 1) / std::max(1, kProducts - 2);           // the last read has two products to come back behind
-  auto read = [&](Fragments& f, int k, int part, int ua, int ub) {
-    if (k < S::FJ) f.b[k] = *reinterpret_cast<const lds_i32x4*>(all + (ub + wj + mine[part] + k * 32 * kDeep));
-    else f.a[k - S::FJ] = *reinterpret_cast<const lds_i32x4*>(all + (ua + wi + mine[part] + (k - S::FJ) * 32 * kDeep));
-  };
-  // The products from registers; among them the reads of the next operands, part `part` of the units at ua and ub, and loads
-  // `from`-th to `to`-th of operand o's step at r into the unit at uo.
-  auto multiply = [&](int part, int ua, int ub, const O& o, int from, int to, int uo, int r) {
+  i32x4 acc[S::FI][S::FJ] = {}, fa[S::FI], fb[2][S::FJ];
+  auto read_a = [&](int k, int part, int u) { fa[k] = *reinterpret_cast<const lds_i32x4*>(all + (u + wi + mine[part] + k * 16 * kDeep)); };
+  auto read_b = [&](int k, int part, int u) { fb[part][k] = *reinterpret_cast<const lds_i32x4*>(all + (u + wj + mine[part] + k * 16 * kDeep)); };
+  auto products = [&](int i, int part) {
 #pragma unroll
-    for (int k = 0; k < kProducts; ++k) {
-      acc[k / S::FJ][k % S::FJ] = __builtin_amdgcn_mfma_i32_32x32x32_i8(now.a[k / S::FJ], now.b[k % S::FJ], acc[k / S::FJ][k % S::FJ], 0, 0, 0);
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int q = k * kAtOnce; q < min((k + 1) * kAtOnce, kReads); ++q) read(next, q, part, ua, ub);
-#pragma unroll
-      for (int q = from + k * (to - from) / kProducts; q < from + (k + 1) * (to - from) / kProducts; ++q) o.load(q, start + uo, r, last);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    now = next;
+    for (int k = 0; k < S::FJ; ++k) acc[i][k] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fa[i], fb[part][k], acc[i][k], 0, 0, 0);
   };
   // Units go round: the weight's and the input's steps take every other one.
   auto behind = [](int u, int n) { u += n * S::unit; return u >= S::units * S::unit ? u - S::units * S::unit : u; };
@@ -179,16 +161,45 @@ __global__ __launch_bounds__(S::threads, S::threads >= 512 ? 2 : 1) void int8_pr
   };
   wait(std::integral_constant<int, O::loads * 2 * (S::ahead - 1)>{});
 #pragma unroll
-  for (int k = 0; k < kReads; ++k) read(now, k, 0, 0, S::unit);
+  for (int k = 0; k < S::FJ; ++k) read_b(k, 0, S::unit);
+#pragma unroll
+  for (int k = 0; k < S::FI; ++k) read_a(k, 0, 0);
+  // The second part's first kHold + 1 fragments are multiplied before the barrier, while the part's last reads come back.
+  constexpr int kHold = S::FI >= 8 ? 1 : 0;
   int ua = 0;
   for (int r = first; r < last; r += kDeep) {
     const int ub = behind(ua, 1), next_a = behind(ua, 2), next_b = behind(ua, 3), free = behind(ua, S::units - 1), ahead = r + S::ahead * kDeep;
-    multiply(1, ua, ub, oa, 0, O::loads / 2, free, ahead);
-    multiply(2, ua, ub, oa, O::loads / 2, O::loads, free, ahead);
-    multiply(3, ua, ub, oa, 0, 0, 0, 0);
-    // The next step's units have come (what may still be on its way: those behind that), and nobody reads this step's any more.
-    wait(std::integral_constant<int, O::loads * (2 * S::ahead - 3)>{});
-    multiply(0, next_a, next_b, ob, 0, O::loads, ua, ahead);
+#pragma unroll
+    for (int i = 0; i < S::FI; ++i) {
+      products(i, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      read_a(i, 1, ua);
+#pragma unroll
+      for (int k = i * S::FJ / S::FI; k < (i + 1) * S::FJ / S::FI; ++k) read_b(k, 1, ub);
+#pragma unroll
+      for (int k = i * O::loads / S::FI; k < (i + 1) * O::loads / S::FI; ++k) oa.load(k, start + free, ahead, last);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int i = 0; i < S::FI; ++i) {
+      products(i, 1);
+      __builtin_amdgcn_sched_barrier(0);
+      if (i < kHold) continue;
+      // The next step's units have come (what may still be on its way: those behind that), and nobody reads this step's any more.
+      if (i == kHold) {
+        wait(std::integral_constant<int, O::loads * (2 * S::ahead - 3)>{});
+#pragma unroll
+        for (int k = 0; k < kHold; ++k) read_a(k, 0, next_a);
+      }
+      read_a(i, 0, next_a);
+      constexpr int kLeft = S::FI - kHold;
+      const int at = i - kHold;
+#pragma unroll
+      for (int k = at * S::FJ / kLeft; k < (at + 1) * S::FJ / kLeft; ++k) read_b(k, 0, next_b);
+#pragma unroll
+      for (int k = at * O::loads / kLeft; k < (at + 1) * O::loads / kLeft; ++k) ob.load(k, start + ua, ahead, last);
+      __builtin_amdgcn_sched_barrier(0);
+    }
     ua = next_a;
   }
 
@@ -196,7 +207,7 @@ __global__ __launch_bounds__(S::threads, S::threads >= 512 ? 2 : 1) void int8_pr
   // instructions come from memory: unrolled it took 10 us more).  Scales and bias go through LDS, behind the strips; the residual's
   // values are asked for four turns ahead.
   constexpr int N = std::is_same_v<T, float> ? 4 : 8;
-  using P = Strips<S::FI, S::FJ, S::WI, S::WJ, N>;
+  using P = Strips<S::FI / 2, S::FJ / 2, S::WI, S::WJ, N>;
   constexpr int kStrips = S::WI * S::WJ * P::bytes;
   static_assert(kStrips + 3 * S::B * 4 <= S::units * S::unit && S::threads >= S::B, "the strips have to fit the operands' place");
   typedef __attribute__((address_space(3))) float lds_float;
@@ -213,10 +224,10 @@ __global__ __launch_bounds__(S::threads, S::threads >= 512 ? 2 : 1) void int8_pr
   };
   auto put = [&](int q) {
 #pragma unroll
-    for (int qq = 0; qq < S::FJ; ++qq) {
-      if (qq != q) continue;
+    for (int k = 0; k < S::FJ; ++k) {
+      if (k / 2 != q) continue;
 #pragma unroll
-      for (int k = 0; k < S::FI; ++k) P::put(strip, k, __builtin_bit_cast(f32x16, acc[k][qq]), lane);
+      for (int i = 0; i < S::FI; ++i) *reinterpret_cast<lds_i32x4*>(strip + P::place(k % 2 * 16 + (lane & 15), 4 * i + (lane >> 4))) = acc[i][k];
     }
   };
   auto end = [&](auto&& others) {
@@ -241,7 +252,7 @@ __global__ __launch_bounds__(S::threads, S::threads >= 512 ? 2 : 1) void int8_pr
 #pragma unroll
     for (int k = 0; k < kAhead - 1; ++k) ask(residual[k], k);
 #pragma clang loop unroll(disable)
-    for (int q = 0; q < S::FJ; ++q) {
+    for (int q = 0; q < S::FJ / 2; ++q) {
       put(q);
 #pragma clang loop unroll(disable)
       for (int turn = 0; turn < P::turns; ++turn) {
@@ -281,7 +292,7 @@ __global__ __launch_bounds__(S::threads, S::threads >= 512 ? 2 : 1) void int8_pr
   };
   ready();
 #pragma clang loop unroll(disable)
-  for (int q = 0; q < S::FJ; ++q) {
+  for (int q = 0; q < S::FJ / 2; ++q) {
     put(q);
 #pragma clang loop unroll(disable)
     for (int turn = 0; turn < P::turns; ++turn) {
