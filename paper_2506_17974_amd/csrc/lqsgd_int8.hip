@@ -49,7 +49,7 @@ struct End {
 // requests to L2 were what bounded the largest products: 4096 x 11008 -> 4096 185 us).  Chunks change places within a row so that the
 // 16 rows that one instruction reads a chunk of lie in different banks.
 constexpr int kRowChunks = kDeep / 16;
-__device__ inline int moved(int row) { return (row & 7) ^ (row >> 3 & 1); }
+__device__ inline int moved(int row) { return row >> 1 & 7; }
 __device__ inline int place(int row, int chunk) { return (row * kRowChunks + (chunk ^ moved(row))) * 16; }
 
 // One operand of a workgroup's tile and its way into LDS: 16 bytes a lane, straight from memory.  Lanes that have nothing there get an
@@ -166,6 +166,7 @@ __global__ __launch_bounds__(S::threads, S::threads >= 512 ? 2 : 1) void int8_pr
   for (int k = 0; k < S::FI; ++k) read_a(k, 0, 0);
   // The second part's first kHold + 1 fragments are multiplied before the barrier, while the part's last reads come back.
   constexpr int kHold = S::FI >= 8 ? 1 : 0;
+  constexpr int kSoon = (2 * S::FJ + S::FI - 1) / S::FI;          // the input's fragments, which all products need, are read in the first half of a part
   int ua = 0;
   for (int r = first; r < last; r += kDeep) {
     const int ub = behind(ua, 1), next_a = behind(ua, 2), next_b = behind(ua, 3), free = behind(ua, S::units - 1), ahead = r + S::ahead * kDeep;
@@ -173,9 +174,9 @@ __global__ __launch_bounds__(S::threads, S::threads >= 512 ? 2 : 1) void int8_pr
     for (int i = 0; i < S::FI; ++i) {
       products(i, 0);
       __builtin_amdgcn_sched_barrier(0);
-      read_a(i, 1, ua);
 #pragma unroll
-      for (int k = i * S::FJ / S::FI; k < (i + 1) * S::FJ / S::FI; ++k) read_b(k, 1, ub);
+      for (int k = i * kSoon; k < std::min((i + 1) * kSoon, S::FJ); ++k) read_b(k, 1, ub);
+      read_a(i, 1, ua);
 #pragma unroll
       for (int k = i * O::loads / S::FI; k < (i + 1) * O::loads / S::FI; ++k) oa.load(k, start + free, ahead, last);
       __builtin_amdgcn_sched_barrier(0);
@@ -188,14 +189,16 @@ __global__ __launch_bounds__(S::threads, S::threads >= 512 ? 2 : 1) void int8_pr
       // The next step's units have come (what may still be on its way: those behind that), and nobody reads this step's any more.
       if (i == kHold) {
         wait(std::integral_constant<int, O::loads * (2 * S::ahead - 3)>{});
+      }
+      constexpr int kLeft = S::FI - kHold;
+      const int at = i - kHold;
+#pragma unroll
+      for (int k = at * kSoon; k < std::min((at + 1) * kSoon, S::FJ); ++k) read_b(k, 0, next_b);
+      if (i == kHold) {
 #pragma unroll
         for (int k = 0; k < kHold; ++k) read_a(k, 0, next_a);
       }
       read_a(i, 0, next_a);
-      constexpr int kLeft = S::FI - kHold;
-      const int at = i - kHold;
-#pragma unroll
-      for (int k = at * S::FJ / kLeft; k < (at + 1) * S::FJ / kLeft; ++k) read_b(k, 0, next_b);
 #pragma unroll
       for (int k = at * O::loads / kLeft; k < (at + 1) * O::loads / kLeft; ++k) ob.load(k, start + ua, ahead, last);
       __builtin_amdgcn_sched_barrier(0);
