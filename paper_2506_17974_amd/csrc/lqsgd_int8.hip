@@ -339,12 +339,14 @@ __global__ __launch_bounds__(S::threads, S::threads >= 512 ? 2 : 1) void int8_pr
 // i = 4 (lane / 16) + register, j = lane mod 16), U steps of 64 on their way.  The sums meet in LDS.
 template <typename T, int FI, int FJ, int WAVES, int U>
 __global__ __launch_bounds__(WAVES * 64) void int8_few_kernel(Int8Args a, int tiles_i, int tiles_j) {
-  // tiles of the same weight rows follow each other on one XCD
-  const int x = (int)blockIdx.x & 7, q = (int)blockIdx.x >> 3, ti = q / tiles_j * 8 + x;
-  if (ti >= tiles_i) return;
+  // workgroups go round the 8 XCDs: tiles of the same weight rows follow each other on one where there are rows for all, as the grid has it
+  const bool rows_first = tiles_i >= 64;
+  const int q = (int)blockIdx.x >> 3, ti = rows_first ? q / tiles_j * 8 + ((int)blockIdx.x & 7) : (int)blockIdx.x % tiles_i;
+  const int tj = rows_first ? q % tiles_j : (int)blockIdx.x / tiles_i;
+  if (ti >= tiles_i || tj >= tiles_j) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int i0 = ti * 16 * FI;
-  const int64_t j0 = (int64_t)(q % tiles_j) * 16 * FJ;
+  const int64_t j0 = (int64_t)tj * 16 * FJ;
   const int at = 16 * (lane >> 4), steps = (a.stride + 63) / 64, each = (steps + WAVES - 1) / WAVES;
   const int first = min(wave * each, steps) * 64, end = min((wave + 1) * each, steps) * 64;
   const int8_t* pa[FI];
