@@ -45,7 +45,7 @@ inline Int8Plan plan_int8(int64_t ni, int64_t nj, int64_t stride) {
   }
   for (int f = 0; f < 2; ++f) {
     const int64_t bj = f ? 32 : 16, ti = (ni + 15) / 16, tj = (nj + bj - 1) / bj;
-    if (ti * tj >= 1 << 20) continue;
+    if ((ti + 7) / 8 * 8 * tj >= 1 << 20) continue;                        // as many workgroups, of 512 threads
     const float all = (float)(ti * tj) * (float)((16 + bj) * stride) / 8e6f, one = (f ? .8f : .3f) + (float)stride * (f ? .75e-3f : .5e-3f);
     offer(f ? kFew32 : kFew16, ti, tj, 1, steps, false, 2.6f + 2.2e-3f * (float)(ti * tj) + std::max(all, one));
   }
