@@ -398,59 +398,52 @@ __global__ __launch_bounds__(WAVES * 64) void int8_few_kernel(Int8Args a, int ti
   e.finish(sum, a, j, i);
 }
 
-// Single tokens, up to M of them: D wavefronts share R weight rows, which they read in runs of 1024 codes, 16 a lane, in turn, U runs on their
-// way, and multiply by v_dot4.  The lanes' sums are added up at the end, the wavefronts' in LDS.
-template <typename T, int M, int R, int U, int D>
-__global__ __launch_bounds__(256) void int8_tokens_kernel(Int8Args a) {
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), slice = wave % D;
-  const int i0 = ((int)blockIdx.x * (4 / D) + wave / D) * R;
-  const int j = lane % M, i = lane / M < R ? i0 + lane / M : a.ni;
+// A single token: the four wavefronts of a workgroup share two weight rows, which they read in runs of 1024 codes, 16 a lane, in turn, U runs on
+// their way, and multiply by v_dot4.  The lanes' sums are added up at the end, the wavefronts' in LDS.  Bound by the weight's stream: 4096 ->
+// 11008 9.2 us (4.9 TB/s with the launch), 8192 -> 8192 12.4 (5.4).  Tried: one, three, four, six and eight rows, and rows to a wavefront or two
+// (4096 -> 11008 9.5 to 16.5 us).
+template <typename T, int U>
+__global__ __launch_bounds__(256) void int8_token_kernel(Int8Args a) {
+  constexpr int R = 2, D = 4;
+  const int lane = threadIdx.x & 63, slice = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int i0 = (int)blockIdx.x * R, i = lane < R ? i0 + lane : a.ni;
   End<T, 1> e;
-  if (slice == 0) e.load(a, j, i);
+  if (slice == 0) e.load(a, 0, i);
   const int8_t* row[R];
 #pragma unroll
   for (int k = 0; k < R; ++k) row[k] = a.a + (int64_t)min(i0 + k, a.ni - 1) * a.stride;
-  int acc[R][M] = {};
+  int acc[R] = {};
   for (int r = 1024 * slice; r < a.stride; r += 1024 * U * D) {
-    i32x4 w[U][R], x[U][M];
+    i32x4 w[U][R], x[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int in = min(r + 1024 * u * D + 16 * lane, a.stride - 16);
 #pragma unroll
       for (int k = 0; k < R; ++k) w[u][k] = *reinterpret_cast<const i32x4*>(row[k] + in);
-#pragma unroll
-      for (int m = 0; m < M; ++m) x[u][m] = *reinterpret_cast<const i32x4*>(a.b + min((int64_t)m, a.nj - 1) * a.stride + in);
+      x[u] = *reinterpret_cast<const i32x4*>(a.b + in);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const bool there = r + 1024 * u * D + 16 * lane < a.stride;
+      const i32x4 v = r + 1024 * u * D + 16 * lane < a.stride ? x[u] : i32x4{};
 #pragma unroll
-      for (int m = 0; m < M; ++m) {
-        const i32x4 v = there ? x[u][m] : i32x4{};
+      for (int k = 0; k < R; ++k)
 #pragma unroll
-        for (int k = 0; k < R; ++k)
-#pragma unroll
-          for (int c = 0; c < 4; ++c) acc[k][m] = __builtin_amdgcn_sdot4(w[u][k][c], v[c], acc[k][m], false);
-      }
+        for (int c = 0; c < 4; ++c) acc[k] = __builtin_amdgcn_sdot4(w[u][k][c], v[c], acc[k], false);
     }
   }
   int sum[1] = {0};
 #pragma unroll
-  for (int k = 0; k < R; ++k)
-#pragma unroll
-    for (int m = 0; m < M; ++m) {
-      const int total = over_wave(acc[k][m], Plus{});
-      if (lane == k * M + m) sum[0] = total;
-    }
-  if constexpr (D > 1) {
-    __shared__ int sums[4][R * M];
-    if (lane < R * M) sums[wave][lane] = sum[0];
-    __syncthreads();
-    if (slice > 0 || lane >= R * M) return;
-#pragma unroll
-    for (int k = 1; k < D; ++k) sum[0] += sums[wave + k][lane];
+  for (int k = 0; k < R; ++k) {
+    const int total = over_wave(acc[k], Plus{});
+    if (lane == k) sum[0] = total;
   }
-  e.finish(sum, a, j, i);
+  __shared__ int sums[D][R];
+  if (lane < R) sums[slice][lane] = sum[0];
+  __syncthreads();
+  if (slice > 0 || lane >= R) return;
+#pragma unroll
+  for (int k = 1; k < D; ++k) sum[0] += sums[k][lane];
+  e.finish(sum, a, 0, i);
 }
 
 template <typename T, typename S>
@@ -472,8 +465,10 @@ hipError_t launch_int8_product(int type, const Int8Args& a, hipStream_t s) {
   return by_type(type, [&](auto zero) {
     using T = decltype(zero);
     switch (p.kernel) {
-      case kTokens:
-        int8_tokens_kernel<T, 1, 4, 2, 4><<<dim3((unsigned)p.sp.tiles_i), 256, 0, s>>>(a);
+      case kToken:
+        // a run a wavefront where there is no second (us, one run / two on their way: 4096 -> 11008 9.2 / 9.7, 11008 -> 4096 11.4 / 10.1)
+        if (a.stride <= 4096) int8_token_kernel<T, 1><<<dim3((unsigned)p.sp.tiles_i), 256, 0, s>>>(a);
+        else int8_token_kernel<T, 2><<<dim3((unsigned)p.sp.tiles_i), 256, 0, s>>>(a);
         return hipGetLastError();
       case kFew16: return run_few<T, 1>(a, p.sp, s);
       case kFew32: return run_few<T, 2>(a, p.sp, s);

@@ -9,7 +9,7 @@
 namespace lqsgd {
 namespace linear {
 
-enum Int8Kernel { kTokens = 0, kFew16, kFew32, kTile64, kTile128, kTile256, kInt8Kernels };
+enum Int8Kernel { kToken = 0, kFew16, kFew32, kTile64, kTile128, kTile256, kInt8Kernels };
 constexpr int kDeep = 128;                  // codes of a step of the tiles' kernels
 
 struct Int8Plan {
@@ -40,7 +40,7 @@ inline Int8Plan plan_int8(int64_t ni, int64_t nj, int64_t stride) {
   };
   const int64_t steps = (stride + kDeep - 1) / kDeep;
   if (nj <= 1) {
-    offer(kTokens, (ni + 3) / 4, 1, 1, steps, false, 0.f);
+    offer(kToken, (ni + 1) / 2, 1, 1, steps, false, 0.f);
     return best;
   }
   for (int f = 0; f < 2; ++f) {

@@ -5,7 +5,7 @@ import subprocess
 
 from tests.linear_plan import ROOT, compiler
 
-KERNELS = ("tokens", "few 16", "few 32", "64", "128", "256")
+KERNELS = ("token", "few 16", "few 32", "64", "128", "256")
 PROGRAM = r"""
 #include <cinttypes>
 #include <cstdio>
@@ -40,7 +40,7 @@ def plans(exe, asked):
 # Products that reach each kernel, with operands of two and of four steps in LDS, the sum whole and in parts, remainders in every
 # direction: (samples, rows, cols, kernel, four steps, in parts).  "few" kernels go by the weight's rows first from 64 tiles of them on.
 CASES = [
-    (1, 1, 1, "tokens", False, False), (1, 4099, 2051, "tokens", False, False), (1, 5, 9001, "tokens", False, False),
+    (1, 1, 1, "token", False, False), (1, 4099, 2051, "token", False, False), (1, 5, 9001, "token", False, False),
     (3, 37, 1001, "few 16", False, False), (15, 1049, 67, "few 16", False, False), (3, 1049, 4099, "few 16", False, False),
     (2991, 39, 1193, "few 32", False, False), (107, 826, 1576, "few 32", False, False), (29, 4459, 335, "few 32", False, False),
     (35, 4946, 370, "64", False, False), (4, 8645, 2299, "64", True, False), (3, 7144, 7475, "64", True, True),

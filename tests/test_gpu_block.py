@@ -369,6 +369,42 @@ def test_dropout_share_and_gradient(ops, kind):
 
 
 # ---------------------------------------------------------------------------
+# large tensors, which are read past the caches
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("kind,samples,features", [("bf16", 8200, 4099), ("f16", 70000, 481), ("f32", 4100, 4101), ("bf16", 3300, 11003), ("f32", 2050, 9001)])
+def test_large_tensors_row_by_row(ops, kind, samples, features):
+    """Norm, rows, the norm's backward and dropout of 64 MiB and more against the same calls on parts of the rows, bit by bit; dgain, whose sum
+    is over all of them, against float64."""
+    import torch
+    _say("large", kind, samples, features)
+    g = torch.Generator(device="cuda").manual_seed(samples)
+    x, r, dy, dh = (torch.randn((samples, features), generator=g, device="cuda").to(_t(kind)) for _ in range(4))
+    assert x.numel() * x.element_size() >= 1 << 26
+    gain = (torch.randn(features, generator=g, device="cuda") * 0.2 + 1).to(_t(kind))
+    held, rows = B.Checkpoint.empty(samples, features), B.RowCodes.empty(samples, features)
+    y, h, rstd = ops.rms_norm(x, gain, r, save_y=held, quantize_y=rows, want_rstd=True)
+    q = ops.quantize(x)
+    dx, dg = ops.rms_norm_backward(dy, h, rstd, gain, dh=dh)
+    drop = ops.dropout(x, 0.2, 77, 5, residual=r)
+    for part in (slice(0, 9), slice(samples // 2, samples // 2 + 130), slice(samples - 7, samples)):
+        c, b = B.Checkpoint.empty(x[part].shape[0], features), B.RowCodes.empty(x[part].shape[0], features)
+        want = ops.rms_norm(x[part], gain, r[part], save_y=c, quantize_y=b, want_rstd=True)
+        for got, w in zip((y, h, rstd, held.codes, held.exponents, rows.codes, rows.scales), want + (c.codes, c.exponents, b.codes, b.scales)):
+            assert torch.equal(got[part], w)
+        w = ops.quantize(x[part])
+        assert torch.equal(q.codes[part], w.codes) and torch.equal(q.scales[part], w.scales)
+        assert torch.equal(dx[part], ops.rms_norm_backward(dy[part], h[part], rstd[part], gain, dh=dh[part], want_dgain=False)[0])
+    assert torch.equal(drop[:50], ops.dropout(x[:50], 0.2, 77, 5, residual=r[:50]))
+    hx, hr = x[:3].double().cpu().numpy(), r[:3].double().cpu().numpy()
+    keep, want = bo.dropout(hx, 0.2, 77, 5, hr)
+    _close(drop[:3], want, 2 * U * (np.abs(want) + np.abs(hr)) + U * np.abs(want) + _rounded(kind, want), "dropout")
+    assert np.array_equal(drop[:3].double().cpu().numpy()[~keep], hr[~keep])
+    terms = dy.double() * h.double() * rstd.double()[:, None]
+    want, size = terms.sum(0), terms.abs().sum(0)
+    assert ((dg.double() - want).abs() <= U * size * (8 + 4 * samples ** 0.5)).all()
+
+
+# ---------------------------------------------------------------------------
 # together
 # ---------------------------------------------------------------------------
 @pytest.mark.parametrize("kind", TYPES)

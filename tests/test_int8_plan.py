@@ -6,8 +6,8 @@ import pytest
 from tests import int8_plan as ip
 
 pytestmark = pytest.mark.skipif(ip.compiler() is None, reason="no C++ compiler")
-TILE = {"tokens": (4, 1), "few 16": (16, 16), "few 32": (16, 32), "64": (64, 64), "128": (128, 128), "256": (256, 256)}
-THREADS = {"tokens": 256, "few 16": 512, "few 32": 512, "64": 256, "128": 512, "256": 512}
+TILE = {"token": (2, 1), "few 16": (16, 16), "few 32": (16, 32), "64": (64, 64), "128": (128, 128), "256": (256, 256)}
+THREADS = {"token": 256, "few 16": 512, "few 32": 512, "64": 256, "128": 512, "256": 512}
 
 
 @pytest.fixture(scope="module")
@@ -29,7 +29,7 @@ def _check(asked, p):
     assert kernel in ("64", "128", "256") or (parts == 1 and not deep)
     if parts > 1:
         assert ti * tj <= 8192 and ti * tj * parts * bi * bj * 4 <= 64 << 20, (asked, p)
-    assert (kernel == "tokens") == (m == 1)
+    assert (kernel == "token") == (m == 1)
 
 
 def test_any_size(exe):
@@ -51,7 +51,7 @@ def test_cases_take_the_kernels_they_are_for(exe):
     assert {c[3:] for c in ip.CASES} >= {(k, d, s) for k in ("64", "128") for d, s in ((False, False), (True, False), (True, True))}
 
 
-@pytest.mark.parametrize("asked,kernel", [((1, 11008, 4096), "tokens"), ((16, 4096, 4096), "few 16"), ((64, 11008, 4096), "64"), ((1024, 4096, 4096), "128"),
+@pytest.mark.parametrize("asked,kernel", [((1, 11008, 4096), "token"), ((16, 4096, 4096), "few 16"), ((64, 11008, 4096), "64"), ((1024, 4096, 4096), "128"),
                                           ((4096, 4096, 11008), "256"), ((4096, 11008, 4096), "256")])
 def test_choice(exe, asked, kernel):
     assert ip.plans(exe, [asked])[0][0] == kernel
