@@ -558,7 +558,7 @@ __global__ __launch_bounds__(256) void norm_gain_kernel(const float* part, float
   if (part4 == 0 && at < n) dgain[at] = accumulate ? dgain[at] + total : total;
 }
 
-constexpr int64_t kAlong = int64_t(1) << 22;              // rows whose means lie in front of the parts in the workspace
+constexpr int64_t kAlong = int64_t(1) << 21;              // rows at a time; wide ones' means lie in front of the parts in the workspace
 constexpr int64_t kPartFloats = (int64_t)(kWorkspaceBytes / 4) - kAlong;
 
 template <typename T, bool HELD, bool PAST>

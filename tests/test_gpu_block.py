@@ -404,6 +404,33 @@ def test_large_tensors_row_by_row(ops, kind, samples, features):
     assert ((dg.double() - want).abs() <= U * size * (8 + 4 * samples ** 0.5)).all()
 
 
+@pytest.mark.parametrize("kind,source", [("f16", "tensor"), ("bf16", "checkpoint"), ("f32", "tensor")])
+def test_more_samples_than_a_launch_takes(ops, kind, source):
+    """2^21 rows and some: norm, rows and the norm's backward go in parts, whose sums add up."""
+    import torch
+    _say("many samples", kind, source)
+    samples, features = (1 << 21) + 777, 9
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x, dy = (torch.randn((samples, features), generator=g, device="cuda").to(_t(kind)) for _ in range(2))
+    y, _, rstd = ops.rms_norm(x, want_rstd=True)
+    q = ops.quantize(x)
+    h = ops.save(x) if source == "checkpoint" else x
+    before = torch.randn(features, generator=g, device="cuda")
+    dg = before.clone()
+    dx, _ = ops.rms_norm_backward(dy, h, rstd, dgain=dg, accumulate=True)
+    for part in (slice(0, 40), slice((1 << 21) - 20, (1 << 21) + 20), slice(samples - 40, samples)):
+        w = ops.rms_norm(x[part], want_rstd=True)
+        assert torch.equal(y[part], w[0]) and torch.equal(rstd[part], w[2])
+        c = ops.quantize(x[part])
+        assert torch.equal(q.codes[part], c.codes) and torch.equal(q.scales[part], c.scales)
+        hp = ops.save(x[part]) if source == "checkpoint" else x[part]
+        assert torch.equal(dx[part], ops.rms_norm_backward(dy[part], hp, rstd[part], want_dgain=False)[0])
+    held = ops.load(h, torch.float32) if source == "checkpoint" else x
+    terms = dy.double() * held.double() * rstd.double()[:, None]
+    want, size = terms.sum(0) + before.double(), terms.abs().sum(0)
+    assert ((dg.double() - want).abs() <= U * size * (8 + 4 * samples ** 0.5) + U * want.abs()).all()
+
+
 # ---------------------------------------------------------------------------
 # together
 # ---------------------------------------------------------------------------
