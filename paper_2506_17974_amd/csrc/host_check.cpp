@@ -9,6 +9,7 @@
 #include <vector>
 
 #include "lqsgd.h"
+#include "lqsgd_block.h"
 #include "lqsgd_linear.h"
 #include "lqsgd_plan.h"
 
@@ -83,6 +84,12 @@ int main() {
   EXPECT(lqsgd_linear_create(nullptr, nullptr) == LQSGD_EINVAL && lqsgd_linear_destroy(nullptr) == LQSGD_OK);
   EXPECT(lqsgd_linear_synchronize(nullptr) == LQSGD_EINVAL && std::strlen(lqsgd_linear_last_error(nullptr)) > 0);
   EXPECT(lqsgd_linear_weight_grad(nullptr, 0, 1, 1, 1, nullptr, 1, nullptr, nullptr, 0, nullptr, 1, 0) == LQSGD_EINVAL);
+  EXPECT(lqsgd_rows_save(nullptr, 0, 1, 1, nullptr, 1, nullptr, nullptr) == LQSGD_EINVAL);
+  EXPECT(lqsgd_rows_load(nullptr, 0, 1, 1, nullptr, nullptr, nullptr, 1) == LQSGD_EINVAL);
+  EXPECT(lqsgd_rms_norm(nullptr, 0, 1, 1, 0.0, nullptr, 1, nullptr, 1, nullptr, nullptr, 1, nullptr, 1, nullptr, nullptr, nullptr, nullptr, nullptr) == LQSGD_EINVAL);
+  EXPECT(lqsgd_rms_norm_backward(nullptr, 0, 1, 1, nullptr, 1, nullptr, 1, nullptr, nullptr, nullptr, nullptr, nullptr, 1, nullptr, 1, nullptr, 0) == LQSGD_EINVAL);
+  EXPECT(lqsgd_int8_forward(nullptr, 0, 0, 1, 1, 1, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, 1, nullptr, 1) == LQSGD_EINVAL);
+  EXPECT(lqsgd_dropout(nullptr, 0, 1, 1, 0.5, 0, 0, nullptr, nullptr, 1, nullptr, 1, nullptr, 1, nullptr, nullptr) == LQSGD_EINVAL);
 
   lqsgd_plan_info info;
   std::vector<lqsgd_layer> resnet = {{64, 27, 0}, {64, 576, 0}, {128, 1152, 0}, {512, 4608, 0}, {10, 512, 0},

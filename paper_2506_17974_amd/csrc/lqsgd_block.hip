@@ -83,7 +83,8 @@ __device__ inline float root(double v) {
 
 // A row to a workgroup, PIECES of 8 values a thread in registers, or, ROWS > 1, to each of its wavefronts; WIDE: a row of any length,
 // read again for its outputs.  NORM: the norm, with what is wanted of it; otherwise 8-bit rows of x alone.  PAST: inputs past the caches.
-// Bound by memory: 8192 x 4096 bfloat16 norm with residual, checkpoint and h 53 us (5.7 TB/s), with 8-bit rows instead 42 (5.6), rows alone 18 (5.6).
+// Bound by memory: 8192 x 4096 bfloat16 norm with residual, checkpoint and h 51.5 us (5.9 TB/s), with 8-bit rows 42 to 45, the norm alone 26, rows alone 18 (5.6);
+// 4096 x 11008 norm 41 us (4.4).
 // Tried: workgroups that stay, keep the gain and have the next row on their way (norm alone 25 -> 29 us, single rows 0.2 us more: fewer
 // wavefronts fit).
 template <typename T, int PIECES, int ROWS, bool NORM, bool WIDE, bool PAST>
@@ -268,7 +269,7 @@ hipError_t run_rows(const NormArgs& a, hipStream_t s) {
 }
 
 // 16 bytes of x a thread: neighbouring threads store whole lines (fp32 by 32 bytes a thread, half a line with each store past the caches, took
-// 8192 x 4096 45 us; bfloat16 17, 6.0 TB/s).
+// 8192 x 4096 45 us, not 24.6; bfloat16 16.7, 6.0 TB/s).
 template <typename T> constexpr int kWide = 16 / (int)sizeof(T);
 
 template <typename T>
@@ -319,7 +320,11 @@ __device__ inline void load_or_ones(float (&g)[kPiece], const void* from, int co
 }
 
 // A workgroup takes a row or, ROWS > 1, one to each of its wavefronts at a time, those that run together neighbouring ones; a thread keeps its columns' gain and sums,
-// and, but for the widest rows, has the next row's values on their way.  dgain: `part`, runs x `stride`, where it is wanted.
+// and, but for the widest rows, has the next row's values on their way.  dgain: `part`, runs x `stride`, where it is wanted.  dot and sums are fp32:
+// what is added up has been rounded to fp32 once and is of the output's size.
+// Bound by memory: 8192 x 4096 bfloat16 with dh 47 to 51 us (5.3 to 5.7 TB/s); the runs' sums, 8 MiB, and norm_gain_kernel take 5 to 7 more (whole call 53, without
+// dgain 46).  Rows of
+// 8193 to 16384 features 4.0 TB/s (4096 x 11008 90 us): no registers are left for the next row's values.  Tried: two rows on their way (no gain).
 template <typename T, bool HELD, int PIECES, int ROWS, int MOST, bool PAST>
 __global__ __launch_bounds__(MOST) void norm_backward_kernel(NormBackwardArgs a, float* part, int stride) {
   const int threads = ROWS > 1 ? 64 : (int)blockDim.x, t = ROWS > 1 ? threadIdx.x & 63 : threadIdx.x, n = a.features;
@@ -536,7 +541,8 @@ __global__ __launch_bounds__(256) void norm_strips_kernel(NormBackwardArgs a, co
     if (col + k < n) part[(int64_t)blockIdx.y * stride + col + k] = sums[k];
 }
 
-// dgain from the runs' sums: a workgroup adds up 16 columns, 64 runs at a time, in an order of its own that is always the same.
+// dgain from the runs' sums: a workgroup adds up 16 columns, 64 runs at a time, in an order of its own that is always the same.  512 runs x 4096
+// features 4.6 us, most of it the launch and a round trip to memory.
 __global__ __launch_bounds__(256) void norm_gain_kernel(const float* part, float* dgain, int accumulate, int n, int stride, int runs) {
   __shared__ float sums[64][17];
   const int col = (int)blockIdx.x * 16 + (threadIdx.x & 3) * 4, slot = threadIdx.x >> 2;
@@ -636,7 +642,7 @@ __device__ inline uint4 philox(uint4 c, uint2 key) {
 }
 
 // A thread takes 16 bytes: 8 values, whose bits are one block of the generator, or in fp32 half of them (two threads make the block: a
-// thread that takes all 8 stores half lines).  A workgroup has a run of 256 such pieces of the whole tensor.  pieces: of a row; whole groups
+// thread that takes all 8 stores half lines).  Bound by memory: 8192 x 4096 bfloat16 with residual 33.9 us (5.9 TB/s).  A workgroup has a run of 256 such pieces of the whole tensor.  pieces: of a row; whole groups
 // of 32 values where a checkpoint is kept.
 template <typename T, bool PAST>
 __global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a, int64_t row_first, uint32_t pieces) {

@@ -126,7 +126,7 @@ int lqsgd_int8_forward(lqsgd_linear* c, int32_t type, int32_t act, int64_t sampl
   if (lies_over({y}, {x_codes, x_scales, w_codes, w_scales, bias})) return fail(c, LQSGD_EINVAL, kOver);
   if (residual == y && ldr != ldy) return fail(c, LQSGD_EINVAL, "y is the residual, with another stride");
   Int8Args a{};
-  a.ni = rows; a.nj = samples; a.depth = cols; a.stride = (cols + kGroup - 1) / kGroup * kGroup;
+  a.ni = rows; a.nj = samples; a.stride = (cols + kGroup - 1) / kGroup * kGroup;
   a.a = w_codes; a.scales_a = w_scales; a.b = x_codes; a.scales_b = x_scales;
   a.bias = bias; a.residual = residual; a.ldr = ldr; a.act = act;
   a.out = y; a.ldo = ldy; a.workspace = c->workspace; a.arrived = c->arrived;

@@ -60,7 +60,7 @@ struct DropoutArgs {
 
 struct Int8Args {                                 // D[j][i] = sum over r of A[i][r] B[j][r]: A the weight, B the input
   int64_t nj;
-  int32_t ni, depth, stride;                      // stride: of the codes' rows, a multiple of 32; zeros behind depth
+  int32_t ni, stride;                             // stride: of the codes' rows, a multiple of 32; zeros behind the depth
   const int8_t* a; const float* scales_a;
   const int8_t* b; const float* scales_b;
   const void* bias; const void* residual; int64_t ldr;
