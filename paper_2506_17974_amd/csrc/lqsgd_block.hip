@@ -37,14 +37,18 @@ __device__ inline uint2 row_codes(const float (&v)[kPiece], float inverse) {
 // ---------------------------------------------------------------------------
 // norm and 8-bit rows
 // ---------------------------------------------------------------------------
-// N values as they lie in memory, on their way: whole words, so that 16-bit values share registers.
-template <typename T, int N = kPiece>
+// N values of a row of n from `col` on, as they lie in memory, on their way: whole words, so that 16-bit values share registers.
+// ENDS (16-bit rows of N values or more): a piece that the row's end cuts, or that lies behind it, is read as the row's last N values, which get()
+// moves to their places, zeros behind them.  Read value by value they are waited for one by one, and the row for them (bfloat16 4096 x 11008
+// norm 42 -> 35 us, backward 90 -> 76; of 4096 x 5000 78 -> 62); fp32 values wait for nothing and have no registers for this.
+template <typename T, int N, bool ENDS>
 struct Raw {
   uint32_t w[N * sizeof(T) / 4];
   // PAST: past the caches.
   template <bool PAST = false>
-  __device__ inline void load(const T* p, int n) {
-    if (n >= N) {
+  __device__ inline void load(const T* row, int col, int n) {
+    const T* const p = row + (ENDS ? min(col, n - N) : col);
+    if (ENDS || n - col >= N) {
       if constexpr (PAST) {
         typedef uint32_t Words __attribute__((ext_vector_type(4), aligned(1)));
 #pragma unroll
@@ -56,6 +60,7 @@ struct Raw {
         __builtin_memcpy(w, p, sizeof w);
       }
     } else {
+      n -= col;
 #pragma unroll
       for (int k = 0; k < (int)(sizeof w / 4); ++k) {
         if constexpr (sizeof(T) == 4) {
@@ -67,13 +72,31 @@ struct Raw {
       }
     }
   }
-  __device__ inline void get(float (&f)[N]) const {
+  __device__ inline void get(float (&f)[N], int col, int n) const {
+    constexpr int W = sizeof w / 4;
+    uint32_t x[W];
+    __builtin_memcpy(x, w, sizeof x);
+    const int by = col - (n - N);
+    if (ENDS && by > 0) {
+#pragma unroll
+      for (int step = W / 2; step > 0; step >>= 1) {
+        const bool on = (by / 2 & step) != 0;
+#pragma unroll
+        for (int k = 0; k < W; ++k) x[k] = on ? (k + step < W ? x[k + step] : 0u) : x[k];
+      }
+#pragma unroll
+      for (int k = 0; k < W; ++k) {
+        x[k] = by & 1 ? x[k] >> 16 | (k + 1 < W ? x[k + 1] << 16 : 0u) : x[k];
+        x[k] = by < N ? x[k] : 0u;
+      }
+    }
     T v[N];
-    __builtin_memcpy(v, w, sizeof v);
+    __builtin_memcpy(v, x, sizeof v);
 #pragma unroll
     for (int k = 0; k < N; ++k) f[k] = widen(v[k]);
   }
 };
+template <typename T> constexpr bool kEnds = sizeof(T) == 2;
 
 // 1 / sqrt(mean + eps) in fp64: the hardware's estimate and a step of Newton's on it, which leaves 2^-40.
 __device__ inline float root(double v) {
@@ -87,8 +110,9 @@ __device__ inline float root(double v) {
 // 4096 x 11008 norm 41 us (4.4).
 // Tried: workgroups that stay, keep the gain and have the next row on their way (norm alone 25 -> 29 us, single rows 0.2 us more: fewer
 // wavefronts fit).
-template <typename T, int PIECES, int ROWS, bool NORM, bool WIDE, bool PAST>
+template <typename T, int PIECES, int ROWS, bool NORM, bool WIDE, bool PAST, bool ENDS = kEnds<T>>
 __global__ __launch_bounds__(ROWS > 1 ? 64 * ROWS : 1024) void row_kernel(NormArgs a) {
+  using R = Raw<T, kPiece, ENDS>;
   const int threads = ROWS > 1 ? 64 : (int)blockDim.x, t = ROWS > 1 ? threadIdx.x & 63 : threadIdx.x;
   const int64_t row = (int64_t)blockIdx.x * ROWS + (ROWS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0);
   if (ROWS > 1 && row >= a.samples) return;
@@ -99,18 +123,18 @@ __global__ __launch_bounds__(ROWS > 1 ? 64 * ROWS : 1024) void row_kernel(NormAr
   T* const h = NORM && a.h ? static_cast<T*>(a.h) + row * a.ldh : nullptr;
 
   // values of the row from `col` on, as the norm sees them; zeros behind its end
-  auto joined = [&](float (&v)[kPiece], const Raw<T>& from, const Raw<T>& more) {
-    from.get(v);
+  auto joined = [&](float (&v)[kPiece], const R& from, const R& more, int col) {
+    from.get(v, col, n);
     if (r) {
       float m[kPiece];
-      more.get(m);
+      more.get(m, col, n);
 #pragma unroll
       for (int k = 0; k < kPiece; ++k) v[k] = widen(narrow<T>(v[k] + m[k]));
     }
   };
-  auto gains = [&](float (&g)[kPiece], const Raw<T>& from) {
+  auto gains = [&](float (&g)[kPiece], const R& from, int col) {
     if (gain) {
-      from.get(g);
+      from.get(g, col, n);
     } else {
 #pragma unroll
       for (int k = 0; k < kPiece; ++k) g[k] = 1.f;
@@ -118,7 +142,7 @@ __global__ __launch_bounds__(ROWS > 1 ? 64 * ROWS : 1024) void row_kernel(NormAr
   };
   double sum = 0.0;
   float most = 0.f;
-  auto count = [&](const float (&v)[kPiece], const Raw<T>& rg) {
+  auto count = [&](const float (&v)[kPiece], const R& rg, int col) {
     if (NORM) {
 #pragma unroll
       for (int k = 0; k < kPiece; ++k) sum = __builtin_fma((double)v[k], (double)v[k], sum);
@@ -127,7 +151,7 @@ __global__ __launch_bounds__(ROWS > 1 ? 64 * ROWS : 1024) void row_kernel(NormAr
       most = __builtin_elementwise_maximum(most, largest(v));
     } else if (a.rows.codes) {
       float g[kPiece];
-      gains(g, rg);
+      gains(g, rg, col);
 #pragma unroll
       for (int k = 0; k < kPiece; ++k) g[k] *= v[k];
       most = __builtin_elementwise_maximum(most, largest(g));
@@ -135,36 +159,36 @@ __global__ __launch_bounds__(ROWS > 1 ? 64 * ROWS : 1024) void row_kernel(NormAr
   };
 
   float v[PIECES][kPiece];
-  Raw<T> rx[PIECES], rr[PIECES], rg[PIECES];
+  R rx[PIECES], rr[PIECES], rg[PIECES];
   const int pieces = (n + kPiece - 1) / kPiece;
   if constexpr (WIDE) {
     for (int p = t; p < pieces; p += threads) {
       const int col = p * kPiece;
-      rx[0].load(x + col, n - col);
-      if (r) rr[0].load(r + col, n - col);
-      if (gain && a.rows.codes) rg[0].load(gain + col, n - col);
-      joined(v[0], rx[0], rr[0]);
+      rx[0].load(x, col, n);
+      if (r) rr[0].load(r, col, n);
+      if (gain && a.rows.codes) rg[0].load(gain, col, n);
+      joined(v[0], rx[0], rr[0], col);
       if (h) store_values(h + col, v[0], n - col);
-      count(v[0], rg[0]);
+      count(v[0], rg[0], col);
     }
   } else {
     // all of it on its way at once
 #pragma unroll
-    for (int p = 0; p < PIECES; ++p) rx[p].template load<PAST>(x + (t + p * threads) * kPiece, n - (t + p * threads) * kPiece);
+    for (int p = 0; p < PIECES; ++p) rx[p].template load<PAST>(x, (t + p * threads) * kPiece, n);
     if (r) {
 #pragma unroll
-      for (int p = 0; p < PIECES; ++p) rr[p].template load<PAST>(r + (t + p * threads) * kPiece, n - (t + p * threads) * kPiece);
+      for (int p = 0; p < PIECES; ++p) rr[p].template load<PAST>(r, (t + p * threads) * kPiece, n);
     }
     if (gain) {
 #pragma unroll
-      for (int p = 0; p < PIECES; ++p) rg[p].load(gain + (t + p * threads) * kPiece, n - (t + p * threads) * kPiece);
+      for (int p = 0; p < PIECES; ++p) rg[p].load(gain, (t + p * threads) * kPiece, n);
     }
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
       const int col = (t + p * threads) * kPiece;
-      joined(v[p], rx[p], rr[p]);
+      joined(v[p], rx[p], rr[p], col);
       if (h) store_values(h + col, v[p], n - col);
-      count(v[p], rg[p]);
+      count(v[p], rg[p], col);
     }
   }
   if (NORM) sum = over_wave(sum, Plus{});
@@ -183,9 +207,9 @@ __global__ __launch_bounds__(ROWS > 1 ? 64 * ROWS : 1024) void row_kernel(NormAr
     if (NORM && a.rstd) a.rstd[row] = rstd;
     if (a.rows.codes) a.rows.scales[row] = NORM ? step * rstd : step;
   }
-  auto write = [&](const float (&v)[kPiece], const Raw<T>& rg, int col) {
+  auto write = [&](const float (&v)[kPiece], const R& rg, int col) {
     float g[kPiece];
-    gains(g, rg);
+    gains(g, rg, col);
     if (a.rows.codes) {
       float q[kPiece];
 #pragma unroll
@@ -210,13 +234,13 @@ __global__ __launch_bounds__(ROWS > 1 ? 64 * ROWS : 1024) void row_kernel(NormAr
     // whole wavefronts go round together: lanes exchange what a group's largest value is
     for (int p = t; p < (pieces + 63) / 64 * 64; p += threads) {
       const int col = p * kPiece;
-      if (gain) rg[0].load(gain + col, n - col);
+      if (gain) rg[0].load(gain, col, n);
       if (h) {
         load_values(v[0], h + col, n - col);      // this thread's own; x or the residual may be gone
       } else {
-        rx[0].load(x + col, n - col);
-        if (r) rr[0].load(r + col, n - col);
-        joined(v[0], rx[0], rr[0]);
+        rx[0].load(x, col, n);
+        if (r) rr[0].load(r, col, n);
+        joined(v[0], rx[0], rr[0], col);
       }
       write(v[0], rg[0], col);
     }
@@ -226,8 +250,8 @@ __global__ __launch_bounds__(ROWS > 1 ? 64 * ROWS : 1024) void row_kernel(NormAr
   }
 }
 
-// Inputs of this size and more are read past the caches (bfloat16 8192 x 4096: norm with residual and checkpoint 58.8 -> 53.3 us, backward 65.6 ->
-// 59.8, rows 19.7 -> 18.1, dropout with residual 38.4 -> 33.9; of half the size the norm 25.4 -> 30.2), but not by the norm and dropout of a single input
+// Inputs of this size and more are read past the caches (bfloat16 8192 x 4096: norm with residual and checkpoint 58.8 -> 53.3 us, rows
+// 19.7 -> 18.1, dropout with residual 38.4 -> 33.9; of half the size the norm 25.4 -> 30.2), but not by the norm and dropout of a single input
 // (25.6 -> 29.5, 24.3 -> 25.7).
 constexpr int64_t kPastBytes = int64_t(1) << 26;
 
@@ -252,7 +276,8 @@ hipError_t run_rows(const NormArgs& all, hipStream_t s) {
     auto threads = [&](int each) { return dim3((unsigned)((pieces + 64 * each - 1) / (64 * each)) * 64); };
     // the norm by one piece a thread where that goes: the more wavefronts, the sooner a row is there (two pieces: 1 x 4096 4.4 us, not 3.6;
     // 8192 x 4096 57.7, not 54.9); rows of more than 14 wavefronts by four pieces, so that two fit a CU (2000 x 16384 28.8 us, not 32.9)
-    if (pieces <= 64) row_kernel<T, 1, 4, NORM, false, PAST><<<dim3((n + 3) / 4), 256, 0, s>>>(a);
+    if (pieces == 1) row_kernel<T, 1, 4, NORM, false, PAST, false><<<dim3((n + 3) / 4), 256, 0, s>>>(a);
+    else if (pieces <= 64) row_kernel<T, 1, 4, NORM, false, PAST><<<dim3((n + 3) / 4), 256, 0, s>>>(a);
     else if (NORM && pieces <= 1024) row_kernel<T, 1, 1, NORM, false, PAST><<<dim3(n), threads(1), 0, s>>>(a);
     else if (pieces <= 2 * 64 * 14) row_kernel<T, 2, 1, NORM, false, PAST><<<dim3(n), threads(2), 0, s>>>(a);
     else if (pieces <= 4096) row_kernel<T, 4, 1, NORM, false, PAST><<<dim3(n), threads(4), 0, s>>>(a);
@@ -322,17 +347,17 @@ __device__ inline void load_or_ones(float (&g)[kPiece], const void* from, int co
 // A workgroup takes a row or, ROWS > 1, one to each of its wavefronts at a time, those that run together neighbouring ones; a thread keeps its columns' gain and sums,
 // and, but for the widest rows, has the next row's values on their way.  dgain: `part`, runs x `stride`, where it is wanted.  dot and sums are fp32:
 // what is added up has been rounded to fp32 once and is of the output's size.
-// Bound by memory: 8192 x 4096 bfloat16 with dh 47 to 51 us (5.3 to 5.7 TB/s); the runs' sums, 8 MiB, and norm_gain_kernel take 5 to 7 more (whole call 53, without
-// dgain 46).  Rows of
-// 8193 to 16384 features 4.0 TB/s (4096 x 11008 90 us): no registers are left for the next row's values.  Tried: two rows on their way (no gain).
-template <typename T, bool HELD, int PIECES, int ROWS, int MOST, bool PAST>
-__global__ __launch_bounds__(MOST) void norm_backward_kernel(NormBackwardArgs a, float* part, int stride) {
+// Bound by memory: 8192 x 4096 bfloat16 with dh 44 us (6.1 TB/s) without dgain; the runs' sums, 8 MiB, and norm_gain_kernel take 8 more.  Rows of
+// 8193 to 12288 features 68 us (4096 x 11008, 5.3 TB/s; without the next row on its way 76), up to 16384 4.1 TB/s.  Tried: two rows on their way (no gain).
+template <typename T, bool HELD, int PIECES, int ROWS, int MOST, bool PAST, bool ENDS = kEnds<T>>
+__global__ __launch_bounds__(MOST, MOST == 768 && PIECES == 1 ? 6 : 1) void norm_backward_kernel(NormBackwardArgs a, float* part, int stride) {
   const int threads = ROWS > 1 ? 64 : (int)blockDim.x, t = ROWS > 1 ? threadIdx.x & 63 : threadIdx.x, n = a.features;
   const int slot = ROWS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
   const int64_t step = (int64_t)gridDim.x * ROWS, last = a.samples;
+  using R = Raw<T, kPiece, ENDS>;
   struct Row {
-    Raw<T> dy[PIECES], dh[PIECES];
-    std::conditional_t<HELD, uint2, Raw<T>> h[PIECES];
+    R dy[PIECES], dh[PIECES];
+    std::conditional_t<HELD, uint2, R> h[PIECES];
     uint32_t exps[HELD ? PIECES : 1];
     float rstd;
   };
@@ -342,26 +367,26 @@ __global__ __launch_bounds__(MOST) void norm_backward_kernel(NormBackwardArgs a,
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
       const int col = (t + p * threads) * kPiece;
-      q.dy[p].template load<PAST>(static_cast<const T*>(a.dy) + row * a.lddy + col, n - col);
+      q.dy[p].template load<PAST>(static_cast<const T*>(a.dy) + row * a.lddy, col, n);
       if constexpr (HELD) {
         const int in = min(col, groups * kGroup - kPiece);                  // codes go on to the end of their group
         q.h[p] = *reinterpret_cast<const uint2*>(a.held.codes + row * ((int64_t)groups * kGroup) + in);
         q.exps[p] = a.held.exponents[row * groups + in / kGroup];
       } else {
-        q.h[p].template load<PAST>(static_cast<const T*>(a.h) + row * a.ldh + col, n - col);
+        q.h[p].template load<PAST>(static_cast<const T*>(a.h) + row * a.ldh, col, n);
       }
-      if (a.dh) q.dh[p].template load<PAST>(static_cast<const T*>(a.dh) + row * a.lddh + col, n - col);
+      if (a.dh) q.dh[p].template load<PAST>(static_cast<const T*>(a.dh) + row * a.lddh, col, n);
     }
   };
-  constexpr bool kNext = MOST <= 512;              // 1024 threads have no registers for it
-  Raw<T> gain[PIECES];
+  constexpr bool kNext = MOST <= 768;              // 1024 threads have no registers for it (2048 x 14000 60 -> 78 us)
+  R gain[PIECES];
   float sums[PIECES][kPiece] = {};
   Row now, next;
   int64_t row = (int64_t)blockIdx.x * ROWS + slot;
   if (kNext && row < last) ask(now, row);
   if (a.gain) {
 #pragma unroll
-    for (int p = 0; p < PIECES; ++p) gain[p].load(static_cast<const T*>(a.gain) + (t + p * threads) * kPiece, n - (t + p * threads) * kPiece);
+    for (int p = 0; p < PIECES; ++p) gain[p].load(static_cast<const T*>(a.gain), (t + p * threads) * kPiece, n);
   }
   __shared__ float dots[2][16];
   for (int turn = 0; row < last; row += step, turn ^= 1) {
@@ -370,18 +395,19 @@ __global__ __launch_bounds__(MOST) void norm_backward_kernel(NormBackwardArgs a,
     float dy[PIECES][kPiece], h[PIECES][kPiece], dot = 0.f;
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
-      now.dy[p].get(dy[p]);
+      const int col = (t + p * threads) * kPiece;
+      now.dy[p].get(dy[p], col, n);
       if constexpr (HELD) {
         decode(h[p], now.h[p], factor_of(now.exps[p]));                    // behind the row's end dy is 0, and so is what is made of h
-        const int left = n - (t + p * threads) * kPiece;
+        const int left = n - col;
 #pragma unroll
         for (int k = 0; k < kPiece; ++k) h[p][k] = k < left ? h[p][k] : 0.f;
       } else {
-        now.h[p].get(h[p]);
+        now.h[p].get(h[p], col, n);
       }
       float g[kPiece];
       if (a.gain) {
-        gain[p].get(g);
+        gain[p].get(g, col, n);
       } else {
 #pragma unroll
         for (int k = 0; k < kPiece; ++k) g[k] = 1.f;
@@ -407,7 +433,7 @@ __global__ __launch_bounds__(MOST) void norm_backward_kernel(NormBackwardArgs a,
       for (int p = 0; p < PIECES; ++p) {
         const int col = (t + p * threads) * kPiece;
         float d[kPiece] = {};
-        if (a.dh) now.dh[p].get(d);
+        if (a.dh) now.dh[p].get(d, col, n);
 #pragma unroll
         for (int k = 0; k < kPiece; ++k) d[k] = fmaf(now.rstd, fmaf(-h[p][k], along, dy[p][k]), d[k]);
         store_values(static_cast<T*>(a.dx) + row * a.lddx + col, d, n - col);
@@ -591,21 +617,37 @@ hipError_t run_norm_backward(const NormBackwardArgs& all, hipStream_t s) {
     const bool wide = pieces > 2 * 1024;
     int64_t run = wide ? std::max<int64_t>(1, a.samples * a.features / (1024 * 2048)) : rows;
     while (!wide && (run / rows + 1) * (run / rows + 1) * (rows > 1 ? 512 : 32) <= a.samples) run += rows;
-    // no more runs than workgroups run together, 12 wavefronts a CU
-    const int64_t together = 256 * std::max(1, 12 / waves);
+    // one piece a thread where two such workgroups of up to 12 wavefronts fit a CU, which fp32 has no registers for (by two pieces and
+    // one workgroup: bfloat16 4096 x 4608 46 us, not 40, 4096 x 6000 55, not 49; fp32 by one piece 81, by two 62)
+    const bool single = kEnds<T> && pieces > 512 && pieces <= 768;
+    // no more runs than workgroups run together: 12 wavefronts a CU, but a workgroup of five or more has it alone (its wavefronts lie on the four
+    // SIMDs unevenly)
+    const int64_t together = 256 * (waves <= 4 ? 12 / waves : single ? 2 : 1);
     if (!wide && run * together < a.samples) run = (a.samples + together * rows - 1) / (together * rows) * rows;
     const int64_t least = (a.samples + kPartFloats / stride - 1) / (kPartFloats / stride);
     if (run < least) run = (least + rows - 1) / rows * rows;
+    // as many runs for each CU (fp32 4096 x 5000 85 -> 75 us)
+    if (!wide && a.samples > 256 * run) {
+      const int64_t even = ((a.samples + run - 1) / run + 255) / 256 * 256;
+      run = ((a.samples + even - 1) / even + rows - 1) / rows * rows;
+      if (run < least) run = (least + rows - 1) / rows * rows;
+    }
     const unsigned runs = (unsigned)((a.samples + run - 1) / run);
     float* const part = a.dgain ? parts : nullptr;
     // few sums are joined in the kernel itself: no second launch (64 x 1024 fp32 6.5 us, not 6.1, but 3.5 less on the host; 300 x 513 11.3, not 7.1)
     const bool joins = part && !wide && a.samples > 0 && (int64_t)runs * stride <= int64_t(1) << 14;
     if (!joins) a.arrived = nullptr;
     if (a.samples > 0) {
-      if (pieces <= 64) norm_backward_kernel<T, HELD, 1, 4, 256, PAST><<<dim3(runs), 256, 0, s>>>(a, part, stride);
+      // 8 features or fewer: there may be no whole piece to read
+      if (pieces == 1) norm_backward_kernel<T, HELD, 1, 4, 256, PAST, false><<<dim3(runs), 256, 0, s>>>(a, part, stride);
+      else if (pieces <= 64) norm_backward_kernel<T, HELD, 1, 4, 256, PAST><<<dim3(runs), 256, 0, s>>>(a, part, stride);
       else if (pieces <= 128) norm_backward_kernel<T, HELD, 2, 4, 256, PAST><<<dim3(runs), 256, 0, s>>>(a, part, stride);
       else if (waves <= 4) norm_backward_kernel<T, HELD, 2, 1, 256, PAST><<<dim3(runs), dim3((unsigned)waves * 64), 0, s>>>(a, part, stride);
+      else if (single) {
+        if constexpr (kEnds<T>) norm_backward_kernel<T, HELD, 1, 1, 768, PAST><<<dim3(runs), dim3((unsigned)(pieces + 63) / 64 * 64), 0, s>>>(a, part, stride);
+      }
       else if (waves <= 8) norm_backward_kernel<T, HELD, 2, 1, 512, PAST><<<dim3(runs), dim3((unsigned)waves * 64), 0, s>>>(a, part, stride);
+      else if (waves <= 12) norm_backward_kernel<T, HELD, 2, 1, 768, PAST><<<dim3(runs), dim3((unsigned)waves * 64), 0, s>>>(a, part, stride);
       else if (!wide) norm_backward_kernel<T, HELD, 2, 1, 1024, PAST><<<dim3(runs), dim3((unsigned)waves * 64), 0, s>>>(a, part, stride);
       else {
         norm_along_kernel<T, HELD><<<dim3((unsigned)a.samples), 1024, 0, s>>>(a, along);
@@ -644,30 +686,33 @@ __device__ inline uint4 philox(uint4 c, uint2 key) {
 // A thread takes 16 bytes: 8 values, whose bits are one block of the generator, or in fp32 half of them (two threads make the block: a
 // thread that takes all 8 stores half lines).  Bound by memory: 8192 x 4096 bfloat16 with residual 33.9 us (5.9 TB/s).  A workgroup has a run of 256 such pieces of the whole tensor.  pieces: of a row; whole groups
 // of 32 values where a checkpoint is kept.
-template <typename T, bool PAST>
+template <typename T, bool PAST, bool ENDS>
 __global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a, int64_t row_first, uint32_t pieces) {
   constexpr int N = kWide<T>, kParts = 8 / N, kGroupPieces = kGroup / N;
   const int64_t first = (int64_t)blockIdx.x * 256, row0 = first / pieces;
   const uint32_t at = (uint32_t)(first - row0 * pieces) + threadIdx.x, piece = at % pieces;
   const int64_t row = row0 + at / pieces;
   const bool there = row < a.samples;
-  const int col = (int)piece * N, n = there ? a.features - col : 0;
+  const int col = (int)piece * N;
   float v[N], r[N] = {};
-  Raw<T, N> rx, rr;
-  rx.template load<PAST>(static_cast<const T*>(a.x) + row * a.ldx + col, n);
-  if (a.residual) rr.template load<PAST>(static_cast<const T*>(a.residual) + row * a.ldr + col, n);
+  Raw<T, N, ENDS> rx, rr;
+  // threads behind the last row read that one's
+  const int64_t from = there ? row : a.samples - 1;
+  rx.template load<PAST>(static_cast<const T*>(a.x) + from * a.ldx, col, a.features);
+  if (a.residual) rr.template load<PAST>(static_cast<const T*>(a.residual) + from * a.ldr, col, a.features);
   const uint64_t offset = a.offset + (a.more_offset ? *a.more_offset : 0);
   const uint4 bits = philox(make_uint4(piece / kParts, (uint32_t)(row_first + row), (uint32_t)offset, (uint32_t)(offset >> 32)),
                             make_uint2((uint32_t)a.seed, (uint32_t)(a.seed >> 32)));
   const bool high = kParts > 1 && piece % kParts;
   const uint32_t words[4] = {high ? bits.z : bits.x, high ? bits.w : bits.y, bits.z, bits.w};
-  rx.get(v);
-  if (a.residual) rr.get(r);
+  rx.get(v, col, a.features);
+  if (a.residual) rr.get(r, col, a.features);
 #pragma unroll
   for (int k = 0; k < N; ++k) {
     const uint32_t b = k & 1 ? words[k >> 1] >> 16 : words[k >> 1] & 0xffffu;
     v[k] = (b >= a.least ? v[k] * a.factor : 0.f) + r[k];
   }
+  const int n = there ? a.features - col : 0;
   store_values(static_cast<T*>(a.y) + row * a.ldy + col, v, n);
   if (!a.kept.codes) return;
 #pragma unroll
@@ -706,7 +751,8 @@ hipError_t launch_rms_norm(int type, const NormArgs& a, hipStream_t s) {
 hipError_t launch_rms_norm_backward(int type, const NormBackwardArgs& a, hipStream_t s) {
   return by_type(type, [&](auto zero) {
     using T = decltype(zero);
-    const bool past = a.samples * a.features * (int64_t)sizeof(T) >= kPastBytes;
+    // by values: bfloat16 of 2^25 bytes 31.3 us, past the caches 32.6, of 5.6e7 59 and 47; fp32 of 4.9e7 bytes 45.5 and 48.7, of 2^26 the same
+    const bool past = a.samples * a.features > int64_t(1) << 24;
     if (a.held.codes) return past ? run_norm_backward<T, true, true>(a, s) : run_norm_backward<T, true, false>(a, s);
     return past ? run_norm_backward<T, false, true>(a, s) : run_norm_backward<T, false, false>(a, s);
   });
@@ -725,8 +771,9 @@ hipError_t launch_dropout(int type, const DropoutArgs& all, hipStream_t s) {
       if (a.residual) a.residual = static_cast<const T*>(all.residual) + at * all.ldr;
       a.y = static_cast<T*>(all.y) + at * all.ldy;
       if (a.kept.codes) a.kept = Codes{all.kept.codes + at * pieces * N, all.kept.exponents + at * (pieces / (kGroup / N))};
-      if (past) dropout_kernel<T, true><<<dim3(blocks), 256, 0, s>>>(a, at, pieces);
-      else dropout_kernel<T, false><<<dim3(blocks), 256, 0, s>>>(a, at, pieces);
+      if (all.features < N) dropout_kernel<T, false, false><<<dim3(blocks), 256, 0, s>>>(a, at, pieces);
+      else if (past) dropout_kernel<T, true, kEnds<T>><<<dim3(blocks), 256, 0, s>>>(a, at, pieces);
+      else dropout_kernel<T, false, kEnds<T>><<<dim3(blocks), 256, 0, s>>>(a, at, pieces);
       return hipGetLastError();
     });
   });
