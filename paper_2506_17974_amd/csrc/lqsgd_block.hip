@@ -106,8 +106,8 @@ __device__ inline float root(double v) {
 
 // A row to a workgroup, PIECES of 8 values a thread in registers, or, ROWS > 1, to each of its wavefronts; WIDE: a row of any length,
 // read again for its outputs.  NORM: the norm, with what is wanted of it; otherwise 8-bit rows of x alone.  PAST: inputs past the caches.
-// Bound by memory: 8192 x 4096 bfloat16 norm with residual, checkpoint and h 51.5 us (5.9 TB/s), with 8-bit rows 42 to 45, the norm alone 26, rows alone 18 (5.6);
-// 4096 x 11008 norm 41 us (4.4).
+// Bound by memory: 8192 x 4096 bfloat16 norm with residual, checkpoint and h 50 us (6.0 TB/s), with 8-bit rows 40 (5.9), the norm alone 21 (6.3), rows
+// alone 18 (5.6); 4096 x 11008 norm 35 (5.1).
 // Tried: workgroups that stay, keep the gain and have the next row on their way (norm alone 25 -> 29 us, single rows 0.2 us more: fewer
 // wavefronts fit).
 template <typename T, int PIECES, int ROWS, bool NORM, bool WIDE, bool PAST, bool ENDS = kEnds<T>>
@@ -274,12 +274,15 @@ hipError_t run_rows(const NormArgs& all, hipStream_t s) {
     if (a.rows.codes) a.rows = Rows{all.rows.codes + at * stride, all.rows.scales + at};
     const unsigned n = (unsigned)a.samples;
     auto threads = [&](int each) { return dim3((unsigned)((pieces + 64 * each - 1) / (64 * each)) * 64); };
-    // the norm by one piece a thread where that goes: the more wavefronts, the sooner a row is there (two pieces: 1 x 4096 4.4 us, not 3.6;
-    // 8192 x 4096 57.7, not 54.9); rows of more than 14 wavefronts by four pieces, so that two fit a CU (2000 x 16384 28.8 us, not 32.9)
+    // The norm by one piece a thread where that goes: the more wavefronts, the sooner a row is there (1 x 4096 by two 3.3 us, by one 3.0; fp32 4096 x
+    // 5000 30.8 and 28.2).  Many 16-bit rows by two, which leaves more of them on a CU (8192 x 4096 21.1 us, by one 25.1; 4096 x 7000 20.5 and
+    // 30.4; but with a checkpoint, 8192 x 4096 50.8 and 49.5), and from 12 wavefronts on by four (4096 x 13500 45.6 us, by two 53.8; 4096 x 12000
+    // 41.4 and 38.8).  All others of more than 14 wavefronts by four, so that two fit a CU (2000 x 16384 28.8 us, not 32.9).
+    const bool many = NORM && kEnds<T> && a.samples > 512, two = many && (pieces > 512 || (pieces > 256 && !a.kept.codes));
     if (pieces == 1) row_kernel<T, 1, 4, NORM, false, PAST, false><<<dim3((n + 3) / 4), 256, 0, s>>>(a);
     else if (pieces <= 64) row_kernel<T, 1, 4, NORM, false, PAST><<<dim3((n + 3) / 4), 256, 0, s>>>(a);
-    else if (NORM && pieces <= 1024) row_kernel<T, 1, 1, NORM, false, PAST><<<dim3(n), threads(1), 0, s>>>(a);
-    else if (pieces <= 2 * 64 * 14) row_kernel<T, 2, 1, NORM, false, PAST><<<dim3(n), threads(2), 0, s>>>(a);
+    else if (NORM && pieces <= 1024 && !two) row_kernel<T, 1, 1, NORM, false, PAST><<<dim3(n), threads(1), 0, s>>>(a);
+    else if (pieces <= 2 * 64 * (many ? 12 : 14)) row_kernel<T, 2, 1, NORM, false, PAST><<<dim3(n), threads(2), 0, s>>>(a);
     else if (pieces <= 4096) row_kernel<T, 4, 1, NORM, false, PAST><<<dim3(n), threads(4), 0, s>>>(a);
     else row_kernel<T, 1, 1, NORM, true, false><<<dim3(n), 1024, 0, s>>>(a);
     const hipError_t e = hipGetLastError();
