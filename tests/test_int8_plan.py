@@ -55,3 +55,8 @@ def test_cases_take_the_kernels_they_are_for(exe):
                                           ((4096, 4096, 11008), "256"), ((4096, 11008, 4096), "256")])
 def test_choice(exe, asked, kernel):
     assert ip.plans(exe, [asked])[0][0] == kernel
+
+
+def test_contexts_side_by_side_share_sums_in_parts(exe):
+    """What tests/test_gpu_block_graphs.py multiplies."""
+    assert ip.plans(exe, [(64, 2048, 11008)])[0][2] > 1
