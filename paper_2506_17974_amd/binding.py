@@ -858,8 +858,9 @@ class LinearOps:
         pdg = self._vector("dgain", dgain, self._f32, n) if dgain is not None else None
         self._check(self._L.lqsgd_rms_norm_backward(self._h, self._types[T], m, n, dy.data_ptr(), lddy, ph, ldh, hc, he, ps, g, pdh, lddh,
                                                     pdx, lddx, pdg, 1 if accumulate else 0))
-        inputs = (dy, None if hc else h, rstd, gain, dh)
-        if any(t is not None and t.requires_grad for t in inputs):
+        if dy.requires_grad or rstd.requires_grad or (gain is not None and gain.requires_grad) or (dh is not None and dh.requires_grad) or \
+                (hc is None and h.requires_grad):
+            inputs = (dy, None if hc else h, rstd, gain, dh)
             dx, dgain = (_without_autograd(t, *inputs) if new and t is not None else t for new, t in ((new_dx, dx), (new_dg, dgain)))
         return dx, dgain
 
