@@ -18,21 +18,24 @@ namespace {
 __device__ inline float row_step(float absmax) {
   return absmax < __builtin_inff() ? fmaxf(absmax * (1.f / 127.f), 0x1p-126f) : __builtin_nanf("");
 }
-// Codes of 8 values, `inverse` = 1 / step; 0 where that is NaN.  |v| inverse is 127 (1 + 2^-22) at most, which rounds to 127; the product is
-// rounded before the sum that rounds it to an integer, as the definition has it.
-__device__ inline uint2 row_codes(const float (&v)[kPiece], float inverse) {
+// Codes of N values, four to a word, `inverse` = 1 / step; 0 where that is NaN.  |v| inverse is 127 (1 + 2^-22) at most, which rounds to 127; the
+// product is rounded before the sum that rounds it to an integer, as the definition has it.
+template <int N>
+__device__ inline void row_codes(uint32_t (&w)[N / 4], const float (&v)[N], float inverse) {
 #pragma clang fp contract(off)
-  uint32_t w[2];
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
+  for (int k = 0; k < N / 4; ++k) {
     uint32_t q[4];
 #pragma unroll
     for (int c = 0; c < 4; ++c) q[c] = __builtin_bit_cast(uint32_t, v[4 * k + c] * inverse + 12582912.f);
     const uint32_t low = __builtin_amdgcn_perm(q[1], q[0], 0x0c0c0400u), high = __builtin_amdgcn_perm(q[3], q[2], 0x04000c0cu);
     w[k] = inverse == inverse ? low | high : 0u;
   }
-  return make_uint2(w[0], w[1]);
 }
+
+// 16 bytes of values: neighbouring threads load and store whole lines (fp32 by 32 bytes a thread stores half a line at a time, past the caches: 8192 x
+// 4096 with 8-bit rows read back 45 us, not 24.6, norm with residual and checkpoint 111, not 94, backward 105, not 95).
+template <typename T> constexpr int kWide = 16 / (int)sizeof(T);
 
 // ---------------------------------------------------------------------------
 // norm and 8-bit rows
@@ -104,7 +107,7 @@ __device__ inline float root(double v) {
   return (float)(v > 0.0 && v < __builtin_inf() ? y + 0.5 * y * (1.0 - v * y * y) : y);
 }
 
-// A row to a workgroup, PIECES of 8 values a thread in registers, or, ROWS > 1, to each of its wavefronts; WIDE: a row of any length,
+// A row to a workgroup, PIECES of 16 bytes a thread in registers, or, ROWS > 1, to each of its wavefronts; WIDE: a row of any length,
 // read again for its outputs.  NORM: the norm, with what is wanted of it; otherwise 8-bit rows of x alone.  PAST: inputs past the caches.
 // Bound by memory: 8192 x 4096 bfloat16 norm with residual, checkpoint and h 50 us (6.0 TB/s), with 8-bit rows 40 (5.9), the norm alone 21 (6.3), rows
 // alone 18 (5.6); 4096 x 11008 norm 35 (5.1).
@@ -112,7 +115,8 @@ __device__ inline float root(double v) {
 // wavefronts fit).
 template <typename T, int PIECES, int ROWS, bool NORM, bool WIDE, bool PAST, bool ENDS = kEnds<T>>
 __global__ __launch_bounds__(ROWS > 1 ? 64 * ROWS : 1024) void row_kernel(NormArgs a) {
-  using R = Raw<T, kPiece, ENDS>;
+  constexpr int N = kWide<T>;
+  using R = Raw<T, N, ENDS>;
   const int threads = ROWS > 1 ? 64 : (int)blockDim.x, t = ROWS > 1 ? threadIdx.x & 63 : threadIdx.x;
   const int64_t row = (int64_t)blockIdx.x * ROWS + (ROWS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0);
   if (ROWS > 1 && row >= a.samples) return;
@@ -123,47 +127,47 @@ __global__ __launch_bounds__(ROWS > 1 ? 64 * ROWS : 1024) void row_kernel(NormAr
   T* const h = NORM && a.h ? static_cast<T*>(a.h) + row * a.ldh : nullptr;
 
   // values of the row from `col` on, as the norm sees them; zeros behind its end
-  auto joined = [&](float (&v)[kPiece], const R& from, const R& more, int col) {
+  auto joined = [&](float (&v)[N], const R& from, const R& more, int col) {
     from.get(v, col, n);
     if (r) {
-      float m[kPiece];
+      float m[N];
       more.get(m, col, n);
 #pragma unroll
-      for (int k = 0; k < kPiece; ++k) v[k] = widen(narrow<T>(v[k] + m[k]));
+      for (int k = 0; k < N; ++k) v[k] = widen(narrow<T>(v[k] + m[k]));
     }
   };
-  auto gains = [&](float (&g)[kPiece], const R& from, int col) {
+  auto gains = [&](float (&g)[N], const R& from, int col) {
     if (gain) {
       from.get(g, col, n);
     } else {
 #pragma unroll
-      for (int k = 0; k < kPiece; ++k) g[k] = 1.f;
+      for (int k = 0; k < N; ++k) g[k] = 1.f;
     }
   };
   double sum = 0.0;
   float most = 0.f;
-  auto count = [&](const float (&v)[kPiece], const R& rg, int col) {
+  auto count = [&](const float (&v)[N], const R& rg, int col) {
     if (NORM) {
 #pragma unroll
-      for (int k = 0; k < kPiece; ++k) sum = __builtin_fma((double)v[k], (double)v[k], sum);
+      for (int k = 0; k < N; ++k) sum = __builtin_fma((double)v[k], (double)v[k], sum);
     }
     if (!NORM) {
       most = __builtin_elementwise_maximum(most, largest(v));
     } else if (a.rows.codes) {
-      float g[kPiece];
+      float g[N];
       gains(g, rg, col);
 #pragma unroll
-      for (int k = 0; k < kPiece; ++k) g[k] *= v[k];
+      for (int k = 0; k < N; ++k) g[k] *= v[k];
       most = __builtin_elementwise_maximum(most, largest(g));
     }
   };
 
-  float v[PIECES][kPiece];
+  float v[PIECES][N];
   R rx[PIECES], rr[PIECES], rg[PIECES];
-  const int pieces = (n + kPiece - 1) / kPiece;
+  const int pieces = (n + N - 1) / N;
   if constexpr (WIDE) {
     for (int p = t; p < pieces; p += threads) {
-      const int col = p * kPiece;
+      const int col = p * N;
       rx[0].load(x, col, n);
       if (r) rr[0].load(r, col, n);
       if (gain && a.rows.codes) rg[0].load(gain, col, n);
@@ -174,18 +178,18 @@ __global__ __launch_bounds__(ROWS > 1 ? 64 * ROWS : 1024) void row_kernel(NormAr
   } else {
     // all of it on its way at once
 #pragma unroll
-    for (int p = 0; p < PIECES; ++p) rx[p].template load<PAST>(x, (t + p * threads) * kPiece, n);
+    for (int p = 0; p < PIECES; ++p) rx[p].template load<PAST>(x, (t + p * threads) * N, n);
     if (r) {
 #pragma unroll
-      for (int p = 0; p < PIECES; ++p) rr[p].template load<PAST>(r, (t + p * threads) * kPiece, n);
+      for (int p = 0; p < PIECES; ++p) rr[p].template load<PAST>(r, (t + p * threads) * N, n);
     }
     if (gain) {
 #pragma unroll
-      for (int p = 0; p < PIECES; ++p) rg[p].load(gain, (t + p * threads) * kPiece, n);
+      for (int p = 0; p < PIECES; ++p) rg[p].load(gain, (t + p * threads) * N, n);
     }
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
-      const int col = (t + p * threads) * kPiece;
+      const int col = (t + p * threads) * N;
       joined(v[p], rx[p], rr[p], col);
       if (h) store_values(h + col, v[p], n - col);
       count(v[p], rg[p], col);
@@ -207,33 +211,34 @@ __global__ __launch_bounds__(ROWS > 1 ? 64 * ROWS : 1024) void row_kernel(NormAr
     if (NORM && a.rstd) a.rstd[row] = rstd;
     if (a.rows.codes) a.rows.scales[row] = NORM ? step * rstd : step;
   }
-  auto write = [&](const float (&v)[kPiece], const R& rg, int col) {
-    float g[kPiece];
+  auto write = [&](const float (&v)[N], const R& rg, int col) {
+    float g[N];
     gains(g, rg, col);
     if (a.rows.codes) {
-      float q[kPiece];
+      float q[N];
 #pragma unroll
-      for (int k = 0; k < kPiece; ++k) q[k] = NORM ? v[k] * g[k] : v[k];
-      const uint2 w = row_codes(q, inverse);
-      if (col < stride) *reinterpret_cast<uint2*>(a.rows.codes + row * stride + col) = w;
+      for (int k = 0; k < N; ++k) q[k] = NORM ? v[k] * g[k] : v[k];
+      uint32_t w[N / 4];
+      row_codes<N>(w, q, inverse);
+      if (col < stride) __builtin_memcpy(__builtin_assume_aligned(a.rows.codes + row * stride + col, N), w, N);
     }
     if (!NORM || (!a.y && !a.kept.codes)) return;
 #pragma unroll
-    for (int k = 0; k < kPiece; ++k) g[k] *= v[k] * rstd;
+    for (int k = 0; k < N; ++k) g[k] *= v[k] * rstd;
     if (a.y) store_values(static_cast<T*>(a.y) + row * a.ldy + col, g, n - col);
     if (!a.kept.codes) return;
 #pragma unroll
-    for (int k = 0; k < kPiece; ++k) g[k] = widen(narrow<T>(g[k]));
-    uint32_t w[2], byte;
-    pack_codes<T>(w, g, group_largest<kPiece>(largest(g)), &byte);
+    for (int k = 0; k < N; ++k) g[k] = widen(narrow<T>(g[k]));
+    uint32_t w[N / 4], byte;
+    pack_codes<T>(w, g, group_largest<N>(largest(g)), &byte);
     if (col >= stride) return;
-    *reinterpret_cast<uint2*>(a.kept.codes + row * stride + col) = make_uint2(w[0], w[1]);
+    __builtin_memcpy(__builtin_assume_aligned(a.kept.codes + row * stride + col, N), w, N);
     if (col % kGroup == 0) a.kept.exponents[row * (stride / kGroup) + col / kGroup] = (uint8_t)byte;
   };
   if constexpr (WIDE) {
     // whole wavefronts go round together: lanes exchange what a group's largest value is
     for (int p = t; p < (pieces + 63) / 64 * 64; p += threads) {
-      const int col = p * kPiece;
+      const int col = p * N;
       if (gain) rg[0].load(gain, col, n);
       if (h) {
         load_values(v[0], h + col, n - col);      // this thread's own; x or the residual may be gone
@@ -246,7 +251,7 @@ __global__ __launch_bounds__(ROWS > 1 ? 64 * ROWS : 1024) void row_kernel(NormAr
     }
   } else {
 #pragma unroll
-    for (int p = 0; p < PIECES; ++p) write(v[p], rg[p], (t + p * threads) * kPiece);
+    for (int p = 0; p < PIECES; ++p) write(v[p], rg[p], (t + p * threads) * N);
   }
 }
 
@@ -273,17 +278,22 @@ hipError_t run_rows(const NormArgs& all, hipStream_t s) {
     if (a.kept.codes) a.kept = Codes{all.kept.codes + at * stride, all.kept.exponents + at * (stride / kGroup)};
     if (a.rows.codes) a.rows = Rows{all.rows.codes + at * stride, all.rows.scales + at};
     const unsigned n = (unsigned)a.samples;
+    constexpr int Q = kPiece / kWide<T>;
     auto threads = [&](int each) { return dim3((unsigned)((pieces + 64 * each - 1) / (64 * each)) * 64); };
-    // The norm by one piece a thread where that goes: the more wavefronts, the sooner a row is there (1 x 4096 by two 3.3 us, by one 3.0; fp32 4096 x
-    // 5000 30.8 and 28.2).  Many 16-bit rows by two, which leaves more of them on a CU (8192 x 4096 21.1 us, by one 25.1; 4096 x 7000 20.5 and
-    // 30.4; but with a checkpoint, 8192 x 4096 50.8 and 49.5), and from 12 wavefronts on by four (4096 x 13500 45.6 us, by two 53.8; 4096 x 12000
-    // 41.4 and 38.8).  All others of more than 14 wavefronts by four, so that two fit a CU (2000 x 16384 28.8 us, not 32.9).
-    const bool many = NORM && kEnds<T> && a.samples > 512, two = many && (pieces > 512 || (pieces > 256 && !a.kept.codes));
-    if (pieces == 1) row_kernel<T, 1, 4, NORM, false, PAST, false><<<dim3((n + 3) / 4), 256, 0, s>>>(a);
-    else if (pieces <= 64) row_kernel<T, 1, 4, NORM, false, PAST><<<dim3((n + 3) / 4), 256, 0, s>>>(a);
-    else if (NORM && pieces <= 1024 && !two) row_kernel<T, 1, 1, NORM, false, PAST><<<dim3(n), threads(1), 0, s>>>(a);
-    else if (pieces <= 2 * 64 * (many ? 12 : 14)) row_kernel<T, 2, 1, NORM, false, PAST><<<dim3(n), threads(2), 0, s>>>(a);
-    else if (pieces <= 4096) row_kernel<T, 4, 1, NORM, false, PAST><<<dim3(n), threads(4), 0, s>>>(a);
+    // Threads take 1, 2 or 4 times 8 values.  The norm by 8 where that goes: the more wavefronts, the sooner a row is there (1 x 4096 by 16 3.3 us,
+    // by 8 3.0; fp32 4096 x 5000 30.8 and 28.2).  Many rows by 16, which leaves more of them on a CU (8192 x 4096 21.1 us, by 8
+    // 25.1; 4096 x 7000 20.5 and 30.4; but with a checkpoint, 8192 x 4096 50.8 and 49.5; fp32 4096 x 7000 43.5 and 50.4, with a checkpoint 92.9
+    // and 90.4), and from 12 wavefronts on by 32 (4096 x 13500 45.6 us, by 16 53.8; 4096 x 12000 41.4 and 38.8; fp32 4096 x 13500 89 and 104).  All others of more than 14 wavefronts by 32, so that two fit a CU (2000 x 16384 28.8
+    // us, not 32.9).
+    const bool many = NORM && a.samples > 512, kept = a.kept.codes != nullptr;
+    const bool two = many && (Q == 2 ? pieces > 768 && !kept : pieces > (kept ? 512 : 256));
+    // few short fp32 rows by 4 (300 x 513 with a checkpoint 4.0 us, by 8 4.6; 1 x 4096 3.8 and 3.7)
+    if (Q == 2 && NORM && a.samples <= 512 && pieces <= 256) row_kernel<T, 1, 1, NORM, false, PAST><<<dim3(n), dim3((unsigned)(2 * pieces + 63) / 64 * 64), 0, s>>>(a);
+    else if (pieces == 1) row_kernel<T, Q, 4, NORM, false, PAST, false><<<dim3((n + 3) / 4), 256, 0, s>>>(a);
+    else if (pieces <= 64) row_kernel<T, Q, 4, NORM, false, PAST><<<dim3((n + 3) / 4), 256, 0, s>>>(a);
+    else if (NORM && pieces <= 1024 && !two) row_kernel<T, Q, 1, NORM, false, PAST><<<dim3(n), threads(1), 0, s>>>(a);
+    else if (pieces <= 2 * 64 * (many ? 12 : 14)) row_kernel<T, 2 * Q, 1, NORM, false, PAST><<<dim3(n), threads(2), 0, s>>>(a);
+    else if (pieces <= 4096) row_kernel<T, 4 * Q, 1, NORM, false, PAST><<<dim3(n), threads(4), 0, s>>>(a);
     else row_kernel<T, 1, 1, NORM, true, false><<<dim3(n), 1024, 0, s>>>(a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -296,10 +306,7 @@ hipError_t run_rows(const NormArgs& a, hipStream_t s) {
   return past ? run_rows<T, NORM, true>(a, s) : run_rows<T, NORM, false>(a, s);
 }
 
-// 16 bytes of x a thread: neighbouring threads store whole lines (fp32 by 32 bytes a thread, half a line with each store past the caches, took
-// 8192 x 4096 45 us, not 24.6; bfloat16 16.7, 6.0 TB/s).
-template <typename T> constexpr int kWide = 16 / (int)sizeof(T);
-
+// 8192 x 4096 bfloat16 16.6 us, 6.1 TB/s.
 template <typename T>
 __global__ __launch_bounds__(256) void rows_load_kernel(T* x, int64_t ldx, Rows rows, int64_t samples, int features, uint32_t pieces) {
   constexpr int N = kWide<T>;
@@ -357,10 +364,13 @@ __global__ __launch_bounds__(MOST, MOST == 768 && PIECES == 1 ? 6 : 1) void norm
   const int threads = ROWS > 1 ? 64 : (int)blockDim.x, t = ROWS > 1 ? threadIdx.x & 63 : threadIdx.x, n = a.features;
   const int slot = ROWS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
   const int64_t step = (int64_t)gridDim.x * ROWS, last = a.samples;
-  using R = Raw<T, kPiece, ENDS>;
+  // (rows of a wavefront each are as fast by 32 bytes, and the sooner there where they are few: 64 x 1024 fp32 7.0 us, by 16 7.3)
+  constexpr int N = ROWS > 1 ? kPiece : kWide<T>;
+  using R = Raw<T, N, ENDS>;
+  struct Held { uint32_t w[N / 4]; };
   struct Row {
     R dy[PIECES], dh[PIECES];
-    std::conditional_t<HELD, uint2, R> h[PIECES];
+    std::conditional_t<HELD, Held, R> h[PIECES];
     uint32_t exps[HELD ? PIECES : 1];
     float rstd;
   };
@@ -369,11 +379,11 @@ __global__ __launch_bounds__(MOST, MOST == 768 && PIECES == 1 ? 6 : 1) void norm
     q.rstd = a.rstd[row];
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
-      const int col = (t + p * threads) * kPiece;
+      const int col = (t + p * threads) * N;
       q.dy[p].template load<PAST>(static_cast<const T*>(a.dy) + row * a.lddy, col, n);
       if constexpr (HELD) {
-        const int in = min(col, groups * kGroup - kPiece);                  // codes go on to the end of their group
-        q.h[p] = *reinterpret_cast<const uint2*>(a.held.codes + row * ((int64_t)groups * kGroup) + in);
+        const int in = min(col, groups * kGroup - N);                  // codes go on to the end of their group
+        __builtin_memcpy(&q.h[p], __builtin_assume_aligned(a.held.codes + row * ((int64_t)groups * kGroup) + in, N), N);
         q.exps[p] = a.held.exponents[row * groups + in / kGroup];
       } else {
         q.h[p].template load<PAST>(static_cast<const T*>(a.h) + row * a.ldh, col, n);
@@ -383,40 +393,40 @@ __global__ __launch_bounds__(MOST, MOST == 768 && PIECES == 1 ? 6 : 1) void norm
   };
   constexpr bool kNext = MOST <= 768;              // 1024 threads have no registers for it (2048 x 14000 60 -> 78 us)
   R gain[PIECES];
-  float sums[PIECES][kPiece] = {};
+  float sums[PIECES][N] = {};
   Row now, next;
   int64_t row = (int64_t)blockIdx.x * ROWS + slot;
   if (kNext && row < last) ask(now, row);
   if (a.gain) {
 #pragma unroll
-    for (int p = 0; p < PIECES; ++p) gain[p].load(static_cast<const T*>(a.gain), (t + p * threads) * kPiece, n);
+    for (int p = 0; p < PIECES; ++p) gain[p].load(static_cast<const T*>(a.gain), (t + p * threads) * N, n);
   }
   __shared__ float dots[2][16];
   for (int turn = 0; row < last; row += step, turn ^= 1) {
     if (!kNext) ask(now, row);
     else if (row + step < last) ask(next, row + step);
-    float dy[PIECES][kPiece], h[PIECES][kPiece], dot = 0.f;
+    float dy[PIECES][N], h[PIECES][N], dot = 0.f;
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
-      const int col = (t + p * threads) * kPiece;
+      const int col = (t + p * threads) * N;
       now.dy[p].get(dy[p], col, n);
       if constexpr (HELD) {
-        decode(h[p], now.h[p], factor_of(now.exps[p]));                    // behind the row's end dy is 0, and so is what is made of h
-        const int left = n - col;
+        const float f = factor_of(now.exps[p]);
+        const int left = n - col;                                          // behind the row's end dy is 0, and so is what is made of h
 #pragma unroll
-        for (int k = 0; k < kPiece; ++k) h[p][k] = k < left ? h[p][k] : 0.f;
+        for (int k = 0; k < N; ++k) h[p][k] = k < left ? (float)(int8_t)(now.h[p].w[k / 4] >> (8 * (k % 4))) * f : 0.f;
       } else {
         now.h[p].get(h[p], col, n);
       }
-      float g[kPiece];
+      float g[N];
       if (a.gain) {
         gain[p].get(g, col, n);
       } else {
 #pragma unroll
-        for (int k = 0; k < kPiece; ++k) g[k] = 1.f;
+        for (int k = 0; k < N; ++k) g[k] = 1.f;
       }
 #pragma unroll
-      for (int k = 0; k < kPiece; ++k) {
+      for (int k = 0; k < N; ++k) {
         h[p][k] *= now.rstd;
         sums[p][k] = fmaf(dy[p][k], h[p][k], sums[p][k]);
         dy[p][k] *= g[k];
@@ -434,11 +444,11 @@ __global__ __launch_bounds__(MOST, MOST == 768 && PIECES == 1 ? 6 : 1) void norm
       const float along = dot / (float)n;
 #pragma unroll
       for (int p = 0; p < PIECES; ++p) {
-        const int col = (t + p * threads) * kPiece;
-        float d[kPiece] = {};
+        const int col = (t + p * threads) * N;
+        float d[N] = {};
         if (a.dh) now.dh[p].get(d, col, n);
 #pragma unroll
-        for (int k = 0; k < kPiece; ++k) d[k] = fmaf(now.rstd, fmaf(-h[p][k], along, dy[p][k]), d[k]);
+        for (int k = 0; k < N; ++k) d[k] = fmaf(now.rstd, fmaf(-h[p][k], along, dy[p][k]), d[k]);
         store_values(static_cast<T*>(a.dx) + row * a.lddx + col, d, n - col);
       }
     }
@@ -454,11 +464,11 @@ __global__ __launch_bounds__(MOST, MOST == 768 && PIECES == 1 ? 6 : 1) void norm
     else out[f] = v;
   };
   if constexpr (ROWS > 1) {
-    __shared__ float all[ROWS][PIECES * 64 * kPiece];
+    __shared__ float all[ROWS][PIECES * 64 * N];
 #pragma unroll
     for (int p = 0; p < PIECES; ++p)
 #pragma unroll
-      for (int k = 0; k < kPiece; ++k) all[slot][(t + p * threads) * kPiece + k] = sums[p][k];
+      for (int k = 0; k < N; ++k) all[slot][(t + p * threads) * N + k] = sums[p][k];
     __syncthreads();
     for (int f = threadIdx.x; f < n; f += 64 * ROWS) {
       float total = 0.f;
@@ -469,11 +479,11 @@ __global__ __launch_bounds__(MOST, MOST == 768 && PIECES == 1 ? 6 : 1) void norm
   } else {
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
-      const int f = (t + p * threads) * kPiece;
+      const int f = (t + p * threads) * N;
       if (f >= n) continue;                                                // `stride` has room for whole pieces
       if (joins) {
 #pragma unroll
-        for (int k = 0; k < kPiece; ++k) put(f + k, sums[p][k]);
+        for (int k = 0; k < N; ++k) put(f + k, sums[p][k]);
       } else {
         __builtin_memcpy(__builtin_assume_aligned(out + f, 16), sums[p], sizeof sums[p]);
       }
@@ -600,6 +610,7 @@ template <typename T, bool HELD, bool PAST>
 hipError_t run_norm_backward(const NormBackwardArgs& all, hipStream_t s) {
   float* const along = static_cast<float*>(all.workspace);
   float* const parts = along + kAlong;
+  constexpr int Q = kPiece / kWide<T>;
   const int64_t groups = (all.features + kGroup - 1) / kGroup;
   const int pieces = (all.features + kPiece - 1) / kPiece, stride = (all.features + 15) / 16 * 16;
   int64_t at = 0;
@@ -645,13 +656,13 @@ hipError_t run_norm_backward(const NormBackwardArgs& all, hipStream_t s) {
       if (pieces == 1) norm_backward_kernel<T, HELD, 1, 4, 256, PAST, false><<<dim3(runs), 256, 0, s>>>(a, part, stride);
       else if (pieces <= 64) norm_backward_kernel<T, HELD, 1, 4, 256, PAST><<<dim3(runs), 256, 0, s>>>(a, part, stride);
       else if (pieces <= 128) norm_backward_kernel<T, HELD, 2, 4, 256, PAST><<<dim3(runs), 256, 0, s>>>(a, part, stride);
-      else if (waves <= 4) norm_backward_kernel<T, HELD, 2, 1, 256, PAST><<<dim3(runs), dim3((unsigned)waves * 64), 0, s>>>(a, part, stride);
+      else if (waves <= 4) norm_backward_kernel<T, HELD, 2 * Q, 1, 256, PAST><<<dim3(runs), dim3((unsigned)waves * 64), 0, s>>>(a, part, stride);
       else if (single) {
         if constexpr (kEnds<T>) norm_backward_kernel<T, HELD, 1, 1, 768, PAST><<<dim3(runs), dim3((unsigned)(pieces + 63) / 64 * 64), 0, s>>>(a, part, stride);
       }
-      else if (waves <= 8) norm_backward_kernel<T, HELD, 2, 1, 512, PAST><<<dim3(runs), dim3((unsigned)waves * 64), 0, s>>>(a, part, stride);
-      else if (waves <= 12) norm_backward_kernel<T, HELD, 2, 1, 768, PAST><<<dim3(runs), dim3((unsigned)waves * 64), 0, s>>>(a, part, stride);
-      else if (!wide) norm_backward_kernel<T, HELD, 2, 1, 1024, PAST><<<dim3(runs), dim3((unsigned)waves * 64), 0, s>>>(a, part, stride);
+      else if (waves <= 8) norm_backward_kernel<T, HELD, 2 * Q, 1, 512, PAST><<<dim3(runs), dim3((unsigned)waves * 64), 0, s>>>(a, part, stride);
+      else if (waves <= 12) norm_backward_kernel<T, HELD, 2 * Q, 1, 768, PAST><<<dim3(runs), dim3((unsigned)waves * 64), 0, s>>>(a, part, stride);
+      else if (!wide) norm_backward_kernel<T, HELD, 2 * Q, 1, 1024, PAST><<<dim3(runs), dim3((unsigned)waves * 64), 0, s>>>(a, part, stride);
       else {
         norm_along_kernel<T, HELD><<<dim3((unsigned)a.samples), 1024, 0, s>>>(a, along);
         const hipError_t e = hipGetLastError();
