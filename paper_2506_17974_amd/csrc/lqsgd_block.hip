@@ -354,9 +354,9 @@ __device__ inline void load_or_ones(float (&g)[kPiece], const void* from, int co
   }
 }
 
-// A workgroup takes a row or, ROWS > 1, one to each of its wavefronts at a time, those that run together neighbouring ones; a thread keeps its columns' gain and sums,
-// and, but for the widest rows, has the next row's values on their way.  dgain: `part`, runs x `stride`, where it is wanted.  dot and sums are fp32:
-// what is added up has been rounded to fp32 once and is of the output's size.
+// A workgroup takes a row or, ROWS > 1, one to each of its wavefronts at a time, those that run together neighbouring ones; a thread keeps its
+// columns' gain and sums, and, but for the widest rows, has the next row's values on their way.  dgain: `part`, runs x `stride`, where it is
+// wanted.  dot and sums are fp32: what is added up has been rounded to fp32 once and is of the output's size.
 // Bound by memory: 8192 x 4096 bfloat16 with dh 44 us (6.1 TB/s) without dgain; the runs' sums, 8 MiB, and norm_gain_kernel take 8 more.  Rows of
 // 8193 to 12288 features 68 us (4096 x 11008, 5.3 TB/s; without the next row on its way 76), up to 16384 4.1 TB/s.  Tried: two rows on their way (no gain).
 template <typename T, bool HELD, int PIECES, int ROWS, int MOST, bool PAST, bool ENDS = kEnds<T>>
@@ -659,8 +659,7 @@ hipError_t run_norm_backward(const NormBackwardArgs& all, hipStream_t s) {
       else if (waves <= 4) norm_backward_kernel<T, HELD, 2 * Q, 1, 256, PAST><<<dim3(runs), dim3((unsigned)waves * 64), 0, s>>>(a, part, stride);
       else if (single) {
         if constexpr (kEnds<T>) norm_backward_kernel<T, HELD, 1, 1, 768, PAST><<<dim3(runs), dim3((unsigned)(pieces + 63) / 64 * 64), 0, s>>>(a, part, stride);
-      }
-      else if (waves <= 8) norm_backward_kernel<T, HELD, 2 * Q, 1, 512, PAST><<<dim3(runs), dim3((unsigned)waves * 64), 0, s>>>(a, part, stride);
+      } else if (waves <= 8) norm_backward_kernel<T, HELD, 2 * Q, 1, 512, PAST><<<dim3(runs), dim3((unsigned)waves * 64), 0, s>>>(a, part, stride);
       else if (waves <= 12) norm_backward_kernel<T, HELD, 2 * Q, 1, 768, PAST><<<dim3(runs), dim3((unsigned)waves * 64), 0, s>>>(a, part, stride);
       else if (!wide) norm_backward_kernel<T, HELD, 2 * Q, 1, 1024, PAST><<<dim3(runs), dim3((unsigned)waves * 64), 0, s>>>(a, part, stride);
       else {
