@@ -50,8 +50,12 @@ int lqsgd_rows_load(lqsgd_linear* ctx, int32_t type, int64_t samples, int32_t fe
  *   rstd    float, samples: what the backward pass needs
  *   y_codes, y_exponents   a checkpoint of y as it was rounded to `type` (the bits that lqsgd_checkpoint_save of y gives)
  *   q_codes, q_scales      8-bit rows of h gain, the scales multiplied by rstd: those of y, without y's rounding
- * is not NULL; one of the last four at least.  eps: 0 or more, finite.  Squares are added up in fp64: no value of a type overflows or
- * is lost.  A row of zeros with eps = 0 is NaN, as the formula has it.  q_scales of h gain beyond fp32's range are NaN. */
+ * is not NULL; one of the last four at least.  eps: 0 or more, finite.  Squares are added up in fp64, where none overflows or is lost.
+ * Where rstd is no normal fp32 number (mean h^2 + eps below 2^-252 or above 2^252), y and the 8-bit rows are made of h 2^k and rstd 2^-k, 2^k the power of
+ * two below rstd (2^-126 to 2^126), and so are the 8-bit rows where |h gain| stays below 2^-119 and rstd is above 1, or h gain leaves fp32's
+ * range and rstd is below 1: no digit of a small row is lost, and no large one overflows.  rstd itself is rounded to fp32; it is infinite up
+ * to a mean of 2^-256, and the gradients that the backward pass makes with it are not finite.  A row of zeros with eps = 0 is NaN, as the
+ * formula has it. */
 int lqsgd_rms_norm(lqsgd_linear* ctx, int32_t type, int64_t samples, int32_t features, double eps, const void* x, int64_t ldx,
                    const void* residual, int64_t ldr, const void* gain, void* h, int64_t ldh, void* y, int64_t ldy, float* rstd,
                    int8_t* y_codes, uint8_t* y_exponents, int8_t* q_codes, float* q_scales);

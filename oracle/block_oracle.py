@@ -44,6 +44,21 @@ def rows_save(v):
     return codes, np.where(fine, s, np.float32(np.nan)).astype(np.float32)
 
 
+def norm_rows(h, gain=None, eps=1e-6):
+    """(codes, scales) of the norm's 8-bit rows: those of h gain, their scales times rstd; of h 2^k gain, times rstd 2^-k, where rstd is not a
+    normal number, h gain is too small for the least step or beyond fp32, 2^k the power of two below rstd (2^-126 to 2^126).  Rows of finite values."""
+    h = np.asarray(h, np.float32)
+    g = np.ones(h.shape[1], np.float32) if gain is None else np.asarray(gain, np.float32)
+    with np.errstate(divide="ignore", over="ignore", under="ignore", invalid="ignore"):
+        rstd = 1.0 / np.sqrt((h.astype(np.float64) ** 2).mean(1) + eps)
+        k = np.clip(np.floor(np.log2(rstd)), -126, 126)
+        most = np.abs(h * g).max(1)
+        far = ~((rstd > 2.0 ** -126) & (rstd < 2.0 ** 126))
+        k = np.where(far | ((most > 0) & (most < 2.0 ** -119) & (rstd > 1)) | (~(most < np.inf) & (rstd < 1)), k, 0)
+        codes, scales = rows_save((h * np.exp2(k).astype(np.float32)[:, None]) * g)
+    return codes, scales.astype(np.float64) * rstd * np.exp2(-k)
+
+
 def rows_load(codes, scales, features):
     return codes[:, :features].astype(np.float64) * np.asarray(scales, np.float64)[:, None]
 

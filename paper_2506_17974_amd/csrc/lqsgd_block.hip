@@ -102,10 +102,13 @@ struct Raw {
 template <typename T> constexpr bool kEnds = sizeof(T) == 2;
 
 // 1 / sqrt(mean + eps) in fp64: the hardware's estimate and a step of Newton's on it, which leaves 2^-40.
-__device__ inline float root(double v) {
+__device__ inline double root(double v) {
   const double y = __builtin_amdgcn_rsq(v);
-  return (float)(v > 0.0 && v < __builtin_inf() ? y + 0.5 * y * (1.0 - v * y * y) : y);
+  return v > 0.0 && v < __builtin_inf() ? y + 0.5 * y * (1.0 - v * y * y) : y;
 }
+__device__ inline double power_of_two_64(int e) { return __builtin_bit_cast(double, (uint64_t)(e + 1023) << 52); }
+// Its exponent, held to what powers of two fp32 has beside their inverses.
+__device__ inline int exponent_of(double v) { return min(max((int)(__builtin_bit_cast(uint64_t, v) >> 52 & 2047) - 1023, -126), 126); }
 
 // A row to a workgroup, PIECES of 16 bytes a thread in registers, or, ROWS > 1, to each of its wavefronts; WIDE: a row of any length,
 // read again for its outputs.  NORM: the norm, with what is wanted of it; otherwise 8-bit rows of x alone.  PAST: inputs past the caches.
@@ -146,11 +149,7 @@ __global__ __launch_bounds__(ROWS > 1 ? 64 * ROWS : 1024) void row_kernel(NormAr
   };
   double sum = 0.0;
   float most = 0.f;
-  auto count = [&](const float (&v)[N], const R& rg, int col) {
-    if (NORM) {
-#pragma unroll
-      for (int k = 0; k < N; ++k) sum = __builtin_fma((double)v[k], (double)v[k], sum);
-    }
+  auto count_rows = [&](const float (&v)[N], const R& rg, int col) {
     if (!NORM) {
       most = __builtin_elementwise_maximum(most, largest(v));
     } else if (a.rows.codes) {
@@ -161,10 +160,27 @@ __global__ __launch_bounds__(ROWS > 1 ? 64 * ROWS : 1024) void row_kernel(NormAr
       most = __builtin_elementwise_maximum(most, largest(g));
     }
   };
+  auto count = [&](const float (&v)[N], const R& rg, int col) {
+    if (NORM) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) sum = __builtin_fma((double)v[k], (double)v[k], sum);
+    }
+    count_rows(v, rg, col);
+  };
 
   float v[PIECES][N];
   R rx[PIECES], rr[PIECES], rg[PIECES];
   const int pieces = (n + N - 1) / N;
+  // what this thread has read before
+  auto again = [&](float (&v)[N], int col) {
+    if (h) {
+      load_values(v, h + col, n - col);           // its own; x or the residual may be gone
+    } else {
+      rx[0].load(x, col, n);
+      if (r) rr[0].load(r, col, n);
+      joined(v, rx[0], rr[0], col);
+    }
+  };
   if constexpr (WIDE) {
     for (int p = t; p < pieces; p += threads) {
       const int col = p * N;
@@ -195,22 +211,64 @@ __global__ __launch_bounds__(ROWS > 1 ? 64 * ROWS : 1024) void row_kernel(NormAr
       count(v[p], rg[p], col);
     }
   }
+  __shared__ double sums[ROWS == 1 ? 16 : 1];
+  __shared__ float mosts[ROWS == 1 ? 16 : 1];
   if (NORM) sum = over_wave(sum, Plus{});
   if (!NORM || a.rows.codes) most = over_wave(most, Larger{});
   if (ROWS == 1 && threads > 64) {
-    __shared__ double sums[16];
-    __shared__ float mosts[16];
     if ((t & 63) == 0) sums[t >> 6] = sum, mosts[t >> 6] = most;
     __syncthreads();
     sum = 0.0, most = 0.f;
     for (int k = 0; k < threads >> 6; ++k) sum += sums[k], most = __builtin_elementwise_maximum(most, mosts[k]);
   }
-  const float rstd = NORM ? root(sum * a.inverse + a.eps) : 1.f;
-  const float step = row_step(most), inverse = 1.f / step;
-  if (t == 0) {
-    if (NORM && a.rstd) a.rstd[row] = rstd;
-    if (a.rows.codes) a.rows.scales[row] = NORM ? step * rstd : step;
+  // Rows (all of a row's threads find the same) whose root is no normal fp32 number, or whose h gain the least step would leave without digits
+  // or fp32 without a value: h is multiplied by `up`, the power of two below the root, and the rest of the root, 1 to 2, takes its place;
+  // more than that, held to the largest number, only where h is 0 and eps next to nothing.
+  float rstd = 1.f, up = 1.f;
+  auto scaled = [&](float (&v)[N]) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] *= up;
+  };
+  if constexpr (NORM) {
+    const double mean = sum * a.inverse + a.eps, exact = root(mean);
+    rstd = (float)exact;
+    if (t == 0 && a.rstd) a.rstd[row] = rstd;
+    bool far = !(rstd > 0x1p-126f && rstd < 0x1p126f);
+    if (a.rows.codes) far |= rstd > 1.f ? most > 0.f && most < 0x1p-119f : !(most < __builtin_inff());
+    if (__builtin_expect(far && mean > 0.0 && mean < __builtin_inf(), 0)) {
+      const int e = exponent_of(exact);
+      rstd = fminf((float)(exact * power_of_two_64(-e)), 0x1.fffffep127f);
+      up = power_of_two(e);
+      if constexpr (!WIDE) {
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) scaled(v[p]);
+      }
+      if (a.rows.codes) {
+        most = 0.f;
+        if constexpr (WIDE) {
+          for (int p = t; p < pieces; p += threads) {
+            again(v[0], p * N);
+            if (gain) rg[0].load(gain, p * N, n);
+            scaled(v[0]);
+            count_rows(v[0], rg[0], p * N);
+          }
+        } else {
+#pragma unroll
+          for (int p = 0; p < PIECES; ++p) count_rows(v[p], rg[p], (t + p * threads) * N);
+        }
+        most = over_wave(most, Larger{});
+        if (ROWS == 1 && threads > 64) {
+          __syncthreads();                        // all have read the first ones
+          if ((t & 63) == 0) mosts[t >> 6] = most;
+          __syncthreads();
+          most = 0.f;
+          for (int k = 0; k < threads >> 6; ++k) most = __builtin_elementwise_maximum(most, mosts[k]);
+        }
+      }
+    }
   }
+  const float step = row_step(most), inverse = 1.f / step;
+  if (t == 0 && a.rows.codes) a.rows.scales[row] = NORM ? step * rstd : step;
   auto write = [&](const float (&v)[N], const R& rg, int col) {
     float g[N];
     gains(g, rg, col);
@@ -240,13 +298,8 @@ __global__ __launch_bounds__(ROWS > 1 ? 64 * ROWS : 1024) void row_kernel(NormAr
     for (int p = t; p < (pieces + 63) / 64 * 64; p += threads) {
       const int col = p * N;
       if (gain) rg[0].load(gain, col, n);
-      if (h) {
-        load_values(v[0], h + col, n - col);      // this thread's own; x or the residual may be gone
-      } else {
-        rx[0].load(x, col, n);
-        if (r) rr[0].load(r, col, n);
-        joined(v[0], rx[0], rr[0], col);
-      }
+      again(v[0], col);
+      scaled(v[0]);
       write(v[0], rg[0], col);
     }
   } else {
