@@ -690,7 +690,7 @@ class LinearOps:
         yc, ye = self._held("save_y", save_y, m, n) if save_y is not None else (None, None)
         self._check(self._L.lqsgd_linear_forward(self._h, self._types[T], ACTS[act], m, n, k, x.data_ptr(), ldx, w.data_ptr(), ldw,
                                                  b, r, ldr, out.data_ptr(), ldy, zc, ze, yc, ye))
-        if new and (x.requires_grad or w.requires_grad or (b and bias.requires_grad) or (r and residual.requires_grad)):
+        if new and (x.requires_grad or w.requires_grad or (b and bias.requires_grad) or (residual is not None and residual.requires_grad)):
             return _without_autograd(out, x, w, bias, residual)
         return out
 
@@ -824,7 +824,7 @@ class LinearOps:
         yc, ye = self._held("save_y", save_y, m, n) if save_y is not None else (None, None)
         qc, qs = self._rows("quantize_y", quantize_y, m, n) if quantize_y is not None else (None, None)
         self._check(self._L.lqsgd_rms_norm(self._h, self._types[T], m, n, eps, x.data_ptr(), ldx, r, ldr, g, ph, ldh, py, ldy, ps, yc, ye, qc, qs))
-        if x.requires_grad or (g and gain.requires_grad) or (r and residual.requires_grad):
+        if x.requires_grad or (g and gain.requires_grad) or (residual is not None and residual.requires_grad):
             out, h, rstd = (_without_autograd(t, x, gain, residual) if new and t is not None else t
                             for new, t in ((new_y, out), (new_h, h), (new_rstd, rstd)))
         return out, h, rstd
@@ -835,7 +835,8 @@ class LinearOps:
         self._begin()
         m, n, lddy = self._matrix("dy", dy)
         T = dy.dtype
-        if isinstance(h, Checkpoint):
+        t = None if isinstance(h, Checkpoint) else h
+        if t is None:
             ph, ldh = None, 0
             hc, he = self._held("h", h, m, n)
         else:
@@ -859,9 +860,9 @@ class LinearOps:
         self._check(self._L.lqsgd_rms_norm_backward(self._h, self._types[T], m, n, dy.data_ptr(), lddy, ph, ldh, hc, he, ps, g, pdh, lddh,
                                                     pdx, lddx, pdg, 1 if accumulate else 0))
         if dy.requires_grad or rstd.requires_grad or (gain is not None and gain.requires_grad) or (dh is not None and dh.requires_grad) or \
-                (hc is None and h.requires_grad):
-            inputs = (dy, None if hc else h, rstd, gain, dh)
-            dx, dgain = (_without_autograd(t, *inputs) if new and t is not None else t for new, t in ((new_dx, dx), (new_dg, dgain)))
+                (t is not None and t.requires_grad):
+            inputs = (dy, t, rstd, gain, dh)
+            dx, dgain = (_without_autograd(o, *inputs) if new and o is not None else o for new, o in ((new_dx, dx), (new_dg, dgain)))
         return dx, dgain
 
     def int8_forward(self, x, w, bias=None, residual=None, act="none", dtype=None, out=None):
@@ -884,7 +885,7 @@ class LinearOps:
         else:
             ldy = self._matrix("out", out, T, m, n)[2]
         self._check(self._L.lqsgd_int8_forward(self._h, self._types[T], ACTS[act], m, n, k, xc, xs, wc, ws, b, r, ldr, out.data_ptr(), ldy))
-        if new and ((b and bias.requires_grad) or (r and residual.requires_grad)):
+        if new and ((b and bias.requires_grad) or (residual is not None and residual.requires_grad)):
             return _without_autograd(out, bias, residual)
         return out
 
@@ -913,6 +914,6 @@ class LinearOps:
         yc, ye = self._held("save_y", save_y, m, n) if save_y is not None else (None, None)
         self._check(self._L.lqsgd_dropout(self._h, self._types[T], m, n, p, seed, offset, more, x.data_ptr(), ldx, r, ldr, out.data_ptr(), ldy,
                                           yc, ye))
-        if new and (x.requires_grad or (r and residual.requires_grad)):
+        if new and (x.requires_grad or (residual is not None and residual.requires_grad)):
             return _without_autograd(out, x, residual)
         return out

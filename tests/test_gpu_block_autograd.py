@@ -1,0 +1,45 @@
+"""GPU tests of what autograd makes of the calls around the linear layer: a backward() that reaches one raises, whatever required the gradient, and
+forward-mode tangents are refused rather than left out."""
+import pytest
+
+from paper_2506_17974_amd import binding as B
+from tests.test_gpu_linear import _say, ops  # noqa: F401  (ops: the fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+def _needs(t):
+    return t.clone().requires_grad_()
+
+
+def _raises_in_backward(t):
+    assert t.requires_grad
+    with pytest.raises(B.LqsgdError) as e:
+        t.sum().backward()
+    assert e.value.code == B.EINVAL
+
+
+def test_empty_batch_from_a_checkpoint(ops):
+    """No samples, h from a checkpoint: the gradients of sums over nothing are zeros, and marked like those of any batch."""
+    import torch
+    _say("autograd, empty batch")
+    dy, rstd, gain = torch.empty((0, 40), device="cuda"), torch.empty(0, device="cuda"), torch.randn(40, device="cuda")
+    held = B.Checkpoint.empty(0, 40)
+    dx, dgain = ops.rms_norm_backward(dy, held, rstd, gain)
+    assert dx.shape == (0, 40) and not dgain.any() and not dgain.requires_grad
+    for args in ((_needs(dy), rstd, gain), (dy, _needs(rstd), gain), (dy, rstd, _needs(gain))):
+        dx, dgain = ops.rms_norm_backward(args[0], held, *args[1:])
+        assert dx.shape == (0, 40) and not dgain.any()
+        _raises_in_backward(dx)
+        _raises_in_backward(dgain)
+
+
+def test_empty_residual(ops):
+    """No samples: a residual of none is an input as any other."""
+    import torch
+    _say("autograd, empty residual")
+    x, w = torch.empty((0, 40), device="cuda"), torch.randn((40, 40), device="cuda")
+    r, q = _needs(x), ops.quantize(w)
+    for out in (*ops.rms_norm(x, residual=r)[:2], ops.forward(x, w, residual=r), ops.int8_forward(ops.quantize(x), q, residual=r), ops.dropout(x, 0.5, 1, residual=r)):
+        assert out.shape == (0, 40)
+        _raises_in_backward(out)
