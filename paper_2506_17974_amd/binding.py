@@ -492,6 +492,11 @@ class RowCodes:
         return self._at[0] if self._at else self._codes.shape[0]
 
     @property
+    def needs_grad(self):
+        """Whether a gradient of the scales is wanted (of those of empty(), not unless somebody has had them)."""
+        return self._scales is not None and self._scales.requires_grad
+
+    @property
     def nbytes(self):
         return self.samples * (-(-self.features // CHECKPOINT_GROUP) * CHECKPOINT_GROUP + 4)
 
@@ -533,8 +538,8 @@ class LinearOps:
     side by side takes a LinearOps each.
 
     The calls are a layer's passes, made by hand; autograd does not go through them.  A new tensor that a call returns, made from tensors that
-    require a gradient while autograd records, raises where a backward() reaches it.  Checkpoints, and tensors given for the
-    results, are plain memory: nothing is recorded for those."""
+    require a gradient while autograd records (the scales of RowCodes among them), raises where a backward() reaches it.  Checkpoints and
+    RowCodes that a call writes, and tensors given for the results, are plain memory: nothing is recorded for those."""
 
     def __init__(self):
         import torch
@@ -783,7 +788,8 @@ class LinearOps:
         self._begin()
         codes, scales = self._rows("rows", rows)
         m, n = rows.samples, rows.features
-        if out is None:
+        new = out is None
+        if new:
             dtype, ld = dtype or self._torch.bfloat16, n
             if dtype not in self._types:
                 raise LqsgdError(EINVAL, "8-bit rows are not read back as %s" % (dtype,))
@@ -791,6 +797,8 @@ class LinearOps:
         else:
             ld = self._matrix("out", out, dtype, m, n)[2]
         self._check(self._L.lqsgd_rows_load(self._h, self._types[out.dtype], m, n, codes, scales, out.data_ptr(), ld))
+        if new and rows.needs_grad:
+            return _without_autograd(out, rows.scales)
         return out
 
     def rms_norm(self, x, gain=None, residual=None, eps=1e-6, h=None, out=None, rstd=None, save_y=None, quantize_y=None, want_h=True,
@@ -885,8 +893,8 @@ class LinearOps:
         else:
             ldy = self._matrix("out", out, T, m, n)[2]
         self._check(self._L.lqsgd_int8_forward(self._h, self._types[T], ACTS[act], m, n, k, xc, xs, wc, ws, b, r, ldr, out.data_ptr(), ldy))
-        if new and ((b and bias.requires_grad) or (residual is not None and residual.requires_grad)):
-            return _without_autograd(out, bias, residual)
+        if new and ((b and bias.requires_grad) or (residual is not None and residual.requires_grad) or x.needs_grad or w.needs_grad):
+            return _without_autograd(out, bias, residual, x.scales, w.scales)
         return out
 
     def dropout(self, x, p, seed, offset=0, residual=None, out=None, save_y=None, more_offset=None):

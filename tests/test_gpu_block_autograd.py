@@ -43,3 +43,24 @@ def test_empty_residual(ops):
     for out in (*ops.rms_norm(x, residual=r)[:2], ops.forward(x, w, residual=r), ops.int8_forward(ops.quantize(x), q, residual=r), ops.dropout(x, 0.5, 1, residual=r)):
         assert out.shape == (0, 40)
         _raises_in_backward(out)
+
+
+def test_scales_that_require_a_gradient(ops):
+    """Scales of 8-bit rows given as tensors are inputs like the others."""
+    import torch
+    _say("autograd, scales")
+    q, w = (ops.quantize(torch.randn((5, 40), device="cuda")) for _ in range(2))
+    plain = ops.int8_forward(q, w, dtype=torch.float32)
+    mine = [B.RowCodes(c.codes, _needs(c.scales), 40) for c in (q, w)]
+    assert not plain.requires_grad and not ops.dequantize(q).requires_grad
+    for args in ((mine[0], w), (q, mine[1])):
+        y = ops.int8_forward(*args, dtype=torch.float32)
+        assert torch.equal(y.detach(), plain)
+        _raises_in_backward(y)
+    _raises_in_backward(ops.dequantize(mine[0]))
+    q.scales.requires_grad_()                                 # of one made by the calls, too
+    _raises_in_backward(ops.dequantize(q))
+    with torch.no_grad():
+        assert not ops.dequantize(q).requires_grad and not ops.int8_forward(q, mine[1]).requires_grad
+    out = torch.empty((5, 40), device="cuda")
+    assert ops.dequantize(mine[0], out=out) is out and not out.requires_grad       # plain memory
