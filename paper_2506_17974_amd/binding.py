@@ -538,14 +538,16 @@ class LinearOps:
     side by side takes a LinearOps each.
 
     The calls are a layer's passes, made by hand; autograd does not go through them.  A new tensor that a call returns, made from tensors that
-    require a gradient while autograd records (the scales of RowCodes among them), raises where a backward() reaches it.  Checkpoints and
-    RowCodes that a call writes, and tensors given for the results, are plain memory: nothing is recorded for those."""
+    require a gradient while autograd records (the scales of RowCodes among them), raises where a backward() reaches it; a call that would make
+    one from a tensor with a forward-mode tangent is refused.  Checkpoints and RowCodes that a call writes, and tensors given for the
+    results, are plain memory: nothing is recorded for those."""
 
     def __init__(self):
         import torch
         if not torch.cuda.is_available():
             raise RuntimeError("no GPU visible: the linear layer has no CPU path")
-        self._torch, self._Tensor, self._empty = torch, torch.Tensor, torch.empty
+        import torch.autograd.forward_ad as dual
+        self._torch, self._Tensor, self._empty, self._dual = torch, torch.Tensor, torch.empty, dual
         self._types = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16, torch.float16: TYPE_F16}
         self._f32, self._codes_type, self._exponents_type = torch.float32, torch.int8, torch.uint8
         self._h = C.c_void_p()
@@ -633,6 +635,14 @@ class LinearOps:
             self._bad("%s: contiguous int8 codes of %d x %d wanted" % (what, samples, stride), codes)
         return codes.data_ptr(), self._vector("%s's scales" % what, scales, self._f32, samples)
 
+    def _new(self, inputs, *shape, dtype):
+        """A tensor for a result of `inputs` (None: not there).  Forward-mode tangents on them would be left out in silence, and are refused."""
+        if getattr(self._dual, "_current_level", 0) >= 0:
+            for t in inputs:
+                if t is not None and self._dual.unpack_dual(t).tangent is not None:
+                    raise LqsgdError(EINVAL, "an input carries a forward-mode tangent, which the linear layer's calls do not pass on")
+        return self._empty(*shape, dtype=dtype, device=self.device)
+
     def close(self):
         if self._h:
             self._L.lqsgd_linear_destroy(self._h)
@@ -688,7 +698,7 @@ class LinearOps:
         new = out is None
         r, ldr = (residual.data_ptr(), self._matrix("residual", residual, T, m, n)[2]) if residual is not None else (None, 0)
         if out is None:
-            out, ldy = self._empty(m, n, dtype=T, device=self.device), n
+            out, ldy = self._new((x, w, bias, residual), m, n, dtype=T), n
         else:
             ldy = self._matrix("out", out, T, m, n)[2]
         zc, ze = self._held("save_z", save_z, m, n) if save_z is not None else (None, None)
@@ -715,12 +725,12 @@ class LinearOps:
         if dz is not None:
             pz, lddz = dz.data_ptr(), self._matrix("dz", dz, T, m, n)[2]
         elif want_dz:
-            dz = self._empty(m, n, dtype=T, device=self.device)
+            dz = self._new((dy,), m, n, dtype=T)
             pz, lddz = dz.data_ptr(), n
         if dbias is None and want_dbias:
             if accumulate:
                 raise LqsgdError(EINVAL, "accumulate needs the dbias to add to")
-            dbias = self._empty(n, dtype=self._f32, device=self.device)
+            dbias = self._new((dy,), n, dtype=self._f32)
         db = self._vector("dbias", dbias, self._f32, n) if dbias is not None else None
         self._check(self._L.lqsgd_linear_activation_backward(self._h, self._types[T], ACTS[act], m, n, dy.data_ptr(), lddy, zc, ze, pz, lddz,
                                                              db, 1 if accumulate else 0))
@@ -739,7 +749,7 @@ class LinearOps:
         _, k, ldw = self._matrix("w", w, T, n, None)
         new = out is None
         if new:
-            out, lddx = self._empty(m, k, dtype=T, device=self.device), k
+            out, lddx = self._new((dz, w), m, k, dtype=T), k
         else:
             lddx = self._matrix("out", out, T, m, k)[2]
         self._check(self._L.lqsgd_linear_input_grad(self._h, self._types[T], m, n, k, dz.data_ptr(), lddz, w.data_ptr(), ldw, out.data_ptr(),
@@ -763,7 +773,7 @@ class LinearOps:
             dtype, lddw = dtype or self._f32, k
             if dtype not in self._types:
                 raise LqsgdError(EINVAL, "a gradient is not written as %s" % (dtype,))
-            out = self._empty(n, k, dtype=dtype, device=self.device)
+            out = self._new((dz,), n, k, dtype=dtype)
         else:
             lddw = self._matrix("out", out, dtype, n, k)[2]
         self._check(self._L.lqsgd_linear_weight_grad(self._h, self._types[dz.dtype], m, n, k, dz.data_ptr(), lddz, xc, xe,
@@ -793,7 +803,7 @@ class LinearOps:
             dtype, ld = dtype or self._torch.bfloat16, n
             if dtype not in self._types:
                 raise LqsgdError(EINVAL, "8-bit rows are not read back as %s" % (dtype,))
-            out = self._empty(m, n, dtype=dtype, device=self.device)
+            out = self._new((rows._scales,), m, n, dtype=dtype)
         else:
             ld = self._matrix("out", out, dtype, m, n)[2]
         self._check(self._L.lqsgd_rows_load(self._h, self._types[out.dtype], m, n, codes, scales, out.data_ptr(), ld))
@@ -815,7 +825,7 @@ class LinearOps:
         if residual is not None:
             r, ldr = residual.data_ptr(), self._matrix("residual", residual, T, m, n)[2]
             if new_h and want_h:
-                h, ldh = self._empty(m, n, dtype=T, device=self.device), n
+                h, ldh = self._new((x, gain, residual), m, n, dtype=T), n
                 ph = h.data_ptr()
         if not new_h:
             if residual is None:
@@ -824,10 +834,10 @@ class LinearOps:
         if not new_y:
             py, ldy = out.data_ptr(), self._matrix("out", out, T, m, n)[2]
         elif want_y:
-            out, ldy = self._empty(m, n, dtype=T, device=self.device), n
+            out, ldy = self._new((x, gain, residual), m, n, dtype=T), n
             py = out.data_ptr()
         if new_rstd and want_rstd:
-            rstd = self._empty(m, dtype=self._f32, device=self.device)
+            rstd = self._new((x, gain, residual), m, dtype=self._f32)
         ps = self._vector("rstd", rstd, self._f32, m) if rstd is not None else None
         yc, ye = self._held("save_y", save_y, m, n) if save_y is not None else (None, None)
         qc, qs = self._rows("quantize_y", quantize_y, m, n) if quantize_y is not None else (None, None)
@@ -858,12 +868,12 @@ class LinearOps:
         if not new_dx:
             pdx, lddx = dx.data_ptr(), self._matrix("dx", dx, T, m, n)[2]
         elif want_dx:
-            dx, lddx = self._empty(m, n, dtype=T, device=self.device), n
+            dx, lddx = self._new((dy, t, rstd, gain, dh), m, n, dtype=T), n
             pdx = dx.data_ptr()
         if new_dg and want_dgain:
             if accumulate:
                 raise LqsgdError(EINVAL, "accumulate needs the dgain to add to")
-            dgain = self._empty(n, dtype=self._f32, device=self.device)
+            dgain = self._new((dy, t, rstd, gain, dh), n, dtype=self._f32)
         pdg = self._vector("dgain", dgain, self._f32, n) if dgain is not None else None
         self._check(self._L.lqsgd_rms_norm_backward(self._h, self._types[T], m, n, dy.data_ptr(), lddy, ph, ldh, hc, he, ps, g, pdh, lddh,
                                                     pdx, lddx, pdg, 1 if accumulate else 0))
@@ -889,7 +899,7 @@ class LinearOps:
         b = self._vector("bias", bias, T, n) if bias is not None else None
         r, ldr = (residual.data_ptr(), self._matrix("residual", residual, T, m, n)[2]) if residual is not None else (None, 0)
         if new:
-            out, ldy = self._empty(m, n, dtype=T, device=self.device), n
+            out, ldy = self._new((bias, residual, x._scales, w._scales), m, n, dtype=T), n
         else:
             ldy = self._matrix("out", out, T, m, n)[2]
         self._check(self._L.lqsgd_int8_forward(self._h, self._types[T], ACTS[act], m, n, k, xc, xs, wc, ws, b, r, ldr, out.data_ptr(), ldy))
@@ -916,7 +926,7 @@ class LinearOps:
         new = out is None
         r, ldr = (residual.data_ptr(), self._matrix("residual", residual, T, m, n)[2]) if residual is not None else (None, 0)
         if new:
-            out, ldy = self._empty(m, n, dtype=T, device=self.device), n
+            out, ldy = self._new((x, residual), m, n, dtype=T), n
         else:
             ldy = self._matrix("out", out, T, m, n)[2]
         yc, ye = self._held("save_y", save_y, m, n) if save_y is not None else (None, None)

@@ -64,3 +64,46 @@ def test_scales_that_require_a_gradient(ops):
         assert not ops.dequantize(q).requires_grad and not ops.int8_forward(q, mine[1]).requires_grad
     out = torch.empty((5, 40), device="cuda")
     assert ops.dequantize(mine[0], out=out) is out and not out.requires_grad       # plain memory
+
+
+def test_forward_mode_tangents(ops):
+    """A tangent on an input of what would be a new tensor is refused; tensors given for the results are plain memory, here too."""
+    import torch
+    import torch.autograd.forward_ad as ad
+    _say("autograd, tangents")
+    g = torch.Generator(device="cuda").manual_seed(4)
+    x, r, w = (torch.randn((40, 40), generator=g, device="cuda") for _ in range(3))
+    gain = torch.randn(40, generator=g, device="cuda")
+    held, q = ops.save(x), ops.quantize(x)
+    rstd = ops.rms_norm(x, want_rstd=True, want_y=False)[2]
+    calls = {                                                # what is called, and its inputs
+        "forward": (lambda a, b, c, d: ops.forward(a, b, c, d), (x, w, gain, r)),
+        "activation_backward": (lambda a: ops.activation_backward(a), (x,)),
+        "input_grad": (lambda a, b: ops.input_grad(a, b), (x, w)),
+        "weight_grad": (lambda a: ops.weight_grad(a, held), (x,)),
+        "rms_norm": (lambda a, b, c: ops.rms_norm(a, b, c), (x, gain, r)),
+        "rstd alone": (lambda a: ops.rms_norm(a, want_y=False, want_rstd=True), (x,)),
+        "h alone": (lambda a, b: ops.rms_norm(a, residual=b, out=torch.empty_like(x)), (x, r)),
+        "rms_norm_backward": (lambda a, b, c, d, e: ops.rms_norm_backward(a, b, c, d, e), (x, w, rstd, gain, r)),
+        "dgain alone": (lambda a, b, c: ops.rms_norm_backward(a, held, b, c, want_dx=False), (x, rstd, gain)),
+        "dequantize": (lambda s: ops.dequantize(B.RowCodes(q.codes, s, 40)), (q.scales,)),
+        "int8_forward": (lambda a, b, c, d: ops.int8_forward(B.RowCodes(q.codes, c, 40), B.RowCodes(q.codes, d, 40), a, b), (gain, r, q.scales, q.scales)),
+        "dropout": (lambda a, b: ops.dropout(a, 0.5, 1, residual=b), (x, r)),
+    }
+    for name, (call, args) in calls.items():
+        call(*args)
+        with ad.dual_level():
+            call(*args)                                      # a level without tangents is no matter
+            for k in range(len(args)):
+                duals = [ad.make_dual(t, torch.ones_like(t)) if i == k else t for i, t in enumerate(args)]
+                with pytest.raises(B.LqsgdError) as e:
+                    call(*duals)
+                assert e.value.code == B.EINVAL and "tangent" in str(e.value), (name, k)
+    with ad.dual_level():
+        d, out = ad.make_dual(x, torch.ones_like(x)), torch.empty_like(x)
+        assert ops.rms_norm(d, out=out)[0] is out and ad.unpack_dual(out).tangent is None
+        ops.save(d, out=held)
+        ops.quantize(d, out=q)
+        ops.rms_norm(d, quantize_y=q, want_y=False)
+    with pytest.raises(Exception):                           # a transform's own tensors have no memory
+        torch.func.jvp(lambda t: ops.rms_norm(t)[0], (x,), (x,))
