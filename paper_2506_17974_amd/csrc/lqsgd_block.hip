@@ -509,7 +509,7 @@ __global__ __launch_bounds__(MOST, MOST == 768 && PIECES == 1 ? 6 : 1) void norm
   }
   if (!part) return;
   float* const out = part + (int64_t)blockIdx.x * stride;
-  const bool joins = a.arrived != nullptr, whole = joins && gridDim.x == 1;
+  const bool whole = a.arrived != nullptr && gridDim.x == 1, joins = ROWS > 1 && a.arrived != nullptr;
   auto put = [&](int f, float v) {
     if (f >= n) return;
     if (whole) a.dgain[f] = a.accumulate ? a.dgain[f] + v : v;
@@ -532,9 +532,10 @@ __global__ __launch_bounds__(MOST, MOST == 768 && PIECES == 1 ? 6 : 1) void norm
   } else {
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
-      const int f = (t + p * threads) * N;
+      int f = (t + p * threads) * N;
+      asm volatile("" : "+v"(f));                                          // found anew: what would be kept of it through the loop goes to scratch in its stead
       if (f >= n) continue;                                                // `stride` has room for whole pieces
-      if (joins) {
+      if (whole) {
 #pragma unroll
         for (int k = 0; k < N; ++k) put(f + k, sums[p][k]);
       } else {
@@ -542,41 +543,43 @@ __global__ __launch_bounds__(MOST, MOST == 768 && PIECES == 1 ? 6 : 1) void norm
       }
     }
   }
-  if (!joins || whole) return;
-  // The workgroup that comes last joins the runs' sums, in the runs' order, whichever it is.  They are stored and read with agent-scope
-  // atomics, which go past the caches that the XCDs do not share: every store has arrived when vmcnt says so, and the barrier puts all of the
-  // workgroup's before its count.
-  __shared__ int last_one;
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(0);
-  asm volatile("" ::: "memory");
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    last_one = __hip_atomic_fetch_add(a.arrived, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.x - 1;
-    if (last_one) __hip_atomic_store(a.arrived, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);        // for the next launch
-  }
-  __syncthreads();
-  if (!last_one) return;
-  // two columns and 16 runs at a time
-  for (int f = 2 * (int)threadIdx.x; f < n; f += 2 * (int)blockDim.x) {
-    float total[2] = {};
-    for (int k = 0; k < (int)gridDim.x; k += 16) {
-      uint64_t x[16];
-#pragma unroll
-      for (int u = 0; u < 16; ++u)
-        x[u] = __hip_atomic_load(reinterpret_cast<const uint64_t*>(part + (int64_t)min(k + u, (int)gridDim.x - 1) * stride + f), __ATOMIC_RELAXED,
-                                 __HIP_MEMORY_SCOPE_AGENT);
-#pragma unroll
-      for (int u = 0; u < 16; ++u) {
-        float v[2];
-        __builtin_memcpy(v, &x[u], sizeof v);
-#pragma unroll
-        for (int c = 0; c < 2; ++c) total[c] += k + u < (int)gridDim.x ? v[c] : 0.f;
-      }
+  if constexpr (ROWS > 1) {
+    if (!joins || whole) return;
+    // The workgroup that comes last joins the runs' sums, in the runs' order, whichever it is.  They are stored and read with agent-scope
+    // atomics, which go past the caches that the XCDs do not share: every store has arrived when vmcnt says so, and the barrier puts all of the
+    // workgroup's before its count.
+    __shared__ int last_one;
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0);
+    asm volatile("" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      last_one = __hip_atomic_fetch_add(a.arrived, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.x - 1;
+      if (last_one) __hip_atomic_store(a.arrived, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);        // for the next launch
     }
+    __syncthreads();
+    if (!last_one) return;
+    // two columns and 16 runs at a time
+    for (int f = 2 * (int)threadIdx.x; f < n; f += 2 * (int)blockDim.x) {
+      float total[2] = {};
+      for (int k = 0; k < (int)gridDim.x; k += 16) {
+        uint64_t x[16];
 #pragma unroll
-    for (int c = 0; c < 2; ++c)
-      if (f + c < n) a.dgain[f + c] = a.accumulate ? a.dgain[f + c] + total[c] : total[c];
+        for (int u = 0; u < 16; ++u)
+          x[u] = __hip_atomic_load(reinterpret_cast<const uint64_t*>(part + (int64_t)min(k + u, (int)gridDim.x - 1) * stride + f), __ATOMIC_RELAXED,
+                                   __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+        for (int u = 0; u < 16; ++u) {
+          float v[2];
+          __builtin_memcpy(v, &x[u], sizeof v);
+#pragma unroll
+          for (int c = 0; c < 2; ++c) total[c] += k + u < (int)gridDim.x ? v[c] : 0.f;
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+        if (f + c < n) a.dgain[f + c] = a.accumulate ? a.dgain[f + c] + total[c] : total[c];
+    }
   }
 }
 
@@ -701,8 +704,10 @@ hipError_t run_norm_backward(const NormBackwardArgs& all, hipStream_t s) {
     }
     const unsigned runs = (unsigned)((a.samples + run - 1) / run);
     float* const part = a.dgain ? parts : nullptr;
-    // few sums are joined in the kernel itself: no second launch (64 x 1024 fp32 6.5 us, not 6.1, but 3.5 less on the host; 300 x 513 11.3, not 7.1)
-    const bool joins = part && !wide && a.samples > 0 && (int64_t)runs * stride <= int64_t(1) << 14;
+    // One run's sums, and few that wavefronts with a row each have made, are joined in the kernel itself: no second launch, 3 us less on the host.
+    // The last workgroup does that by itself, 16 runs at a time (us, itself / second launch, bfloat16: 64 x 256 4.8 / 5.4, 64 x 1024 6.5 / 6.0,
+    // 256 x 64 6.8 / 5.4; not so 512 x 32 9.5 / 5.4, 8192 x 16 28.4 / 8.3, 300 x 513 11.1 / 6.8, nor runs of a row to a workgroup, 2 x 2048 10.1 / 5.5).
+    const bool joins = part && !wide && a.samples > 0 && (runs == 1 || (rows > 1 && runs <= 64)) && (int64_t)runs * stride <= int64_t(1) << 14;
     if (!joins) a.arrived = nullptr;
     if (a.samples > 0) {
       // 8 features or fewer: there may be no whole piece to read

@@ -15,6 +15,9 @@ SEVERAL = [(601, 1500), (601, 3001), (601, 4608), (601, 7001), (601, 8192), (601
 # more than 2^24 values: inputs past the caches
 LARGE = [(35000, 481), (8200, 2049), (4200, 4099), (3300, 5090), (2400, 7003), (1600, 11003), (1200, 14003), (1060, 16001), (1000, 17003)]
 
+# to either side of where one kernel makes dgain: a run alone, up to 64 runs of four rows, one row or more to a workgroup
+FEW = [(1, 9), (4, 1024), (5, 1024), (64, 1024), (65, 1024), (256, 64), (257, 64), (260, 24), (512, 32), (1, 1025), (2, 1025), (1, 4097), (2, 4097), (1, 16384), (2, 16384)]
+
 
 def _check(ops, kind, samples, features, source):
     import torch
@@ -65,3 +68,11 @@ def test_several_rows_to_a_workgroup(ops, kind, samples, features, source):
 def test_past_the_caches(ops, kind, samples, features, source):
     assert samples * features > 1 << 24
     _check(ops, kind, samples, features, source)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("samples,features", FEW)
+@pytest.mark.parametrize("source", ["tensor", "checkpoint"])
+def test_few_runs(ops, kind, samples, features, source):
+    for _ in range(2):                                        # whoever joins the runs leaves the count as it was
+        _check(ops, kind, samples, features, source)
