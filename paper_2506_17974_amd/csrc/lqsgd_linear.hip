@@ -148,6 +148,23 @@ __global__ __launch_bounds__(256) void activation_backward_kernel(const T* dy, i
   }
 }
 
+// Features' sums over `runs` runs of samples, in the runs' order by four.
+__global__ __launch_bounds__(256) void sum_runs_kernel(const float* part, float* dbias, int accumulate, int rows, int runs) {
+  __shared__ float sums[4][64];
+  const int f = (int)blockIdx.x * 64 + (threadIdx.x & 63), w = threadIdx.x >> 6;
+  float s = 0.f;
+  if (f < rows) {
+#pragma unroll 8
+    for (int k = w; k < runs; k += 4) s += part[(int64_t)k * rows + f];
+  }
+  sums[w][threadIdx.x & 63] = s;
+  __syncthreads();
+  if (w == 0 && f < rows) {
+    s = (sums[0][threadIdx.x] + sums[1][threadIdx.x]) + (sums[2][threadIdx.x] + sums[3][threadIdx.x]);
+    dbias[f] = accumulate ? dbias[f] + s : s;
+  }
+}
+
 // ---------------------------------------------------------------------------
 // products
 // ---------------------------------------------------------------------------

@@ -271,24 +271,6 @@ hipError_t by_slabs(int64_t samples, uint32_t pieces, F&& launch) {
   return hipSuccess;
 }
 
-// Features' sums over `runs` runs of samples, in the runs' order by four.
-template <typename Sum>
-__global__ __launch_bounds__(256) void sum_runs_kernel(const Sum* part, Sum* dbias, int accumulate, int rows, int runs) {
-  __shared__ Sum sums[4][64];
-  const int f = (int)blockIdx.x * 64 + (threadIdx.x & 63), w = threadIdx.x >> 6;
-  Sum s = 0;
-  if (f < rows) {
-#pragma unroll 8
-    for (int k = w; k < runs; k += 4) s += part[(int64_t)k * rows + f];
-  }
-  sums[w][threadIdx.x & 63] = s;
-  __syncthreads();
-  if (w == 0 && f < rows) {
-    s = (sums[0][threadIdx.x] + sums[1][threadIdx.x]) + (sums[2][threadIdx.x] + sums[3][threadIdx.x]);
-    dbias[f] = accumulate ? dbias[f] + s : s;
-  }
-}
-
 // ---------------------------------------------------------------------------
 // a tile's end
 // ---------------------------------------------------------------------------
