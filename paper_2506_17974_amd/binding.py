@@ -5,6 +5,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import types
 from typing import List, Optional, Sequence
 
 import numpy as np
@@ -492,11 +493,6 @@ class RowCodes:
         return self._at[0] if self._at else self._codes.shape[0]
 
     @property
-    def needs_grad(self):
-        """Whether a gradient of the scales is wanted (of those of empty(), not unless somebody has had them)."""
-        return self._scales is not None and self._scales.requires_grad
-
-    @property
     def nbytes(self):
         return self.samples * (-(-self.features // CHECKPOINT_GROUP) * CHECKPOINT_GROUP + 4)
 
@@ -547,7 +543,9 @@ class LinearOps:
         if not torch.cuda.is_available():
             raise RuntimeError("no GPU visible: the linear layer has no CPU path")
         import torch.autograd.forward_ad as dual
-        self._torch, self._Tensor, self._empty, self._dual = torch, torch.Tensor, torch.empty, dual
+        self._torch, self._Tensor, self._empty = torch, torch.Tensor, torch.empty
+        # inputs are asked for tangents within a level of forward-mode differentiation, or always where torch does not say that there is one
+        self._dual = dual if hasattr(dual, "_current_level") else types.SimpleNamespace(_current_level=0, unpack_dual=dual.unpack_dual)
         self._types = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16, torch.float16: TYPE_F16}
         self._f32, self._codes_type, self._exponents_type = torch.float32, torch.int8, torch.uint8
         self._h = C.c_void_p()
@@ -570,12 +568,14 @@ class LinearOps:
             raise LqsgdError(rc, self._L.lqsgd_linear_last_error(self._h).decode())
 
     def _begin(self):
+        """Whether the call may go on; True: after a look for tangents."""
         if not self._h:
             raise LqsgdError(ESTATE, "the context is closed")
         if self._current_device is not None and self._current_device() != self._index:
             raise LqsgdError(ESTATE, "the current device is not the one this context was made on, %s" % self.device)
         if self._stream(self._index) != self.stream_handle:
             raise LqsgdError(ESTATE, "the current stream is not the one this context was made on")
+        return self._dual._current_level >= 0                 # inputs may have forward-mode tangents
 
     def _bad(self, what, t):
         raise LqsgdError(ESHAPE, "%s: %s" % (what, "%s %s on %s, strides %s" % (t.dtype, tuple(t.shape), t.device, t.stride())
@@ -635,13 +635,11 @@ class LinearOps:
             self._bad("%s: contiguous int8 codes of %d x %d wanted" % (what, samples, stride), codes)
         return codes.data_ptr(), self._vector("%s's scales" % what, scales, self._f32, samples)
 
-    def _new(self, inputs, *shape, dtype):
-        """A tensor for a result of `inputs` (None: not there).  Forward-mode tangents on them would be left out in silence, and are refused."""
-        if getattr(self._dual, "_current_level", 0) >= 0:
-            for t in inputs:
-                if t is not None and self._dual.unpack_dual(t).tangent is not None:
-                    raise LqsgdError(EINVAL, "an input carries a forward-mode tangent, which the linear layer's calls do not pass on")
-        return self._empty(*shape, dtype=dtype, device=self.device)
+    def _no_tangents(self, *inputs):
+        """Forward-mode tangents would be left out of a new result in silence."""
+        for t in inputs:
+            if isinstance(t, self._Tensor) and self._dual.unpack_dual(t).tangent is not None:
+                raise LqsgdError(EINVAL, "an input carries a forward-mode tangent, which the linear layer's calls do not pass on")
 
     def close(self):
         if self._h:
@@ -688,7 +686,8 @@ class LinearOps:
     # -- forward ---------------------------------------------------------
     def forward(self, x, w, bias=None, residual=None, act="none", out=None, save_z=None, save_y=None):
         """act(x w^T + bias) + residual.  save_z, save_y: Checkpoints of samples x rows that receive z and y as well."""
-        self._begin()
+        if self._begin() and out is None:
+            self._no_tangents(x, w, bias, residual)
         m, k, ldx = self._matrix("x", x)
         T = x.dtype
         n, _, ldw = self._matrix("w", w, T, None, k)
@@ -698,7 +697,7 @@ class LinearOps:
         new = out is None
         r, ldr = (residual.data_ptr(), self._matrix("residual", residual, T, m, n)[2]) if residual is not None else (None, 0)
         if out is None:
-            out, ldy = self._new((x, w, bias, residual), m, n, dtype=T), n
+            out, ldy = self._empty(m, n, dtype=T, device=self.device), n
         else:
             ldy = self._matrix("out", out, T, m, n)[2]
         zc, ze = self._held("save_z", save_z, m, n) if save_z is not None else (None, None)
@@ -712,7 +711,8 @@ class LinearOps:
     # -- backward --------------------------------------------------------
     def activation_backward(self, dy, z=None, act="none", dz=None, dbias=None, accumulate=False, want_dz=True, want_dbias=True):
         """(dz, dbias) of dy and the checkpoint z (not needed without an activation); what is not wanted is None.  dz may be dy."""
-        self._begin()
+        if self._begin() and ((dz is None and want_dz) or (dbias is None and want_dbias)):
+            self._no_tangents(dy)
         m, n, lddy = self._matrix("dy", dy)
         T = dy.dtype
         if act not in ACTS:
@@ -725,12 +725,12 @@ class LinearOps:
         if dz is not None:
             pz, lddz = dz.data_ptr(), self._matrix("dz", dz, T, m, n)[2]
         elif want_dz:
-            dz = self._new((dy,), m, n, dtype=T)
+            dz = self._empty(m, n, dtype=T, device=self.device)
             pz, lddz = dz.data_ptr(), n
         if dbias is None and want_dbias:
             if accumulate:
                 raise LqsgdError(EINVAL, "accumulate needs the dbias to add to")
-            dbias = self._new((dy,), n, dtype=self._f32)
+            dbias = self._empty(n, dtype=self._f32, device=self.device)
         db = self._vector("dbias", dbias, self._f32, n) if dbias is not None else None
         self._check(self._L.lqsgd_linear_activation_backward(self._h, self._types[T], ACTS[act], m, n, dy.data_ptr(), lddy, zc, ze, pz, lddz,
                                                              db, 1 if accumulate else 0))
@@ -743,13 +743,14 @@ class LinearOps:
 
     def input_grad(self, dz, w, out=None):
         """dz w."""
-        self._begin()
+        if self._begin() and out is None:
+            self._no_tangents(dz, w)
         m, n, lddz = self._matrix("dz", dz)
         T = dz.dtype
         _, k, ldw = self._matrix("w", w, T, n, None)
         new = out is None
         if new:
-            out, lddx = self._new((dz, w), m, k, dtype=T), k
+            out, lddx = self._empty(m, k, dtype=T, device=self.device), k
         else:
             lddx = self._matrix("out", out, T, m, k)[2]
         self._check(self._L.lqsgd_linear_input_grad(self._h, self._types[T], m, n, k, dz.data_ptr(), lddz, w.data_ptr(), ldw, out.data_ptr(),
@@ -760,7 +761,8 @@ class LinearOps:
 
     def weight_grad(self, dz, x, out=None, dtype=None, accumulate=False):
         """dz^T x^ of the checkpoint x, in float32 or bfloat16 (`dtype`; default: out's, else float32): a gradient for Compressor.step."""
-        self._begin()
+        if self._begin() and out is None:
+            self._no_tangents(dz)
         m, n, lddz = self._matrix("dz", dz)
         if not isinstance(x, Checkpoint):
             raise LqsgdError(EINVAL, "x has to be a Checkpoint")
@@ -773,7 +775,7 @@ class LinearOps:
             dtype, lddw = dtype or self._f32, k
             if dtype not in self._types:
                 raise LqsgdError(EINVAL, "a gradient is not written as %s" % (dtype,))
-            out = self._new((dz,), n, k, dtype=dtype)
+            out = self._empty(n, k, dtype=dtype, device=self.device)
         else:
             lddw = self._matrix("out", out, dtype, n, k)[2]
         self._check(self._L.lqsgd_linear_weight_grad(self._h, self._types[dz.dtype], m, n, k, dz.data_ptr(), lddz, xc, xe,
@@ -795,7 +797,8 @@ class LinearOps:
 
     def dequantize(self, rows, dtype=None, out=None):
         """The tensor that 8-bit rows stand for, in `dtype` (default: out's, else bfloat16)."""
-        self._begin()
+        if self._begin() and out is None:
+            self._no_tangents(getattr(rows, "_scales", None))
         codes, scales = self._rows("rows", rows)
         m, n = rows.samples, rows.features
         new = out is None
@@ -803,12 +806,12 @@ class LinearOps:
             dtype, ld = dtype or self._torch.bfloat16, n
             if dtype not in self._types:
                 raise LqsgdError(EINVAL, "8-bit rows are not read back as %s" % (dtype,))
-            out = self._new((rows._scales,), m, n, dtype=dtype)
+            out = self._empty(m, n, dtype=dtype, device=self.device)
         else:
             ld = self._matrix("out", out, dtype, m, n)[2]
         self._check(self._L.lqsgd_rows_load(self._h, self._types[out.dtype], m, n, codes, scales, out.data_ptr(), ld))
-        if new and rows.needs_grad:
-            return _without_autograd(out, rows.scales)
+        if new and rows._scales is not None and rows._scales.requires_grad:       # of those of empty(): not unless somebody has had them
+            return _without_autograd(out, rows._scales)
         return out
 
     def rms_norm(self, x, gain=None, residual=None, eps=1e-6, h=None, out=None, rstd=None, save_y=None, quantize_y=None, want_h=True,
@@ -816,7 +819,8 @@ class LinearOps:
         """(y, h, rstd): h = x + residual (None without a residual, and where it is not wanted), y = h gain / sqrt(mean h^2 + eps), and
         rstd, which the backward pass needs.  save_y: a Checkpoint that receives y as well; quantize_y: RowCodes that do.  h may be x or the
         residual."""
-        self._begin()
+        if self._begin() and ((h is None and want_h and residual is not None) or (out is None and want_y) or (rstd is None and want_rstd)):
+            self._no_tangents(x, gain, residual)
         m, n, ldx = self._matrix("x", x)
         T = x.dtype
         g = self._vector("gain", gain, T, n) if gain is not None else None
@@ -825,7 +829,7 @@ class LinearOps:
         if residual is not None:
             r, ldr = residual.data_ptr(), self._matrix("residual", residual, T, m, n)[2]
             if new_h and want_h:
-                h, ldh = self._new((x, gain, residual), m, n, dtype=T), n
+                h, ldh = self._empty(m, n, dtype=T, device=self.device), n
                 ph = h.data_ptr()
         if not new_h:
             if residual is None:
@@ -834,10 +838,10 @@ class LinearOps:
         if not new_y:
             py, ldy = out.data_ptr(), self._matrix("out", out, T, m, n)[2]
         elif want_y:
-            out, ldy = self._new((x, gain, residual), m, n, dtype=T), n
+            out, ldy = self._empty(m, n, dtype=T, device=self.device), n
             py = out.data_ptr()
         if new_rstd and want_rstd:
-            rstd = self._new((x, gain, residual), m, dtype=self._f32)
+            rstd = self._empty(m, dtype=self._f32, device=self.device)
         ps = self._vector("rstd", rstd, self._f32, m) if rstd is not None else None
         yc, ye = self._held("save_y", save_y, m, n) if save_y is not None else (None, None)
         qc, qs = self._rows("quantize_y", quantize_y, m, n) if quantize_y is not None else (None, None)
@@ -850,7 +854,8 @@ class LinearOps:
     def rms_norm_backward(self, dy, h, rstd, gain=None, dh=None, dx=None, dgain=None, accumulate=False, want_dx=True, want_dgain=True):
         """(dx, dgain) of dy and of dh, which came to h past the norm: dx is the gradient of rms_norm's x and of its residual alike.  h: the
         tensor that the norm was taken of (x without a residual), or a Checkpoint of it.  What is not wanted is None.  dx may be dy or dh."""
-        self._begin()
+        if self._begin() and ((dx is None and want_dx) or (dgain is None and want_dgain)):
+            self._no_tangents(dy, h, rstd, gain, dh)
         m, n, lddy = self._matrix("dy", dy)
         T = dy.dtype
         t = None if isinstance(h, Checkpoint) else h
@@ -868,12 +873,12 @@ class LinearOps:
         if not new_dx:
             pdx, lddx = dx.data_ptr(), self._matrix("dx", dx, T, m, n)[2]
         elif want_dx:
-            dx, lddx = self._new((dy, t, rstd, gain, dh), m, n, dtype=T), n
+            dx, lddx = self._empty(m, n, dtype=T, device=self.device), n
             pdx = dx.data_ptr()
         if new_dg and want_dgain:
             if accumulate:
                 raise LqsgdError(EINVAL, "accumulate needs the dgain to add to")
-            dgain = self._new((dy, t, rstd, gain, dh), n, dtype=self._f32)
+            dgain = self._empty(n, dtype=self._f32, device=self.device)
         pdg = self._vector("dgain", dgain, self._f32, n) if dgain is not None else None
         self._check(self._L.lqsgd_rms_norm_backward(self._h, self._types[T], m, n, dy.data_ptr(), lddy, ph, ldh, hc, he, ps, g, pdh, lddh,
                                                     pdx, lddx, pdg, 1 if accumulate else 0))
@@ -885,7 +890,8 @@ class LinearOps:
 
     def int8_forward(self, x, w, bias=None, residual=None, act="none", dtype=None, out=None):
         """act(x w^T + bias) + residual of RowCodes x and w, in `dtype` (default: out's, the residual's or the bias', else bfloat16)."""
-        self._begin()
+        if self._begin() and out is None:
+            self._no_tangents(bias, residual, getattr(x, "_scales", None), getattr(w, "_scales", None))
         if act not in ACTS:
             raise LqsgdError(EINVAL, "unknown activation %r" % (act,))
         xc, xs = self._rows("x", x)
@@ -899,12 +905,14 @@ class LinearOps:
         b = self._vector("bias", bias, T, n) if bias is not None else None
         r, ldr = (residual.data_ptr(), self._matrix("residual", residual, T, m, n)[2]) if residual is not None else (None, 0)
         if new:
-            out, ldy = self._new((bias, residual, x._scales, w._scales), m, n, dtype=T), n
+            out, ldy = self._empty(m, n, dtype=T, device=self.device), n
         else:
             ldy = self._matrix("out", out, T, m, n)[2]
         self._check(self._L.lqsgd_int8_forward(self._h, self._types[T], ACTS[act], m, n, k, xc, xs, wc, ws, b, r, ldr, out.data_ptr(), ldy))
-        if new and ((b and bias.requires_grad) or (residual is not None and residual.requires_grad) or x.needs_grad or w.needs_grad):
-            return _without_autograd(out, bias, residual, x.scales, w.scales)
+        sx, sw = x._scales, w._scales
+        if new and ((b and bias.requires_grad) or (residual is not None and residual.requires_grad) or (sx is not None and sx.requires_grad) or
+                    (sw is not None and sw.requires_grad)):
+            return _without_autograd(out, bias, residual, sx, sw)
         return out
 
     def dropout(self, x, p, seed, offset=0, residual=None, out=None, save_y=None, more_offset=None):
@@ -912,7 +920,8 @@ class LinearOps:
         decided by seed, offset (64 bits each) and the place in the tensor: the gradient of x is dropout(dy, p, seed, offset).  out may be x or the
         residual; save_y: a Checkpoint that receives the result as well.  more_offset: an int64 tensor of one element on the device
         that is added to offset when the call runs: a graph that counts it up has another mask at each replay."""
-        self._begin()
+        if self._begin() and out is None:
+            self._no_tangents(x, residual)
         m, n, ldx = self._matrix("x", x)
         T = x.dtype
         if not 0 <= seed < 1 << 64 or not 0 <= offset < 1 << 64:
@@ -926,7 +935,7 @@ class LinearOps:
         new = out is None
         r, ldr = (residual.data_ptr(), self._matrix("residual", residual, T, m, n)[2]) if residual is not None else (None, 0)
         if new:
-            out, ldy = self._new((x, residual), m, n, dtype=T), n
+            out, ldy = self._empty(m, n, dtype=T, device=self.device), n
         else:
             ldy = self._matrix("out", out, T, m, n)[2]
         yc, ye = self._held("save_y", save_y, m, n) if save_y is not None else (None, None)
