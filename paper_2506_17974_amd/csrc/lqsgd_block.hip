@@ -411,7 +411,9 @@ __device__ inline void load_or_ones(float (&g)[kPiece], const void* from, int co
 // columns' gain and sums, and, but for the widest rows, has the next row's values on their way.  dgain: `part`, runs x `stride`, where it is
 // wanted.  dot and sums are fp32: what is added up has been rounded to fp32 once and is of the output's size.
 // Bound by memory: 8192 x 4096 bfloat16 with dh 44 us (6.1 TB/s) without dgain; the runs' sums, 8 MiB, and norm_gain_kernel take 8 more.  Rows of
-// 8193 to 12288 features 68 us (4096 x 11008, 5.3 TB/s; without the next row on its way 76), up to 16384 4.1 TB/s.  Tried: two rows on their way (no gain).
+// 8193 to 12288 features 69 us (4096 x 11008, 5.2 TB/s; without the next row on its way 76), up to 16384 4.5 TB/s, of 4097 to 6144, whose workgroups
+// are two a CU with as many runs, 3.7 to 4 (4096 x 5000 43.8 us, 35.3 without dgain).  From a checkpoint 3.5 to 4.8 (50.5 us, 4096 x 7000 57.4, 47.2 from the
+// tensor): codes by 8 bytes and exponents by one a lane, through the caches.  Tried: two rows on their way (no gain).
 template <typename T, bool HELD, int PIECES, int ROWS, int MOST, bool PAST, bool ENDS = kEnds<T>>
 __global__ __launch_bounds__(MOST, MOST == 768 && PIECES == 1 ? 6 : 1) void norm_backward_kernel(NormBackwardArgs a, float* part, int stride) {
   const int threads = ROWS > 1 ? 64 : (int)blockDim.x, t = ROWS > 1 ? threadIdx.x & 63 : threadIdx.x, n = a.features;
@@ -755,8 +757,8 @@ __device__ inline uint4 philox(uint4 c, uint2 key) {
 }
 
 // A thread takes 16 bytes: 8 values, whose bits are one block of the generator, or in fp32 half of them (two threads make the block: a
-// thread that takes all 8 stores half lines).  Bound by memory: 8192 x 4096 bfloat16 with residual 33.9 us (5.9 TB/s).  A workgroup has a run of 256 such pieces of the whole tensor.  pieces: of a row; whole groups
-// of 32 values where a checkpoint is kept.
+// thread that takes all 8 stores half lines).  Bound by memory: 8192 x 4096 bfloat16 with residual 33.9 us (5.9 TB/s), with a checkpoint too 40.4 (5.8).
+// A workgroup has a run of 256 such pieces of the whole tensor.  pieces: of a row; whole groups of 32 values where a checkpoint is kept.
 template <typename T, bool PAST, bool ENDS>
 __global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a, int64_t row_first, uint32_t pieces) {
   constexpr int N = kWide<T>, kParts = 8 / N, kGroupPieces = kGroup / N;

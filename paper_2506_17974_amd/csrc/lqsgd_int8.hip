@@ -111,8 +111,9 @@ __device__ inline Where where(int tiles_i, int tiles_j, int splits) {
 // A tile of D to a workgroup, operands through LDS in steps of 128 codes.  LDS holds the units (a step of one operand each) of `ahead` steps
 // and the weight's of the step behind them.  A step has two parts, whose products run from registers; the reads of the next part and
 // the fetches are issued among them, a weight's fragment read again as soon as its products are.
-// Bound by the matrix pipes, and those by the card's power: in the loop they are busy 91 % of a workgroup's cycles (about 60 % of the
-// launch's, by the card's counters), and the clock follows the codes: 4096 x 11008 -> 4096 143 us on quantised normal values (2.6 POPS; boxes 130 to 158), 98 us on zeros.  A tile's
+// Bound by the matrix pipes, and those by the card's power: of 4096 x 11008 -> 4096's 231 thousand cycles a workgroup (247 with a residual) 176 are
+// matrix work, 84 % of the loop's 210, on random codes and on zeros alike, and the clock follows the codes: 143 us on quantised normal values at 1.65 to
+// 1.8 GHz (2.6 POPS; cards 130 to 158), 98 us on zeros at 2.25.  A tile's
 // start and end are hidden by no other tile's products (one fits a CU).  8192 x 4096 -> 4096 110 to 116 us, 4096 x 4096 -> 11008 163 (688
 // tiles in 2.7 rounds, paid as 3).  Tried: four wavefronts of 128 x 128 (their fragments go to scratch, slower), four for the 128 x 128 tile (slower).
 template <typename T, typename S>

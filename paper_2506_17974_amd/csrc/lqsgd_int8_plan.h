@@ -26,7 +26,8 @@ struct Int8Plan {
 //   128 x 128   5.5 us + steps (0.33 + 0.2 w), 5.5 us + 2.5 us a further turn + turns steps 0.46 us
 //   256 x 256   1.5 us + turns (10 us + steps (0.93 + 0.57 w))
 // for turns of 256 workgroups, w = the share of the 256 CUs that have a workgroup, and for a sum in parts 1.5 us + 1.1 us a part + 0.25 us a MiB of them.  Fits to
-// the kernels' times over 45 products from 1 x 512 x 512 to 8192 x 4096 x 4096 in bfloat16.  E.g. (us, samples x cols -> rows: few / 64 / 128 / 256)
+// the kernels' times over 45 products from 1 x 512 x 512 to 8192 x 4096 x 4096 in bfloat16; over 63 others its choices are 1 to 3 % above the best kernels'
+// times on average, 36 % at worst (1735 x 6526 -> 18 12.2 us, not 9.0).  E.g. (us, samples x cols -> rows: few / 64 / 128 / 256)
 // 16 x 4096 -> 4096 6.9 / 11.7 / - / -, 64 x 4096 -> 11008 36.8 / 14.1 / 30 / -, 256 x 4096 -> 4096 - / 12.7 / 17.0 / 42,
 // 1024 x 4096 -> 4096 - / 28.5 / 20.6 / 42, 4096 x 11008 -> 4096 - / 297 / 186 / 146; 64 x 11008 -> 4096 in four parts 16.6, whole 28.6.
 // Operands of four steps in LDS leave room for half as many workgroups on a CU: for as many as there is room for, and sums of eight steps or
